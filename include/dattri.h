@@ -756,6 +756,148 @@ dattri_status dattri_token_scores(dattri_ctx* ctx, const void* phi_q, dattri_dty
                                   dattri_dtype phi_dtype, int64_t ld_phi, void* workspace,
                                   size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------- model-side operators */
+
+/* The step of the attributed model that makes the factor blocks: embedding
+ * lookup and its table gradient, linear layers with a fused epilogue and their
+ * backward products, and the gradient norm with clipping.  A linear layer's
+ * input X is the block A that dattri_capture_layer borrows, and the rows that
+ * dattri_linear_input_grad writes are the block B of the layer below, so a
+ * backward pass made of these calls leaves every factor block in place.
+ *
+ * Common to the section: no context; row strides (ld) are in elements, 0 means
+ * dense; products, sums and activations are float32 and every output is
+ * rounded once to its type; all sums have a fixed order (bitwise
+ * reproducible); buffers of one call must not overlap unless said otherwise.
+ * Row strides and widths of any size are accepted; rows on 16 bytes (pointer,
+ * stride and width) are read without a repacking pass.  Row and token counts
+ * of zero are allowed and widths are at least 1; every count and width fits
+ * int32, and 256 rows of every stride stay below 4 GiB. */
+
+/* Embedding lookup with scaling: out[i][:] = scale * table[tokens[i]][:], zeros
+ * where tokens[i] lies outside [0, vocab) (padding).
+ *   table:  device [vocab rows of d] of dtype, rows ld_table apart
+ *   tokens: device [n] integers of token_bytes (4 or 8, signed)
+ *   out:    device [n rows of d] of dtype, rows ld_out apart
+ * Errors: INVALID_ARG (NULL buffer, negative size, d < 1, ld < d, token_bytes),
+ * DTYPE, UNSUPPORTED (a size beyond int32), HIP. */
+dattri_status dattri_embedding(const void* table, int64_t ld_table, int64_t vocab, int64_t d,
+                               dattri_dtype dtype, const void* tokens, int32_t token_bytes,
+                               int64_t n, float scale, void* out, int64_t ld_out, void* stream);
+
+/* Gradient of the table: grad_table[v][:] = scale * sum over i with
+ * tokens[i] == v of grad_out[i][:]; tokens outside [0, vocab) take no part.
+ * The positions are sorted by token on the GPU (stable), then every row is
+ * summed in the order of its positions, long runs in parts.
+ *   grad_out:   device [n rows of d] of dtype, rows ld_grad apart
+ *   grad_table: device float32 [vocab rows of d], rows ld_table apart
+ *   accumulate: 0 writes every row (zeros where no token points), nonzero adds
+ *               to the rows that have tokens and leaves the others untouched
+ *   workspace:  device, >= dattri_embedding_grad_workspace_bytes(...), 256-byte
+ *               aligned
+ * Errors: as dattri_embedding, WORKSPACE. */
+dattri_status dattri_embedding_grad_workspace_bytes(int64_t n, int64_t vocab, int64_t d, size_t* bytes);
+dattri_status dattri_embedding_grad(const void* grad_out, int64_t ld_grad, dattri_dtype dtype,
+                                    const void* tokens, int32_t token_bytes, int64_t n, float scale,
+                                    int64_t vocab, int64_t d, float* grad_table, int64_t ld_table,
+                                    int32_t accumulate, void* workspace, size_t ws_bytes, void* stream);
+
+/* Activation of a linear layer's epilogue: identity, max(z, 0), z Phi(z) (the
+ * normal distribution function), its tanh form
+ * z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))), z / (1 + exp(-z)).
+ * relu's slope at 0 is 0. */
+typedef DATTRI_ENUM {
+  DATTRI_ACT_NONE = 0,
+  DATTRI_ACT_RELU = 1,
+  DATTRI_ACT_GELU = 2,
+  DATTRI_ACT_GELU_TANH = 3,
+  DATTRI_ACT_SILU = 4
+} dattri_act;
+
+typedef DATTRI_ENUM {
+  DATTRI_LINEAR_FORWARD = 0,    /* dattri_linear */
+  DATTRI_LINEAR_INPUT_GRAD = 1, /* dattri_linear_input_grad */
+  DATTRI_LINEAR_WEIGHT_GRAD = 2 /* dattri_linear_weight_grad */
+} dattri_linear_op;
+
+/* Device bytes of workspace a call of `op` needs (0 is possible).  aligned:
+ * nonzero if both operands of the product have 16-byte aligned pointers and
+ * row strides of a multiple of 16 bytes (with 0 the size is enough for either).
+ * Errors: INVALID_ARG, DTYPE, UNSUPPORTED. */
+dattri_status dattri_linear_workspace_bytes(dattri_linear_op op, int64_t rows, int64_t d_in,
+                                            int64_t d_out, dattri_dtype dtype, int32_t aligned,
+                                            size_t* bytes);
+
+/* Linear layer with bias, activation and residual in the product's epilogue:
+ *   Z = X W^T + bias,  Y = act(Z) + R.
+ *   X: device [rows of d_in], W: device [d_out rows of d_in], bias: NULL or
+ *   device [d_out], R: NULL or device [rows of d_out], Y: device [rows of
+ *   d_out], Z: NULL or device [rows of d_out] (kept for the backward pass);
+ *   all of dtype.  Y may be R itself (same stride).
+ *   workspace: >= dattri_linear_workspace_bytes(FORWARD, ...), 256-byte
+ *   aligned; NULL where that is 0.
+ * Errors: INVALID_ARG, DTYPE, WORKSPACE, UNSUPPORTED, HIP. */
+dattri_status dattri_linear(const void* X, int64_t ld_x, const void* W, int64_t ld_w, const void* bias,
+                            dattri_act act, const void* R, int64_t ld_r, void* Y, int64_t ld_y, void* Z,
+                            int64_t ld_z, int64_t rows, int64_t d_in, int64_t d_out, dattri_dtype dtype,
+                            void* workspace, size_t ws_bytes, void* stream);
+
+/* Gradient of a linear layer's input, with the derivative of the activation
+ * that made that input in the epilogue:
+ *   D = G W + R,  P = D * act'(Z).
+ * G is the gradient of the layer's pre-activation (its factor block B), R the
+ * gradient that reaches the input by other ways (a residual path), Z the
+ * pre-activation of the layer below; P is then the factor block B of that
+ * layer.
+ *   G: device [rows of d_out], W: device [d_out rows of d_in], R: NULL or
+ *   device [rows of d_in], Z: device [rows of d_in] (NULL if P is, or with
+ *   DATTRI_ACT_NONE), D, P: device [rows of d_in], either may be NULL but not
+ *   both; all of dtype.  D or P may be R itself, P may be Z (same stride).
+ *   workspace: as above for INPUT_GRAD.
+ * Errors: as dattri_linear. */
+dattri_status dattri_linear_input_grad(const void* G, int64_t ld_g, const void* W, int64_t ld_w,
+                                       const void* R, int64_t ld_r, dattri_act act, const void* Z,
+                                       int64_t ld_z, void* D, int64_t ld_d, void* P, int64_t ld_p,
+                                       int64_t rows, int64_t d_in, int64_t d_out, dattri_dtype dtype,
+                                       void* workspace, size_t ws_bytes, void* stream);
+
+/* Gradients of a linear layer's weight and bias, float32 whatever dtype is:
+ *   dW = G^T X,  dbias = sum over rows of G   (added to what is there if
+ *   accumulate is nonzero).
+ *   G: device [rows of d_out], X: device [rows of d_in] of dtype; dW: device
+ *   float32 [d_out rows of d_in], rows ld_dw apart; dbias: device float32
+ *   [d_out]; either output may be NULL but not both.
+ *   workspace: as above for WEIGHT_GRAD.
+ * Errors: as dattri_linear. */
+dattri_status dattri_linear_weight_grad(const void* G, int64_t ld_g, const void* X, int64_t ld_x,
+                                        float* dW, int64_t ld_dw, float* dbias, int32_t accumulate,
+                                        int64_t rows, int64_t d_in, int64_t d_out, dattri_dtype dtype,
+                                        void* workspace, size_t ws_bytes, void* stream);
+
+/* Norm of many gradients together, and clipping to a largest norm:
+ *   norm = sqrt(sum over tensors and elements of g^2)   (float64 sums),
+ *   coef = min(1, max_norm / (norm + 1e-6)),  out = coef * g.
+ *   grads:      host array of n_tensors device pointers (contiguous elements,
+ *               aligned to their type); NULL allowed where the size is 0
+ *   sizes:      host array of element counts (any, also 0)
+ *   dtypes:     host array, F32 or BF16 per tensor
+ *   outs:       NULL (norm only) or host array of device pointers; outs[i] may
+ *               be grads[i] itself (in place, same type): such a tensor is not
+ *               written when coef is 1.  Other overlaps are not allowed.
+ *   out_dtypes: host array, F32 or BF16 per tensor; NULL with outs NULL
+ *   norm_coef:  device float32 [2]: norm, coef
+ *   max_norm:   >= 0, infinity allowed (coef 1)
+ *   workspace:  device, >= dattri_clip_workspace_bytes(sizes, n_tensors), 256-byte
+ *               aligned
+ * The host arrays are read before the call returns.  Infinities and NaN follow
+ * the formulas: an infinite norm gives coef 0, a NaN a NaN coef.
+ * Errors: INVALID_ARG, DTYPE, WORKSPACE, HIP. */
+dattri_status dattri_clip_workspace_bytes(const int64_t* sizes, int64_t n_tensors, size_t* bytes);
+dattri_status dattri_clip_gradients(const void* const* grads, const int64_t* sizes,
+                                    const dattri_dtype* dtypes, void* const* outs,
+                                    const dattri_dtype* out_dtypes, int64_t n_tensors, float max_norm,
+                                    float* norm_coef, void* workspace, size_t ws_bytes, void* stream);
+
 /* ------------------------------------------------------ measurement probes */
 
 /* Measured roofline denominators (not part of the method): the rates a kernel

@@ -36,6 +36,11 @@ __all__ = [
     "dattri_cosine_workspace_bytes", "dattri_score_cosine",
     "DATTRI_ROUTE_MASK", "dattri_register_mask_layer", "dattri_get_mask",
     "dattri_token_scores_workspace_bytes", "dattri_token_scores",
+    "dattri_embedding", "dattri_embedding_grad", "dattri_embedding_grad_workspace_bytes",
+    "DATTRI_ACT_NONE", "DATTRI_ACT_RELU", "DATTRI_ACT_GELU", "DATTRI_ACT_GELU_TANH", "DATTRI_ACT_SILU",
+    "DATTRI_LINEAR_FORWARD", "DATTRI_LINEAR_INPUT_GRAD", "DATTRI_LINEAR_WEIGHT_GRAD",
+    "dattri_linear_workspace_bytes", "dattri_linear", "dattri_linear_input_grad", "dattri_linear_weight_grad",
+    "dattri_clip_workspace_bytes", "dattri_clip_gradients",
     "dattri_probe_read", "dattri_probe_mfma",
 ]
 
@@ -44,6 +49,8 @@ DATTRI_ROUTE_AUTO, DATTRI_ROUTE_FACTORED, DATTRI_ROUTE_MATERIALIZED, DATTRI_ROUT
 DATTRI_FORM_AUTO, DATTRI_FORM_FUSED, DATTRI_FORM_SPLIT = 0, 1, 2
 DATTRI_CURV_KFAC, DATTRI_CURV_EKFAC = 0, 1
 DATTRI_MAP_GAUSSIAN, DATTRI_MAP_RADEMACHER = 0, 1
+DATTRI_ACT_NONE, DATTRI_ACT_RELU, DATTRI_ACT_GELU, DATTRI_ACT_GELU_TANH, DATTRI_ACT_SILU = 0, 1, 2, 3, 4
+DATTRI_LINEAR_FORWARD, DATTRI_LINEAR_INPUT_GRAD, DATTRI_LINEAR_WEIGHT_GRAD = 0, 1, 2
 STATUS_NAMES = {0: "OK", -1: "E_INVALID_ARG", -2: "E_SHAPE", -3: "E_DTYPE", -4: "E_STATE",
                 -5: "E_WORKSPACE", -6: "E_HIP", -7: "E_UNSUPPORTED"}
 
@@ -79,7 +86,7 @@ class CurvatureLayout(ctypes.Structure):
 
 
 _i32, _i64, _u64, _sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_size_t
-_vp, _dbl = ctypes.c_void_p, ctypes.c_double
+_vp, _dbl, _flt = ctypes.c_void_p, ctypes.c_double, ctypes.c_float
 _P = ctypes.POINTER
 
 # name -> (restype, argtypes); the complete exported C ABI.
@@ -137,6 +144,19 @@ _SIGS = {
     "dattri_get_mask": (_i32, [_vp, _i32, _vp, _vp]),
     "dattri_token_scores_workspace_bytes": (_i32, [_vp, _P(_sz)]),
     "dattri_token_scores": (_i32, [_vp, _vp, _i32, _i64, _i64, _vp, _vp, _i32, _i64, _vp, _sz, _vp]),
+    "dattri_embedding": (_i32, [_vp, _i64, _i64, _i64, _i32, _vp, _i32, _i64, _flt, _vp, _i64, _vp]),
+    "dattri_embedding_grad_workspace_bytes": (_i32, [_i64, _i64, _i64, _P(_sz)]),
+    "dattri_embedding_grad": (_i32, [_vp, _i64, _i32, _vp, _i32, _i64, _flt, _i64, _i64, _vp, _i64, _i32, _vp, _sz,
+                                     _vp]),
+    "dattri_linear_workspace_bytes": (_i32, [_i32, _i64, _i64, _i64, _i32, _i32, _P(_sz)]),
+    "dattri_linear": (_i32, [_vp, _i64, _vp, _i64, _vp, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _i64, _i64, _i64, _i32,
+                             _vp, _sz, _vp]),
+    "dattri_linear_input_grad": (_i32, [_vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _i64,
+                                        _i64, _i64, _i32, _vp, _sz, _vp]),
+    "dattri_linear_weight_grad": (_i32, [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _i32, _i64, _i64, _i64, _i32, _vp, _sz,
+                                         _vp]),
+    "dattri_clip_workspace_bytes": (_i32, [_vp, _i64, _P(_sz)]),
+    "dattri_clip_gradients": (_i32, [_vp, _vp, _vp, _vp, _vp, _i64, _flt, _vp, _vp, _sz, _vp]),
     "dattri_probe_read": (_i32, [_vp, _sz, _vp, _i32, _vp]),
     "dattri_probe_mfma": (_i32, [_vp, _i32, _i32, _P(_dbl), _vp]),
     "dattri_cosine_workspace_bytes": (_i32, [_i64, _i64, _i64, _i32, _i32, _i32, _i32, _P(_sz)]),
@@ -183,6 +203,11 @@ def _ptr(x):
     if hasattr(x, "ctypes"):
         return x.ctypes.data
     raise TypeError(f"cannot take a pointer of {type(x)}")
+
+
+def _host(x):
+    """Address of a host array (ctypes or numpy), or None."""
+    return ctypes.addressof(x) if isinstance(x, ctypes.Array) else _ptr(x)
 
 
 def _stream(s):
@@ -548,6 +573,68 @@ def dattri_token_scores(ctx, phi_q, q_dtype, n_q, ld_q, scores, phi, phi_dtype, 
     _check(load().dattri_token_scores(ctx, _ptr(phi_q), q_dtype, n_q, ld_q, _ptr(scores), _ptr(phi), phi_dtype,
                                       ld_phi, _ptr(workspace), ws_bytes, _stream(stream)),
            "dattri_token_scores")
+
+
+def dattri_embedding(table, ld_table, vocab, d, dtype, tokens, token_bytes, n, scale, out, ld_out, stream=None):
+    _check(load().dattri_embedding(_ptr(table), ld_table, vocab, d, dtype, _ptr(tokens), token_bytes, n, scale,
+                                   _ptr(out), ld_out, _stream(stream)), "dattri_embedding")
+
+
+def dattri_embedding_grad_workspace_bytes(n, vocab, d):
+    v = _sz()
+    _check(load().dattri_embedding_grad_workspace_bytes(n, vocab, d, ctypes.byref(v)),
+           "dattri_embedding_grad_workspace_bytes")
+    return v.value
+
+
+def dattri_embedding_grad(grad_out, ld_grad, dtype, tokens, token_bytes, n, scale, vocab, d, grad_table, ld_table,
+                          accumulate, workspace, ws_bytes, stream=None):
+    _check(load().dattri_embedding_grad(_ptr(grad_out), ld_grad, dtype, _ptr(tokens), token_bytes, n, scale, vocab, d,
+                                        _ptr(grad_table), ld_table, int(bool(accumulate)), _ptr(workspace), ws_bytes,
+                                        _stream(stream)), "dattri_embedding_grad")
+
+
+def dattri_linear_workspace_bytes(op, rows, d_in, d_out, dtype, aligned=False):
+    v = _sz()
+    _check(load().dattri_linear_workspace_bytes(op, rows, d_in, d_out, dtype, int(bool(aligned)), ctypes.byref(v)),
+           "dattri_linear_workspace_bytes")
+    return v.value
+
+
+def dattri_linear(X, ld_x, W, ld_w, bias, act, R, ld_r, Y, ld_y, Z, ld_z, rows, d_in, d_out, dtype, workspace,
+                  ws_bytes, stream=None):
+    _check(load().dattri_linear(_ptr(X), ld_x, _ptr(W), ld_w, _ptr(bias), act, _ptr(R), ld_r, _ptr(Y), ld_y, _ptr(Z),
+                                ld_z, rows, d_in, d_out, dtype, _ptr(workspace), ws_bytes, _stream(stream)),
+           "dattri_linear")
+
+
+def dattri_linear_input_grad(G, ld_g, W, ld_w, R, ld_r, act, Z, ld_z, D, ld_d, P, ld_p, rows, d_in, d_out, dtype,
+                             workspace, ws_bytes, stream=None):
+    _check(load().dattri_linear_input_grad(_ptr(G), ld_g, _ptr(W), ld_w, _ptr(R), ld_r, act, _ptr(Z), ld_z, _ptr(D),
+                                           ld_d, _ptr(P), ld_p, rows, d_in, d_out, dtype, _ptr(workspace), ws_bytes,
+                                           _stream(stream)), "dattri_linear_input_grad")
+
+
+def dattri_linear_weight_grad(G, ld_g, X, ld_x, dW, ld_dw, dbias, accumulate, rows, d_in, d_out, dtype, workspace,
+                              ws_bytes, stream=None):
+    _check(load().dattri_linear_weight_grad(_ptr(G), ld_g, _ptr(X), ld_x, _ptr(dW), ld_dw, _ptr(dbias),
+                                            int(bool(accumulate)), rows, d_in, d_out, dtype, _ptr(workspace), ws_bytes,
+                                            _stream(stream)), "dattri_linear_weight_grad")
+
+
+def dattri_clip_workspace_bytes(sizes, n_tensors):
+    """sizes: a ctypes or numpy int64 array."""
+    v = _sz()
+    _check(load().dattri_clip_workspace_bytes(_host(sizes), n_tensors, ctypes.byref(v)), "dattri_clip_workspace_bytes")
+    return v.value
+
+
+def dattri_clip_gradients(grads, sizes, dtypes, outs, out_dtypes, n_tensors, max_norm, norm_coef, workspace, ws_bytes,
+                          stream=None):
+    """grads, outs: ctypes or numpy arrays of device addresses; sizes int64, dtypes int32 likewise."""
+    _check(load().dattri_clip_gradients(_host(grads), _host(sizes), _host(dtypes), _host(outs), _host(out_dtypes),
+                                        n_tensors, max_norm, _ptr(norm_coef), _ptr(workspace), ws_bytes,
+                                        _stream(stream)), "dattri_clip_gradients")
 
 
 def dattri_probe_read(buf, nbytes, sink, workgroups, stream=None):

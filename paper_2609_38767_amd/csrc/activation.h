@@ -1,0 +1,76 @@
+// Activations of the linear layers' epilogue and their slopes, in float32.
+//
+// gelu(z) = z Phi(z) with Phi(z) = (1 + erf(z / sqrt 2)) / 2;
+// its tanh form equals z s(2u), s the logistic function,
+// u = sqrt(2/pi) (z + 0.044715 z^3), since (1 + tanh u) / 2 = s(2u);
+// silu(z) = z s(z).  ELT 2 (bf16 results) takes the hardware's exp2 and
+// reciprocal, off by a few 2^-23; ELT 4 the library functions and a division.
+// s is formed from exp(-|x|), which cannot overflow; a factor that has reached
+// zero ends its product, so infinite z and finite z whose cube overflows give
+// the limits (0 or z, slopes 0 or 1) and not 0 * inf.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "dattri.h"
+
+namespace dattri {
+namespace dev {
+
+constexpr float kSqrt2OverPi = 0.7978845608028654f, kGeluCubic = 0.044715f, kSqrtHalf = 0.7071067811865476f,
+                kInvSqrt2Pi = 0.3989422804014327f;
+
+template <int ELT>
+__device__ inline float exp_of(float x) {
+  if constexpr (ELT == 2) return __builtin_amdgcn_exp2f(x * 1.4426950408889634f);
+  return expf(x);
+}
+// 1 / (1 + exp(-x))
+template <int ELT>
+__device__ inline float logistic(float x) {
+  const float e = exp_of<ELT>(-fabsf(x));
+  const float r = ELT == 2 ? __builtin_amdgcn_rcpf(1.f + e) : 1.f / (1.f + e);
+  return x < 0.f ? e * r : r;
+}
+
+// z * w with w = 0 winning over an infinite z
+__device__ inline float decayed(float z, float w) { return w == 0.f ? 0.f : z * w; }
+
+template <int ELT>
+__device__ inline float act_value(float z, int act) {
+  switch (act) {
+    case DATTRI_ACT_RELU:
+      return z < 0.f ? 0.f : z;  // NaN stays
+    case DATTRI_ACT_GELU:
+      return decayed(z, 0.5f * erfcf(-z * kSqrtHalf));
+    case DATTRI_ACT_GELU_TANH:
+      return decayed(z, logistic<ELT>(2.f * kSqrt2OverPi * (z + kGeluCubic * z * z * z)));
+    case DATTRI_ACT_SILU:
+      return decayed(z, logistic<ELT>(z));
+    default:
+      return z;
+  }
+}
+
+template <int ELT>
+__device__ inline float act_slope(float z, int act) {
+  switch (act) {
+    case DATTRI_ACT_RELU:
+      return z <= 0.f ? 0.f : 1.f;
+    case DATTRI_ACT_GELU:
+      return 0.5f * erfcf(-z * kSqrtHalf) + decayed(z, kInvSqrt2Pi * exp_of<ELT>(-0.5f * z * z));
+    case DATTRI_ACT_GELU_TANH: {  // s(2u) + z 2u' s(2u) (1 - s(2u))
+      const float x = 2.f * kSqrt2OverPi * (z + kGeluCubic * z * z * z), s = logistic<ELT>(x), t = logistic<ELT>(-x);
+      return s + decayed(z * (2.f * kSqrt2OverPi * (1.f + 3.f * kGeluCubic * z * z)), s * t);
+    }
+    case DATTRI_ACT_SILU: {
+      const float s = logistic<ELT>(z), t = logistic<ELT>(-z);
+      return s + decayed(z, s * t);
+    }
+    default:
+      return 1.f;
+  }
+}
+
+}  // namespace dev
+}  // namespace dattri
