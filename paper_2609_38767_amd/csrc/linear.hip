@@ -1,126 +1,580 @@
-// Linear layers with a fused epilogue and their backward products.
+// Linear layers with a fused epilogue and their backward products:
+//   C[m][n] = sum_k A(m, k) B(n, k), then epilogue4.
+//
+// Tile kernel.  Four waves (one per SIMD) each own BI x BJ blocks of 32 x 32
+// outputs; the blocks' rows run along n and their columns along m, so a lane
+// holds four neighbouring n of one m.  bf16 products are
+// v_mfma_f32_32x32x16_bf16, float32 ones v_mfma_f32_32x32x2f32.  Operands come
+// to LDS by direct loads (16 bytes per lane) in stages of 128 bytes of k (64
+// bf16, 32 float32), in the order they have in memory:
+//   k contiguous: [row][128 bytes], 16-byte chunks XORed by row % 8; a fragment
+//     is one 16-byte read per lane: 8 bf16, or 4 float32 that serve four MFMA
+//     (slot j of half-wave h is k = 4h + j for both operands);
+//   k strided: [k][row], read across with the transposing LDS read (bf16) or
+//     by 4-byte reads of 32 neighbouring rows (float32); chunks XORed by k so
+//     that the k rows of one read lie in different banks.
+// Two stage buffers.  A stage's four K steps are read two steps ahead of their
+// products, so halfway through a stage all of it is in registers; the one
+// barrier per stage sits there, behind it the buffer takes the loads of the
+// stage after next, which then have a whole stage of products to arrive.
+//
+// Rows past M or N repeat the last row (their outputs are not stored); k past K
+// reads as zero on both sides, so no product meets what lies behind a row.
+//
+// The accumulators leave through LDS, 32 columns of blocks at a time as float32
+// rows, so that the epilogue is one short loop over whole rows: its loads and
+// stores of Z, R and the outputs are contiguous per wave.
 #include <algorithm>
 
-#include "activation.h"
 #include "api_common.h"
 #include "device_common.h"
+#include "epilogue.h"
+#include "internal.h"
 #include "model_ops.h"
 
 namespace dattri {
 using namespace dev;
 
-template <int ELT>
-__device__ inline float load_elt(const void* p, int64_t i) {
-  return ELT == 2 ? bf16_bits_to_f32(((const uint16_t*)p)[i]) : ((const float*)p)[i];
+namespace {
+
+constexpr int kPartial = 3;  // epilogue of a split product: float32 partial tile
+
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+
+__device__ inline void wait_all() {  // this wave's loads are in LDS, its LDS reads done
+  __builtin_amdgcn_s_waitcnt(0x70);  // vmcnt 0, lgkmcnt 0, other counters untouched
 }
-template <int ELT>
-__device__ inline void store_elt(void* p, int64_t i, float v) {
-  if (ELT == 2)
-    ((uint16_t*)p)[i] = (uint16_t)pack_bf16(v, 0.f);
-  else
-    ((float*)p)[i] = v;
+__device__ inline void stage_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+__device__ inline void direct_load(rsrc_t r, uint8_t* lds, uint32_t off) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, DATTRI_LDS_PTR(lds), 16, off, 0, 0, 0);
 }
 
-// What becomes of the product's element (m, n).
-template <int OP, int ELT>
-__device__ inline void epilogue_one(const GemmArgs& a, int m, int n, float v) {
-  if constexpr (OP == DATTRI_LINEAR_FORWARD) {
-    if (a.bias) v += load_elt<ELT>(a.bias, n);
-    if (a.Z) store_elt<ELT>(a.Z, m * a.ldz + n, v);
-    v = act_value<ELT>(v, a.act);
-    if (a.R) v += load_elt<ELT>(a.R, m * a.ldr + n);
-    store_elt<ELT>(a.out, m * a.ldo + n, v);
-  } else if constexpr (OP == DATTRI_LINEAR_INPUT_GRAD) {
-    if (a.R) v += load_elt<ELT>(a.R, m * a.ldr + n);
-    const float slope = a.out2 && a.act != DATTRI_ACT_NONE ? act_slope<ELT>(load_elt<ELT>(a.Z, m * a.ldz + n), a.act)
-                                                            : 1.f;
-    if (a.out) store_elt<ELT>(a.out, m * a.ldo + n, v);
-    if (a.out2) store_elt<ELT>(a.out2, m * a.ldo2 + n, a.act == DATTRI_ACT_RELU ? (slope == 0.f ? 0.f : v) : v * slope);
-  } else {
-    float* o = (float*)a.out + m * a.ldo + n;
-    *o = a.accumulate ? *o + v : v;
-  }
+// Transposing LDS read: lane 4r + c of every 16 addresses four bf16 of k row r,
+// lane j receives the four k of column j.
+__device__ inline i16x4 read_across(const uint8_t* p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)p);
 }
 
-// 64 x 64 tile, 256 threads of 4 x 4 outputs, float32 products, K in steps of 16
-// staged in LDS as float32.
-template <int OP, int ELT>
-__global__ __launch_bounds__(256) void gemm_simple_kernel(GemmArgs a, int tiles_n) {
-  constexpr bool kAc = OP != DATTRI_LINEAR_WEIGHT_GRAD, kBc = OP == DATTRI_LINEAR_FORWARD;
-  __shared__ float sa[16][65], sb[16][65];
-  const int m0 = (int)(blockIdx.x / tiles_n) * 64, n0 = (int)(blockIdx.x % tiles_n) * 64;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  float acc[4][4] = {};
-  auto fill = [&](const void* P, int64_t ld, bool kc, int r0, int rows, int k0, float (&s)[16][65]) {
-    for (int i = threadIdx.x; i < 1024; i += 256) {
-      const int r = kc ? i >> 4 : i & 63, k = kc ? i & 15 : i >> 6;
-      float v = 0.f;
-      if (r0 + r < rows && k0 + k < a.K)
-        v = load_elt<ELT>(P, kc ? (int64_t)(r0 + r) * ld + k0 + k : (int64_t)(k0 + k) * ld + r0 + r);
-      s[k][r] = v;
-    }
-  };
-  for (int k0 = 0; k0 < a.K; k0 += 16) {
-    fill(a.A, a.lda, kAc, m0, a.M, k0, sa);
-    fill(a.B, a.ldb, kBc, n0, a.N, k0, sb);
-    __syncthreads();
+// One operand's share of a tile: R rows (of the operand's own index) of which
+// `rows` exist, k contiguous (KC) or strided.
+template <int ELT, bool KC, int R>
+struct Side {
+  static constexpr int EPL = 16 / ELT, BK = 128 / ELT;  // elements per chunk, k per stage
+  static constexpr int kBytes = R * 128;                // of a stage
+  static constexpr int kLoads = R / 32;                 // direct loads per wave and stage
+  static constexpr int CH = R * ELT / 16;               // chunks per k row (strided)
+  static constexpr int kReads = KC ? 1 : ELT == 2 ? 2 : 4;  // LDS reads per fragment
+
+  const uint8_t* base;  // the tile's first row (KC) or column (strided) at k = 0
+  int64_t ld;           // bytes
+  int rows, K;
+  rsrc_t rs;         // KC: the tile's rows
+  uint32_t off[kLoads];  // KC: this lane's chunk of each load at k = 0 of the stage; strided: from the stage's first k row
+  int kc;            // KC: k of this lane's chunk within the stage
+
+  __device__ static int swz(int k) { return ELT == 2 ? 2 * (k & 3) + 8 * (k & 1) : 8 * ((k >> 2) & 1); }
+
+  __device__ void init(const void* p, int64_t ld_elts, int row0, int n_rows, int K_, int wave, int lane) {
+    ld = ld_elts * ELT;
+    rows = min(R, n_rows - row0);
+    K = K_;
+    if constexpr (KC) {
+      base = (const uint8_t*)p + (int64_t)row0 * ld;
+      // rows are whole 16-byte chunks (repacked rows end in zeros)
+      rs = make_rsrc(base, (uint32_t)((int64_t)(rows - 1) * ld + ((int64_t)K * ELT + 15) / 16 * 16));
+      const int r8 = lane >> 3;
+      kc = ((lane & 7) ^ r8) * EPL;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-      float x[4], y[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        x[i] = sa[k][4 * ty + i];
-        y[i] = sb[k][tx + 16 * i];
+      for (int j = 0; j < kLoads; ++j) {
+        const int row = min((wave * kLoads + j) * 8 + r8, rows - 1);
+        off[j] = (uint32_t)((int64_t)row * ld + kc * ELT);
       }
+    } else {
+      base = (const uint8_t*)p + (int64_t)row0 * ELT;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(x[i], y[j], acc[i][j]);
+      for (int j = 0; j < kLoads; ++j) {
+        const int slot = (wave * kLoads + j) * 64 + lane, k = slot / CH, c = slot % CH;
+        off[j] = (uint32_t)((int64_t)k * ld + ((c ^ (swz(k) & (CH - 1))) << 4));
+      }
     }
-    __syncthreads();
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int m = m0 + 4 * ty + i, n = n0 + tx + 16 * j;
-      if (m < a.M && n < a.N) epilogue_one<OP, ELT>(a, m, n, acc[i][j]);
+
+  // The direct loads of stage st into `buf` (this side's part of a stage buffer).
+  __device__ void load(int st, uint8_t* buf, int wave, int j) const {
+    uint8_t* d = buf + (wave * kLoads + j) * 1024;
+    if constexpr (KC) {
+      const int k0 = st * BK;
+      const uint32_t o = k0 + kc < K ? off[j] + (uint32_t)k0 * ELT : kOOB;
+      direct_load(rs, d, o);
+    } else {
+      const int64_t left = K - (int64_t)st * BK;  // k rows that exist from here on; none: an empty range
+      const int64_t bytes = left > 0 ? (min(left, (int64_t)BK) - 1) * ld + ((int64_t)rows * ELT + 15) / 16 * 16 : 0;
+      direct_load(make_rsrc(base + (int64_t)st * BK * ld, (uint32_t)bytes), d, off[j]);
     }
+  }
+
+  // Fragment of K step s of the 32-row block at row w0 + 32 i: lane l holds row
+  // l % 32 and the step's k of half-wave l / 32.
+  template <int NB>
+  __device__ static void read(const uint8_t* buf, int s, int w0, int lane, i32x4 (&f)[NB]) {
+    const int l32 = lane & 31, h = lane >> 5;
+    if constexpr (KC) {
+      const uint8_t* p = buf + (w0 + l32) * 128 + (((2 * s + h) ^ (l32 & 7)) << 4);
+#pragma unroll
+      for (int i = 0; i < NB; ++i) f[i] = *(const i32x4*)(p + i * 4096);
+    } else if constexpr (ELT == 2) {
+      const int q = lane >> 4, rr = (lane >> 2) & 3, aa = lane & 3;
+      const uint8_t* p = buf + (16 * s + 8 * (q >> 1) + rr) * (CH * 16) + (aa & 1) * 8;
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        const int c = (w0 >> 3) + 4 * i + 2 * (q & 1) + (aa >> 1);
+        const uint8_t* a = p + ((c ^ (swz(rr) & (CH - 1))) << 4);
+        const i16x4 lo = read_across(a), hi = read_across(a + 4 * CH * 16);
+        const i32x2 x = __builtin_bit_cast(i32x2, lo), y = __builtin_bit_cast(i32x2, hi);
+        f[i] = i32x4{x.x, x.y, y.x, y.y};
+      }
+    } else {
+      const uint8_t* p = buf + (8 * s + 4 * h) * (CH * 16) + (l32 & 3) * 4;
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        const int c = (w0 >> 2) + 8 * i + (l32 >> 2);
+        const uint8_t* a = p + ((c ^ ((8 * h) & (CH - 1))) << 4);
+        f[i] = i32x4{*(const int*)a, *(const int*)(a + CH * 16), *(const int*)(a + 2 * CH * 16),
+                     *(const int*)(a + 3 * CH * 16)};
+      }
+    }
+  }
+};
+
+template <int ELT, int BN, int BM>
+__device__ inline void step_mma(const i32x4 (&b)[BN], const i32x4 (&a)[BM], f32x16 (&acc)[BN][BM]) {
+  if constexpr (ELT == 2) {
+#pragma unroll
+    for (int i = 0; i < BN; ++i)
+#pragma unroll
+      for (int j = 0; j < BM; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b[i]),
+                                                           __builtin_bit_cast(bf16x8, a[j]), acc[i][j], 0, 0, 0);
+  } else {
+    f32x4 fb[BN], fa[BM];
+#pragma unroll
+    for (int i = 0; i < BN; ++i) fb[i] = __builtin_bit_cast(f32x4, b[i]);
+#pragma unroll
+    for (int j = 0; j < BM; ++j) fa[j] = __builtin_bit_cast(f32x4, a[j]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int i = 0; i < BN; ++i)
+#pragma unroll
+        for (int j = 0; j < BM; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(fb[i][e], fa[j][e], acc[i][j], 0, 0, 0);
+  }
 }
 
-// One thread per column, rows in order.
+// Deals a step's LDS reads (first half) and direct loads (second half) out
+// between its MFMA.
+template <int BLOCKS, int READS, int LOADS, int I = 0>
+__device__ inline void spread() {
+  constexpr int kFirst = (BLOCKS + 1) / 2, kRest = BLOCKS - kFirst;
+  if constexpr (I < BLOCKS) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    if constexpr (I < kFirst) {
+      constexpr int n = READS * (I + 1) / kFirst - READS * I / kFirst;
+      if constexpr (n > 0) __builtin_amdgcn_sched_group_barrier(0x100, n, 0);
+    } else {
+      constexpr int n = LOADS * (I - kFirst + 1) / kRest - LOADS * (I - kFirst) / kRest;
+      if constexpr (n > 0) __builtin_amdgcn_sched_group_barrier(0x020, n, 0);
+    }
+    spread<BLOCKS, READS, LOADS, I + 1>();
+  }
+}
+
+// Tile (mt, nt) of launch index b: every XCD takes a contiguous run of tiles,
+// groups of kGroup tile rows walked along n, so the tiles an XCD works on at
+// once share their operands in its L2.
+constexpr int kGroup = 8;
+__device__ inline void tile_of(int b, int nm, int nn, int* mt, int* nt) {
+  const int nb = nm * nn, n_full = nb / kXcds * kXcds;
+  const int L = b < n_full ? (b % kXcds) * (n_full / kXcds) + b / kXcds : b;
+  const int g = L / (kGroup * nn), m_first = g * kGroup, gm = min(kGroup, nm - m_first);
+  const int r = L - g * kGroup * nn;
+  *mt = m_first + r % gm;
+  *nt = r / gm;
+}
+
+}  // namespace
+
+// WM x WN waves; BM x BN blocks of 32 x 32 each.  Grid (tiles, splits of k):
+// split y runs stages [y * sps, min((y + 1) * sps, all)); with several splits
+// (OP kPartial) part holds them as [split][M][ld_part].
+template <int OP, bool AC, bool BC, int ELT, int WM, int WN, int BM, int BN>
+__global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void gemm_kernel(GemmArgs a, int nm, int nn, int sps,
+                                                                          float* __restrict__ part, int64_t ld_part) {
+  static_assert(WM * WN == 4, "four waves");
+  constexpr int TM = WM * BM * 32, TN = WN * BN * 32;
+  typedef Side<ELT, AC, TM> SA;
+  typedef Side<ELT, BC, TN> SB;
+  constexpr int kStage = SA::kBytes + SB::kBytes;
+  constexpr int kSlab = WM * 32 * TN * 4;  // epilogue: one block column of every wave
+  constexpr int kBuf = kStage > kSlab ? kStage : kSlab;
+  __shared__ __align__(1024) uint8_t x0[kBuf], x1[kBuf];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / WN, wn = wave % WN;
+  int mt, nt;
+  tile_of(blockIdx.x, nm, nn, &mt, &nt);
+  const int m0 = mt * TM, n0 = nt * TN;
+  SA sa;
+  SB sb;
+  const int all = (int)(((int64_t)a.K + SA::BK - 1) / SA::BK), s0 = blockIdx.y * sps, ns = min(sps, all - s0);
+  const int k_end = (int)min((int64_t)a.K, (int64_t)(s0 + ns) * SA::BK);
+  sa.init(a.A, a.lda, m0, a.M, k_end, wave, lane);
+  sb.init(a.B, a.ldb, n0, a.N, k_end, wave, lane);
+
+  f32x16 acc[BN][BM];
+#pragma unroll
+  for (int i = 0; i < BN; ++i)
+#pragma unroll
+    for (int j = 0; j < BM; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+
+  i32x4 fb[4][BN], fa[4][BM];
+  auto read = [&](const uint8_t* x, int s) {
+    SA::template read<BM>(x, s, wm * BM * 32, lane, fa[s]);
+    SB::template read<BN>(x + SA::kBytes, s, wn * BN * 32, lane, fb[s]);
+  };
+  auto issue = [&](int st, uint8_t* x, int half) {  // loads half, half + 2, ... of each side
+#pragma unroll
+    for (int j = half; j < SA::kLoads; j += 2) sa.load(s0 + st, x, wave, j);
+#pragma unroll
+    for (int j = half; j < SB::kLoads; j += 2) sb.load(s0 + st, x + SA::kBytes, wave, j);
+  };
+  if (ns > 0) {
+    issue(0, x0, 0);
+    issue(0, x0, 1);
+    issue(1, x1, 0);
+    issue(1, x1, 1);
+    wait_all();
+    stage_barrier();
+    read(x0, 0);
+    read(x0, 1);
+    // loads past the last stage fetch nothing (their k is past the sides' K) and fill with zeros
+    auto stage = [&](int st, uint8_t* cx, const uint8_t* nx) {
+      read(cx, 2);
+      step_mma<ELT, BN, BM>(fb[0], fa[0], acc);
+      spread<BN * BM * (ELT == 2 ? 1 : 4), SA::kReads * BM + SB::kReads * BN, 0>();
+      read(cx, 3);
+      step_mma<ELT, BN, BM>(fb[1], fa[1], acc);
+      spread<BN * BM * (ELT == 2 ? 1 : 4), SA::kReads * BM + SB::kReads * BN, 0>();
+      wait_all();  // stage st + 1 has landed, this stage is in registers
+      stage_barrier();
+      issue(st + 2, cx, 0);
+      read(nx, 0);
+      step_mma<ELT, BN, BM>(fb[2], fa[2], acc);
+      spread<BN * BM * (ELT == 2 ? 1 : 4), SA::kReads * BM + SB::kReads * BN, (SA::kLoads + 1) / 2 + (SB::kLoads + 1) / 2>();
+      issue(st + 2, cx, 1);
+      read(nx, 1);
+      step_mma<ELT, BN, BM>(fb[3], fa[3], acc);
+      spread<BN * BM * (ELT == 2 ? 1 : 4), SA::kReads * BM + SB::kReads * BN, SA::kLoads / 2 + SB::kLoads / 2>();
+    };
+    for (int st = 0; st < ns; st += 2) {  // an odd last stage is followed by one of zeros
+      stage(st, x0, x1);
+      stage(st + 1, x1, x0);
+    }
+    wait_all();
+  }
+
+  // Block column j of every wave as rows of TN float32, 16-byte chunks XORed by
+  // row so that the lanes' writes (32 rows of one chunk) spread over the banks.
+  const int l32 = lane & 31, h = lane >> 5;
+  constexpr int LPR = TN / 4;  // lanes per row in the epilogue
+#pragma unroll
+  for (int j = 0; j < BM; ++j) {
+    uint8_t* x = j & 1 ? x1 : x0;
+    if (j < 2) stage_barrier();  // the last stage's reads are done (j = 0); later ones are ordered by the barrier below
+#pragma unroll
+    for (int i = 0; i < BN; ++i)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int row = wm * 32 + l32, c = (wn * BN + i) * 8 + 2 * v + h;
+        *(f32x4*)(x + row * (TN * 4) + ((c ^ (row & 15)) << 4)) =
+            f32x4{acc[i][j][4 * v], acc[i][j][4 * v + 1], acc[i][j][4 * v + 2], acc[i][j][4 * v + 3]};
+      }
+    stage_barrier();
+    const int c = tid % LPR, n = n0 + 4 * c;
+#pragma unroll 2
+    for (int row = tid / LPR; row < WM * 32; row += 256 / LPR) {
+      const int m = m0 + (row >> 5) * (BM * 32) + 32 * j + (row & 31);
+      const f32x4 v = *(const f32x4*)(x + row * (TN * 4) + ((c ^ (row & 15)) << 4));
+      if (m < a.M && n < a.N) {
+        if constexpr (OP == kPartial)
+          *(f32x4*)(part + ((int64_t)blockIdx.y * a.M + m) * ld_part + n) = v;
+        else
+          epilogue4<OP, ELT>(a, m, n, v);
+      }
+    }
+  }
+}
+
+// Sums of a split product's partial tiles in split order, and the epilogue.
+template <int OP, int ELT>
+__global__ __launch_bounds__(256) void gemm_join_kernel(GemmArgs a, const float* __restrict__ part, int64_t ld_part,
+                                                        int splits) {
+  const int nv = (a.N + 3) / 4;
+  const int64_t total = (int64_t)a.M * nv, step = (int64_t)a.M * ld_part;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int m = (int)(i / nv), n = (int)(i - (int64_t)m * nv) * 4;
+    const float* p = part + m * ld_part + n;
+    f32x4 s = *(const f32x4*)p;
+    int y = 1;
+    for (; y + 3 < splits; y += 4) {
+      const f32x4 v0 = *(const f32x4*)(p + y * step), v1 = *(const f32x4*)(p + (y + 1) * step),
+                  v2 = *(const f32x4*)(p + (y + 2) * step), v3 = *(const f32x4*)(p + (y + 3) * step);
+      s = (((s + v0) + v1) + v2) + v3;
+    }
+    for (; y < splits; ++y) s += *(const f32x4*)(p + y * step);
+    epilogue4<OP, ELT>(a, m, n, s);
+  }
+}
+
+// Rows of `w` elements copied to rows of `ld_out` (a multiple of 16 bytes), zeros behind.
+template <int ELT>
+__global__ __launch_bounds__(256) void repack_kernel(const uint8_t* __restrict__ src, int64_t ld, int w, int64_t rows,
+                                                     uint8_t* __restrict__ dst, int ld_out) {
+  constexpr int EPL = 16 / ELT;
+  const int chunks = ld_out / EPL;
+  const int64_t total = rows * chunks;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / chunks;
+    const int c = (int)(i - r * chunks) * EPL;
+    uint32_t v[EPL];
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) {
+      v[e] = 0;
+      if (c + e < w) v[e] = ELT == 2 ? ((const uint16_t*)src)[r * ld + c + e] : ((const uint32_t*)src)[r * ld + c + e];
+    }
+    i32x4 o;
+    if (ELT == 2)
+      o = i32x4{(int)(v[0] | v[1] << 16), (int)(v[2] | v[3] << 16), (int)(v[4 % EPL] | v[5 % EPL] << 16),
+                (int)(v[6 % EPL] | v[7 % EPL] << 16)};
+    else
+      o = i32x4{(int)v[0], (int)v[1], (int)v[2], (int)v[3]};
+    *(i32x4*)(dst + i * 16) = o;
+  }
+}
+
+// Column sums over rows [y * per, (y + 1) * per): a wave owns 64 columns and
+// every fourth row of the range; the waves' sums are added in wave order.
 template <int ELT>
 __global__ __launch_bounds__(256) void column_sums_kernel(const void* __restrict__ G, int64_t ld, int64_t rows,
-                                                          int cols, float* __restrict__ out, int accumulate) {
+                                                          int cols, int64_t per, float* __restrict__ out,
+                                                          int accumulate) {
+  __shared__ float red[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+  const int64_t r0 = blockIdx.y * per, r1 = min(rows, r0 + per);
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  if (c < cols) {
+    int64_t r = r0 + wave;
+    for (; r + 12 < r1; r += 16)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) s[u] += load_elt<ELT>(G, (r + 4 * u) * ld + c);
+    for (; r < r1; r += 4) s[0] += load_elt<ELT>(G, r * ld + c);
+  }
+  red[wave][lane] = (s[0] + s[1]) + (s[2] + s[3]);
+  __syncthreads();
+  if (wave == 0 && c < cols) {
+    const float v = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
+    float* o = out + (int64_t)blockIdx.y * cols + c;
+    *o = accumulate ? *o + v : v;
+  }
+}
+
+__global__ __launch_bounds__(256) void column_join_kernel(const float* __restrict__ part, int n_parts, int cols,
+                                                          float* __restrict__ out, int accumulate) {
   const int c = blockIdx.x * 256 + threadIdx.x;
   if (c >= cols) return;
   float s = 0.f;
-  for (int64_t r = 0; r < rows; ++r) s += load_elt<ELT>(G, r * ld + c);
+  for (int y = 0; y < n_parts; ++y) s += part[(int64_t)y * cols + c];
   out[c] = accumulate ? out[c] + s : s;
 }
 
-size_t linear_workspace_need(dattri_linear_op op, int64_t rows, int64_t d_in, int64_t d_out, int elt, bool aligned) {
-  return 0;
+namespace {
+
+// How a product is cut: tile variant, splits of k, stages per split.
+enum Variant { kBig, kMid, kFew };
+struct GemmShape {
+  Variant v;
+  int tm, tn;
+  int64_t nm, nn;
+  int splits, sps;
+};
+
+GemmShape gemm_shape(int64_t M, int64_t N, int64_t K, int elt, bool a_contiguous) {
+  GemmShape g;
+  const int64_t big = ((M + 255) / 256) * ((N + 255) / 256);
+  if (a_contiguous && M <= 32) g.v = kFew;
+  else if (big >= 192) g.v = kBig;
+  else g.v = kMid;
+  g.tm = g.v == kBig ? 256 : g.v == kMid ? 128 : 32;
+  g.tn = g.v == kBig ? 256 : 128;
+  g.nm = (M + g.tm - 1) / g.tm;
+  g.nn = (N + g.tn - 1) / g.tn;
+  const int64_t stages = std::max<int64_t>(1, (K * elt + 127) / 128), tiles = g.nm * g.nn;
+  const int64_t target = g.v == kBig ? 256 : g.v == kMid ? 512 : 1024;  // workgroups that fill the chip
+  int64_t splits = std::max<int64_t>(1, std::min<int64_t>({target / std::max<int64_t>(tiles, 1), stages / 4, 64}));
+  g.sps = (int)((stages + splits - 1) / splits);
+  g.splits = (int)((stages + g.sps - 1) / g.sps);
+  return g;
 }
 
-hipError_t launch_column_sums(int elt, const void* G, int64_t ld_g, int64_t rows, int64_t cols, float* out,
-                              bool accumulate, uint8_t* ws, hipStream_t s) {
-  auto k = elt == 2 ? column_sums_kernel<2> : column_sums_kernel<4>;
-  hipLaunchKernelGGL(k, dim3((unsigned)((cols + 255) / 256)), dim3(256), 0, s, G, ld_g, rows, (int)cols, out,
-                     (int)accumulate);
+// Column sums: rows per part, parts.
+void column_shape(int64_t rows, int64_t cols, int64_t* per, int64_t* parts) {
+  const int64_t strips = (cols + 63) / 64;
+  int64_t p = std::max<int64_t>(1, std::min<int64_t>(1024 / strips, rows / 64));
+  *per = std::max<int64_t>(1, (rows + p - 1) / p);
+  *parts = std::max<int64_t>(1, (rows + *per - 1) / *per);
+}
+
+struct LinearLayout {
+  int64_t M, N, K;
+  bool ac, bc;          // operands k contiguous
+  int64_t a_rows, a_w, b_rows, b_w;  // as stored
+  bool pack_a, pack_b;
+  size_t off_a, off_b, off_part, off_cols, total;
+  GemmShape g;
+};
+LinearLayout linear_layout(dattri_linear_op op, int64_t rows, int64_t d_in, int64_t d_out, int elt, bool aligned) {
+  LinearLayout L = {};
+  L.ac = op != DATTRI_LINEAR_WEIGHT_GRAD;
+  L.bc = op == DATTRI_LINEAR_FORWARD;
+  L.M = op == DATTRI_LINEAR_WEIGHT_GRAD ? d_out : rows;
+  L.N = op == DATTRI_LINEAR_FORWARD ? d_out : d_in;
+  L.K = op == DATTRI_LINEAR_FORWARD ? d_in : op == DATTRI_LINEAR_INPUT_GRAD ? d_out : rows;
+  L.a_rows = L.ac ? L.M : L.K;
+  L.a_w = L.ac ? L.K : L.M;
+  L.b_rows = L.bc ? L.N : L.K;
+  L.b_w = L.bc ? L.K : L.N;
+  L.pack_a = !aligned || (L.a_w * elt) % 16;
+  L.pack_b = !aligned || (L.b_w * elt) % 16;
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off = align_up(off + bytes);
+    return at;
+  };
+  auto packed = [&](int64_t r, int64_t w) { return (size_t)r * (size_t)((w * elt + 15) / 16 * 16); };
+  L.off_a = take(L.pack_a ? packed(L.a_rows, L.a_w) : 0);
+  L.off_b = take(L.pack_b ? packed(L.b_rows, L.b_w) : 0);
+  L.g = gemm_shape(std::max<int64_t>(L.M, 1), L.N, L.K, elt, L.ac);
+  L.off_part = take(L.g.splits > 1 ? (size_t)L.g.splits * L.M * ((L.N + 3) / 4 * 4) * 4 : 0);
+  L.off_cols = off;
+  if (op == DATTRI_LINEAR_WEIGHT_GRAD) {
+    int64_t per, parts;
+    column_shape(rows, d_out, &per, &parts);
+    take(parts > 1 ? (size_t)parts * d_out * 4 : 0);
+  }
+  L.total = off;
+  return L;
+}
+
+unsigned flat_grid(int64_t n) { return (unsigned)std::min<int64_t>((n + 255) / 256, 16384); }
+
+hipError_t repack(int elt, const void* src, int64_t ld, int64_t w, int64_t rows, uint8_t* dst, hipStream_t s) {
+  const int ld_out = (int)((w * elt + 15) / 16 * 16 / elt);
+  const int64_t n = rows * (ld_out * elt / 16);
+  if (n == 0) return hipSuccess;
+  hipLaunchKernelGGL(elt == 2 ? repack_kernel<2> : repack_kernel<4>, dim3(flat_grid(n)), dim3(256), 0, s,
+                     (const uint8_t*)src, ld, (int)w, rows, dst, ld_out);
   return hipGetLastError();
 }
 
-hipError_t launch_gemm(dattri_linear_op op, int elt, const GemmArgs& a, uint8_t* ws, hipStream_t s) {
-  const int64_t tm = (a.M + 63) / 64, tn = (a.N + 63) / 64;
-  if (tm * tn > INT32_MAX) return hipErrorInvalidValue;
-  auto go = [&](auto k) {
-    hipLaunchKernelGGL(k, dim3((unsigned)(tm * tn)), dim3(256), 0, s, a, (int)tn);
-    return hipGetLastError();
-  };
-  if (op == DATTRI_LINEAR_FORWARD) return elt == 2 ? go(gemm_simple_kernel<0, 2>) : go(gemm_simple_kernel<0, 4>);
-  if (op == DATTRI_LINEAR_INPUT_GRAD) return elt == 2 ? go(gemm_simple_kernel<1, 2>) : go(gemm_simple_kernel<1, 4>);
-  return elt == 2 ? go(gemm_simple_kernel<2, 2>) : go(gemm_simple_kernel<2, 4>);
+template <int OP, bool AC, bool BC, int ELT, int WM, int WN, int BM, int BN>
+hipError_t launch_tiles(const GemmArgs& a, const GemmShape& g, float* part, int64_t ldp, hipStream_t s) {
+  const dim3 grid((unsigned)(g.nm * g.nn), g.splits);
+  if (g.splits > 1)
+    hipLaunchKernelGGL((gemm_kernel<kPartial, AC, BC, ELT, WM, WN, BM, BN>), grid, dim3(256), 0, s, a, (int)g.nm,
+                       (int)g.nn, g.sps, part, ldp);
+  else
+    hipLaunchKernelGGL((gemm_kernel<OP, AC, BC, ELT, WM, WN, BM, BN>), grid, dim3(256), 0, s, a, (int)g.nm, (int)g.nn,
+                       g.sps, part, ldp);
+  return hipGetLastError();
+}
+
+template <int OP, int ELT>
+hipError_t launch_product(const GemmArgs& a, const GemmShape& g, float* part, hipStream_t s) {
+  constexpr bool AC = OP != DATTRI_LINEAR_WEIGHT_GRAD, BC = OP == DATTRI_LINEAR_FORWARD;
+  if (g.nm * g.nn > INT32_MAX) return hipErrorInvalidValue;
+  const int64_t ldp = (a.N + 3) / 4 * 4;
+  hipError_t e = hipErrorInvalidValue;
+  if (g.v == kBig)
+    e = launch_tiles<OP, AC, BC, ELT, 2, 2, 4, 4>(a, g, part, ldp, s);
+  else if (g.v == kMid)
+    e = launch_tiles<OP, AC, BC, ELT, 2, 2, 2, 2>(a, g, part, ldp, s);
+  else if constexpr (AC)
+    e = launch_tiles<OP, AC, BC, ELT, 1, 4, 1, 1>(a, g, part, ldp, s);
+  if (e != hipSuccess || g.splits == 1) return e;
+  hipLaunchKernelGGL((gemm_join_kernel<OP, ELT>), dim3(flat_grid((int64_t)a.M * (ldp / 4))), dim3(256), 0, s, a, part,
+                     ldp, g.splits);
+  return hipGetLastError();
+}
+
+hipError_t launch_column_sums(int elt, const void* G, int64_t ld_g, int64_t rows, int64_t cols, float* out,
+                              bool accumulate, float* part, hipStream_t s) {
+  int64_t per, parts;
+  column_shape(rows, cols, &per, &parts);
+  auto k = elt == 2 ? column_sums_kernel<2> : column_sums_kernel<4>;
+  hipLaunchKernelGGL(k, dim3((unsigned)((cols + 63) / 64), (unsigned)parts), dim3(256), 0, s, G, ld_g, rows, (int)cols,
+                     per, parts > 1 ? part : out, parts > 1 ? 0 : (int)accumulate);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || parts == 1) return e;
+  hipLaunchKernelGGL(column_join_kernel, dim3((unsigned)((cols + 255) / 256)), dim3(256), 0, s, part, (int)parts,
+                     (int)cols, out, (int)accumulate);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t linear_workspace_need(dattri_linear_op op, int64_t rows, int64_t d_in, int64_t d_out, int elt, bool aligned) {
+  return linear_layout(op, rows, d_in, d_out, elt, aligned).total;
+}
+
+hipError_t launch_linear(dattri_linear_op op, int elt, bool aligned, GemmArgs a, float* dbias, uint8_t* ws,
+                         hipStream_t s) {
+  const bool wgrad = op == DATTRI_LINEAR_WEIGHT_GRAD;
+  const int64_t rows = wgrad ? a.K : a.M, d_out = op == DATTRI_LINEAR_FORWARD ? a.N : wgrad ? a.M : a.K,
+                d_in = op == DATTRI_LINEAR_FORWARD ? a.K : a.N;
+  const LinearLayout L = linear_layout(op, rows, d_in, d_out, elt, aligned);
+  hipError_t e;
+  if (dbias) {
+    e = launch_column_sums(elt, a.A, a.lda, rows, d_out, dbias, a.accumulate, (float*)(ws + L.off_cols), s);
+    if (e != hipSuccess || !a.out) return e;
+  }
+  if (L.pack_a) {
+    e = repack(elt, a.A, a.lda, L.a_w, L.a_rows, ws + L.off_a, s);
+    if (e != hipSuccess) return e;
+    a.A = ws + L.off_a;
+    a.lda = (L.a_w * elt + 15) / 16 * 16 / elt;
+  }
+  if (L.pack_b) {
+    e = repack(elt, a.B, a.ldb, L.b_w, L.b_rows, ws + L.off_b, s);
+    if (e != hipSuccess) return e;
+    a.B = ws + L.off_b;
+    a.ldb = (L.b_w * elt + 15) / 16 * 16 / elt;
+  }
+  const int oelt = wgrad ? 4 : elt;
+  auto on4 = [](const void* p, int64_t ld, int e) { return !p || ((uintptr_t)p % (4 * e) == 0 && ld % 4 == 0); };
+  a.vec = on4(a.bias, 0, elt) && on4(a.R, a.ldr, elt) && on4(a.Z, a.ldz, elt) && on4(a.out, a.ldo, oelt) &&
+          on4(a.out2, a.ldo2, elt);
+  float* part = (float*)(ws + L.off_part);
+  if (op == DATTRI_LINEAR_FORWARD)
+    return elt == 2 ? launch_product<DATTRI_LINEAR_FORWARD, 2>(a, L.g, part, s)
+                    : launch_product<DATTRI_LINEAR_FORWARD, 4>(a, L.g, part, s);
+  if (op == DATTRI_LINEAR_INPUT_GRAD)
+    return elt == 2 ? launch_product<DATTRI_LINEAR_INPUT_GRAD, 2>(a, L.g, part, s)
+                    : launch_product<DATTRI_LINEAR_INPUT_GRAD, 4>(a, L.g, part, s);
+  return elt == 2 ? launch_product<DATTRI_LINEAR_WEIGHT_GRAD, 2>(a, L.g, part, s)
+                  : launch_product<DATTRI_LINEAR_WEIGHT_GRAD, 4>(a, L.g, part, s);
 }
 
 }  // namespace dattri

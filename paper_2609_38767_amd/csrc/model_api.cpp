@@ -167,8 +167,8 @@ dattri_status dattri_linear(const void* X, int64_t ld_x, const void* W, int64_t 
   TRY(check_rows("Z", Z, &ld_z, rows, d_out, elt, false));
   if ((uintptr_t)bias % elt) return fail(DATTRI_E_INVALID_ARG, "bias is not aligned to its elements");
   if (R && R == Y && ld_r != ld_y) return fail(DATTRI_E_INVALID_ARG, "Y may be R only with the same row stride");
-  TRY(check_workspace(workspace, ws_bytes,
-                      linear_workspace_need(DATTRI_LINEAR_FORWARD, rows, d_in, d_out, elt, on_16(X, ld_x, W, ld_w, elt))));
+  const bool aligned = on_16(X, ld_x, W, ld_w, elt);
+  TRY(check_workspace(workspace, ws_bytes, linear_workspace_need(DATTRI_LINEAR_FORWARD, rows, d_in, d_out, elt, aligned)));
   if (rows == 0) return DATTRI_OK;
   GemmArgs a = {};
   a.A = X;
@@ -186,7 +186,7 @@ dattri_status dattri_linear(const void* X, int64_t ld_x, const void* W, int64_t 
   a.out = Y;
   a.ldo = ld_y;
   a.act = act;
-  HIP_TRY(launch_gemm(DATTRI_LINEAR_FORWARD, elt, a, (uint8_t*)workspace, (hipStream_t)stream));
+  HIP_TRY(launch_linear(DATTRI_LINEAR_FORWARD, elt, aligned, a, nullptr, (uint8_t*)workspace, (hipStream_t)stream));
   return DATTRI_OK;
 }
 
@@ -210,9 +210,9 @@ dattri_status dattri_linear_input_grad(const void* G, int64_t ld_g, const void* 
     return fail(DATTRI_E_INVALID_ARG, "D or P may be R only with the same row stride");
   if (Z && ((Z == P && ld_z != ld_p) || Z == D))
     return fail(DATTRI_E_INVALID_ARG, "P may be Z only with the same row stride, D may not");
+  const bool aligned = on_16(G, ld_g, W, ld_w, elt);
   TRY(check_workspace(workspace, ws_bytes,
-                      linear_workspace_need(DATTRI_LINEAR_INPUT_GRAD, rows, d_in, d_out, elt,
-                                            on_16(G, ld_g, W, ld_w, elt))));
+                      linear_workspace_need(DATTRI_LINEAR_INPUT_GRAD, rows, d_in, d_out, elt, aligned)));
   if (rows == 0) return DATTRI_OK;
   GemmArgs a = {};
   a.A = G;
@@ -231,7 +231,8 @@ dattri_status dattri_linear_input_grad(const void* G, int64_t ld_g, const void* 
   a.out2 = P;
   a.ldo2 = ld_p;
   a.act = act;
-  HIP_TRY(launch_gemm(DATTRI_LINEAR_INPUT_GRAD, elt, a, (uint8_t*)workspace, (hipStream_t)stream));
+  HIP_TRY(launch_linear(DATTRI_LINEAR_INPUT_GRAD, elt, aligned, a, nullptr, (uint8_t*)workspace,
+                        (hipStream_t)stream));
   return DATTRI_OK;
 }
 
@@ -247,27 +248,22 @@ dattri_status dattri_linear_weight_grad(const void* G, int64_t ld_g, const void*
   TRY(check_rows("dW", dW, &ld_dw, d_out, d_in, 4, false));
   if ((uintptr_t)dbias % 4) return fail(DATTRI_E_INVALID_ARG, "dbias is not aligned to its elements");
   if (!dW && !dbias) return fail(DATTRI_E_INVALID_ARG, "nothing to compute: dW and dbias are NULL");
+  const bool aligned = on_16(G, ld_g, X, ld_x, elt);
   TRY(check_workspace(workspace, ws_bytes,
-                      linear_workspace_need(DATTRI_LINEAR_WEIGHT_GRAD, rows, d_in, d_out, elt,
-                                            on_16(G, ld_g, X, ld_x, elt))));
+                      linear_workspace_need(DATTRI_LINEAR_WEIGHT_GRAD, rows, d_in, d_out, elt, aligned)));
   if (rows == 0 && accumulate) return DATTRI_OK;
-  hipStream_t s = (hipStream_t)stream;
-  uint8_t* ws = (uint8_t*)workspace;
-  if (dbias) HIP_TRY(launch_column_sums(elt, G, ld_g, rows, d_out, dbias, accumulate != 0, ws, s));
-  if (dW) {
-    GemmArgs a = {};
-    a.A = G;
-    a.B = X;
-    a.lda = ld_g;
-    a.ldb = ld_x;
-    a.M = (int)d_out;
-    a.N = (int)d_in;
-    a.K = (int)rows;
-    a.out = dW;
-    a.ldo = ld_dw;
-    a.accumulate = accumulate != 0;
-    HIP_TRY(launch_gemm(DATTRI_LINEAR_WEIGHT_GRAD, elt, a, ws, s));
-  }
+  GemmArgs a = {};
+  a.A = G;
+  a.B = X;
+  a.lda = ld_g;
+  a.ldb = ld_x;
+  a.M = (int)d_out;
+  a.N = (int)d_in;
+  a.K = (int)rows;
+  a.out = dW;
+  a.ldo = ld_dw;
+  a.accumulate = accumulate != 0;
+  HIP_TRY(launch_linear(DATTRI_LINEAR_WEIGHT_GRAD, elt, aligned, a, dbias, (uint8_t*)workspace, (hipStream_t)stream));
   return DATTRI_OK;
 }
 

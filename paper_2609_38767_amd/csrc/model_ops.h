@@ -46,12 +46,13 @@ struct GemmArgs {
   int64_t ldo2;
   int act;
   int accumulate;  // weight grad
+  int vec;         // rows of the epilogue's buffers start on four elements
 };
 size_t linear_workspace_need(dattri_linear_op op, int64_t rows, int64_t d_in, int64_t d_out, int elt, bool aligned);
-hipError_t launch_gemm(dattri_linear_op op, int elt, const GemmArgs& a, uint8_t* ws, hipStream_t s);
-// dbias[n] (+)= sum over rows of G[row][n]
-hipError_t launch_column_sums(int elt, const void* G, int64_t ld_g, int64_t rows, int64_t cols, float* out,
-                              bool accumulate, uint8_t* ws, hipStream_t s);
+// aligned: both operands' pointers and strides on 16 bytes; dbias (weight grad):
+// null or the bias gradient; a.out may then be null.
+hipError_t launch_linear(dattri_linear_op op, int elt, bool aligned, GemmArgs a, float* dbias, uint8_t* ws,
+                         hipStream_t s);
 
 // ------------------------------------------------------------------ clip
 constexpr int kClipTensors = 128;    // tensors per launch (their list is a kernel argument)
