@@ -5,13 +5,14 @@
 //
 // Gradient: grad_table[v] = scale * sum over positions i with tokens[i] = v of
 // grad_out[i].  The positions are sorted by token with a stable radix sort
-// (digits of at most 9 bits; counts per workgroup, one scan, ranks within a
-// wave by ballots: no float and no ordering depends on timing), so the
-// positions of a row form a run in ascending order.  A run is summed as the
-// positions up to the next multiple of kRun, whole groups of kRun positions
-// whose sums another kernel has formed (so a token that is most of the batch
-// does not wait on one wave), and the positions left; the order is that of the
-// positions in fixed groups, whatever the launch.
+// (digits of at most 9 bits; ranks within a wave by ballots: no float and no
+// order depends on timing), so the positions of a row form a run in ascending
+// order.  A run is summed as the positions up to the next multiple of kRun,
+// whole groups of kRun positions whose sums another kernel has formed (so a
+// token that is most of the batch does not wait on one wave), and the positions
+// left; the order is that of the positions in fixed groups, whatever the launch.
+// A whole table is zeroed first, by workgroups that ride in the launch of the
+// sort's first kernel: the sort is a few waves' latency, the zeros are bandwidth.
 //
 // What bounds it: the lookup and the sums read and write each row once; for a
 // whole table the zeros of rows without tokens are most of the bytes.
@@ -24,29 +25,23 @@
 namespace dattri {
 using namespace dev;
 
-constexpr int kStrip = 512;       // columns per wave: 8 per lane
+constexpr int kStrip = 512;       // lookup: columns per wave, 8 per lane
 constexpr int kRun = 32;          // positions per group of a long run
 constexpr int kMaxDigit = 9;      // bits per sorting pass
 constexpr int kBins = 1 << kMaxDigit;
 constexpr int kSortItems = 4096;  // least positions per sorting workgroup
 constexpr int kSortBlocks = 2048; // most sorting workgroups
 
-// The eight columns a lane owns of a strip: 8 in a row (16 bytes of bf16),
-// twice 4 in a row (16 bytes of float32, or 8 of bf16 against 16 of a float32
-// output), or one in every 64 (rows not on 16 bytes).
+// The E columns a lane owns of a strip of 64 E: 8 in a row (16 bytes of bf16),
+// runs of 4 (16 bytes of float32, or 8 of bf16 against 16 of a float32 output),
+// or one in every 64 (rows not on 16 bytes).
 enum Cols { kCols8, kCols4, kCols1 };
-template <Cols C>
-__device__ inline int col_of(int base, int lane, int e) {
-  if constexpr (C == kCols8) return base + 8 * lane + e;
-  if constexpr (C == kCols4) return base + 256 * (e >> 2) + 4 * lane + (e & 3);
-  return base + 64 * e + lane;
-}
-
-// float32 values of a lane's eight columns; columns >= d read as zero (d is a
+// float32 values of a lane's columns; columns >= d read as zero (d is a
 // multiple of 8 for kCols8, of 4 for kCols4).
-template <int ELT, Cols C>
-__device__ inline void load_cols(const uint8_t* row, int base, int lane, int d, float (&v)[8]) {
+template <int ELT, Cols C, int E>
+__device__ inline void load_cols(const uint8_t* row, int base, int lane, int d, float (&v)[E]) {
   if constexpr (C == kCols8) {
+    static_assert(E == 8, "one run of 8");
     const int c = base + 8 * lane;
     i32x4 w = {0, 0, 0, 0};
     if (c < d) w = *(const i32x4*)(row + (int64_t)c * 2);
@@ -58,7 +53,7 @@ __device__ inline void load_cols(const uint8_t* row, int base, int lane, int d, 
     }
   } else if constexpr (C == kCols4) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < E / 4; ++h) {
       const int c = base + 256 * h + 4 * lane;
       if constexpr (ELT == 2) {
         i32x2 w = {0, 0};
@@ -79,7 +74,7 @@ __device__ inline void load_cols(const uint8_t* row, int base, int lane, int d, 
     }
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < E; ++e) {
       const int c = base + 64 * e + lane;
       v[e] = 0.f;
       if (c < d)
@@ -89,8 +84,8 @@ __device__ inline void load_cols(const uint8_t* row, int base, int lane, int d, 
   }
 }
 
-template <int ELT, Cols C>
-__device__ inline void store_cols(uint8_t* row, int base, int lane, int d, const float (&v)[8]) {
+template <int ELT, Cols C, int E>
+__device__ inline void store_cols(uint8_t* row, int base, int lane, int d, const float (&v)[E]) {
   if constexpr (C == kCols8) {
     const int c = base + 8 * lane;
     const i32x4 w = {(int)pack_bf16(v[0], v[1]), (int)pack_bf16(v[2], v[3]), (int)pack_bf16(v[4], v[5]),
@@ -99,14 +94,14 @@ __device__ inline void store_cols(uint8_t* row, int base, int lane, int d, const
   } else if constexpr (C == kCols4) {
     static_assert(ELT == 4, "four columns in a row are written as float32");
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < E / 4; ++h) {
       const int c = base + 256 * h + 4 * lane;
       const f32x4 w = {v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
       if (c < d) *(f32x4*)(row + (int64_t)c * 4) = w;
     }
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < E; ++e) {
       const int c = base + 64 * e + lane;
       if (c < d) {
         if (ELT == 2)
@@ -167,6 +162,37 @@ __device__ inline uint32_t key_at(const void* tokens, int token_bytes, int64_t v
   return t >= 0 && t < vocab ? (uint32_t)t : (uint32_t)vocab;
 }
 
+// The table to be zeroed (out null: none).
+struct Fill {
+  float* out;
+  int64_t ld, rows;
+  int d;
+};
+// Share `b` of `nb` of it, by T threads, in pieces of 8 T stores (2 GiB in 331
+// us by 1020 workgroups of 1024; store by store around the chip 403: memory
+// takes neighbouring lines better together).
+template <int T>
+__device__ inline void fill_zero(const Fill& f, int64_t b, int64_t nb) {
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  const int t = threadIdx.x;
+  if (f.ld == f.d) {  // one block of memory
+    const int64_t total = f.rows * f.d, head = min(total, (int64_t)(((16 - (uintptr_t)f.out % 16) % 16) / 4));
+    const int64_t n4 = (total - head) / 4, tail = total - head - 4 * n4;
+    f32x4* p = (f32x4*)(f.out + head);
+    for (int64_t c = b; c * (8 * T) < n4; c += nb)
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int64_t i = (c * 8 + u) * T + t;
+        if (i < n4) p[i] = zero;
+      }
+    if (b == 0 && t < head) f.out[t] = 0.f;
+    if (b == 0 && t < tail) f.out[head + 4 * n4 + t] = 0.f;
+    return;
+  }
+  for (int64_t r = b * (T / 64) + t / 64; r < f.rows; r += nb * (T / 64))
+    for (int c = t % 64; c < f.d; c += 64) f.out[r * f.ld + c] = 0.f;
+}
+
 struct SortPass {
   const void* tokens;  // first pass: keys from the tokens, positions in order
   int token_bytes;
@@ -182,8 +208,9 @@ __device__ inline uint32_t pass_key(const SortPass& p, int i) {
   return p.tokens ? key_at(p.tokens, p.token_bytes, p.vocab, i) : p.key_in[i];
 }
 
-__global__ __launch_bounds__(256) void sort_count_kernel(SortPass p) {
+__global__ __launch_bounds__(256) void sort_count_kernel(SortPass p, Fill f) {
   __shared__ uint32_t h[kBins];
+  if ((int)blockIdx.x >= p.blocks) return fill_zero<256>(f, blockIdx.x - p.blocks, gridDim.x - p.blocks);
   const int bins = 1 << p.bits;
   for (int b = threadIdx.x; b < bins; b += 256) h[b] = 0;
   __syncthreads();
@@ -270,99 +297,186 @@ __global__ __launch_bounds__(256) void sort_scatter_kernel(SortPass p) {
   }
 }
 
-// ------------------------------------------------------------------- sums
-template <int ELT, Cols C>
-__device__ inline void add_positions(const uint8_t* g, int64_t ld, const int* pos, int a, int b, int base, int lane,
-                                     int d, float (&acc)[8]) {
-  constexpr int U = 4;  // rows in flight
-  int i = a;
-  for (; i + U <= b; i += U) {
-    float v[U][8];
+// The whole sort in one workgroup: up to kSmallSort positions, each packed with
+// its key into 32 bits.  Wave w holds positions w * per .. + per - 1, 64 at a
+// time; a pass counts and ranks them per wave, scans the counts digit by digit
+// and moves the items through LDS.  509 positions take 10 us with their table's
+// zeros (30 MB), the six launches of the passes above 29.
+constexpr int kSmallSort = 16384, kPosBits = 14, kSmallRounds = kSmallSort / 1024;
+__global__ __launch_bounds__(1024) void sort_small_kernel(const void* __restrict__ tokens, int token_bytes,
+                                                          int64_t vocab, int n, int passes, int bits,
+                                                          uint32_t* __restrict__ key_out, int* __restrict__ pos_out,
+                                                          Fill f) {
+  __shared__ uint32_t items[kSmallSort];
+  __shared__ uint32_t off[16][kBins];
+  __shared__ uint32_t sums[16];
+  if (blockIdx.x > 0) return fill_zero<1024>(f, blockIdx.x - 1, gridDim.x - 1);
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, bins = 1 << bits;
+  const int rounds = (n + 1023) / 1024, first = wave * rounds * 64 + lane;
+  uint32_t v[kSmallRounds];
+  int rank[kSmallRounds];
 #pragma unroll
-    for (int u = 0; u < U; ++u) load_cols<ELT, C>(g + (int64_t)pos[i + u] * ld * ELT, base, lane, d, v[u]);
+  for (int r = 0; r < kSmallRounds; ++r)
+    if (r < rounds) {
+      const int i = first + r * 64;
+      v[r] = i < n ? key_at(tokens, token_bytes, vocab, i) << kPosBits | (uint32_t)i : 0u;
+    }
+  for (int p = 0; p < passes; ++p) {
+    const int shift = kPosBits + p * bits;
+    for (int b = t; b < 16 * kBins; b += 1024) off[b / kBins][b % kBins] = 0;
+    __syncthreads();
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int r = 0; r < kSmallRounds; ++r)
+      if (r < rounds) {
+        const bool ok = first + r * 64 < n;
+        const uint32_t digit = (v[r] >> shift) & (bins - 1);
+        int below, count;
+        digit_rank(digit, bits, __ballot(ok), lane, &below, &count);
+        const uint32_t base = off[wave][digit];
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        if (ok && below == 0) off[wave][digit] = base + count;
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        rank[r] = (int)base + below;
+      }
+    __syncthreads();
+    // exclusive scan of the counts, digit by digit and wave by wave: thread t has waves 8 (t % 2) .. + 7 of digit t / 2
+    uint32_t c[8], s = 0;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] += v[u][e];
+    for (int w = 0; w < 8; ++w) {
+      c[w] = off[8 * (t & 1) + w][t >> 1];
+      s += c[w];
+    }
+    uint32_t x = s;
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint32_t y = __shfl_up(x, o);
+      if (lane >= o) x += y;
+    }
+    if (lane == 63) sums[wave] = x;
+    __syncthreads();
+    uint32_t run = x - s;
+    for (int w = 0; w < wave; ++w) run += sums[w];
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      off[8 * (t & 1) + w][t >> 1] = run;
+      run += c[w];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kSmallRounds; ++r)
+      if (r < rounds && first + r * 64 < n) items[off[wave][(v[r] >> shift) & (bins - 1)] + rank[r]] = v[r];
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kSmallRounds; ++r)
+      if (r < rounds && first + r * 64 < n) v[r] = items[first + r * 64];
   }
-  for (; i < b; ++i) {
-    float v[8];
-    load_cols<ELT, C>(g + (int64_t)pos[i] * ld * ELT, base, lane, d, v);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] += v[e];
+  for (int r = 0; r < kSmallRounds; ++r)
+    if (r < rounds && first + r * 64 < n) {
+      key_out[first + r * 64] = v[r] >> kPosBits;
+      pos_out[first + r * 64] = (int)(v[r] & ((1u << kPosBits) - 1u));
+    }
+}
+
+// ------------------------------------------------------------------- sums
+// acc += rows row(a) .. row(b - 1), in order, F of them loaded before they are added.
+template <int ELT, Cols C, int F, int E, class Row>
+__device__ inline void add_rows(Row row, int a, int b, int base, int lane, int d, float (&acc)[E]) {
+  for (int i = a; i < b; i += F) {
+    float v[F][E];
+#pragma unroll
+    for (int u = 0; u < F; ++u) {
+      if (i + u < b) {  // uniform
+        load_cols<ELT, C>(row(i + u), base, lane, d, v[u]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[u][e] = 0.f;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < F; ++u)
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] += v[u][e];
   }
 }
 
-// Sums of the groups of kRun sorted positions that hold one token only.
+// Sums of the groups of kRun sorted positions that hold one token only: all
+// rows of a group in flight at once, 256 columns per wave.
 template <int ELT, Cols C>
 __global__ __launch_bounds__(256) void embgrad_groups_kernel(const uint8_t* __restrict__ g, int64_t ld, int d,
                                                              const uint32_t* __restrict__ key,
                                                              const int* __restrict__ pos, int n_groups, uint32_t vocab,
-                                                             float* __restrict__ part, int64_t ld_part) {
+                                                             float* __restrict__ part, int64_t ld_part, int strips) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int j = blockIdx.x * 4 + wave;
+  const int64_t unit = (int64_t)blockIdx.x * 4 + wave;
+  const int j = (int)(unit / strips), base = (int)(unit - (int64_t)j * strips) * 256;
   if (j >= n_groups) return;
   const int a = j * kRun;
+  const int at = pos[a + (lane & (kRun - 1))];
   const uint32_t v = key[a];
   if (v >= vocab || key[a + kRun - 1] != v) return;
-  const int base = blockIdx.y * kStrip;
-  float acc[8] = {};
-  add_positions<ELT, C>(g, ld, pos, a, a + kRun, base, lane, d, acc);
+  float acc[4] = {};
+  add_rows<ELT, C, kRun>([&](int i) { return g + (int64_t)__builtin_amdgcn_readlane(at, i) * ld * ELT; }, 0, kRun, base,
+                         lane, d, acc);
   store_cols<4, C>((uint8_t*)(part + (int64_t)j * ld_part), base, lane, d, acc);
 }
 
-constexpr int kRowsPerBlock = 16;
-// grid (table rows / 16, column groups): each wave owns four rows.
-template <int ELT, Cols C>
+// One wave per (sorted position, strip of 64 E columns), a row's strips next to
+// each other (strips of all rows one after the other took 117 us where this
+// takes 84: memory takes a whole row better at once).  The waves at the start
+// of a run sum it.
+template <int ELT, Cols C, int E>
 __global__ __launch_bounds__(256) void embgrad_rows_kernel(const uint8_t* __restrict__ g, int64_t ld, int d,
                                                            const uint32_t* __restrict__ key,
                                                            const int* __restrict__ pos, int n,
                                                            const float* __restrict__ part, int64_t ld_part,
-                                                           float scale, int64_t vocab, int strips_each,
-                                                           float* __restrict__ out, int64_t ld_out, int accumulate) {
-  __shared__ int start[kRowsPerBlock + 1];
+                                                           float scale, uint32_t vocab, float* __restrict__ out,
+                                                           int64_t ld_out, int accumulate, int strips) {
+  constexpr int F = 64 / E;  // rows in flight
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t v0 = (int64_t)blockIdx.x * kRowsPerBlock;
-  if (threadIdx.x <= kRowsPerBlock) {  // first sorted position with a key >= v
-    const uint32_t v = (uint32_t)min(v0 + threadIdx.x, vocab);
-    int lo = 0, hi = n;
+  const int64_t unit = (int64_t)blockIdx.x * 4 + wave, first = unit / strips;
+  const int base = (int)(unit - first * strips) * (64 * E);
+  if (first >= n) return;
+  const int a = (int)first;
+  // keys and positions of the next 64 places, asked for before the first key is known
+  const int64_t mine = min(first + lane, (int64_t)n - 1);
+  const uint32_t next = key[mine];
+  const int at = pos[mine];
+  const uint32_t before = a > 0 ? key[a - 1] : vocab;
+  const uint32_t v = __builtin_amdgcn_readfirstlane(next);
+  if (v >= vocab || before == v) return;
+  const uint64_t other = __ballot(first + lane >= n || next != v);
+  int b;
+  if (other) {
+    b = a + __builtin_ctzll(other);
+  } else {  // a longer run: its end by bisection
+    int lo = a + 64, hi = n;
     while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (key[mid] < v) lo = mid + 1;
+      const int mid = lo + ((hi - lo) >> 1);
+      if (key[mid] == v) lo = mid + 1;
       else hi = mid;
     }
-    start[threadIdx.x] = lo;
+    b = lo;
   }
-  __syncthreads();
-  const int c0 = blockIdx.y * strips_each * kStrip, c1 = min(d, c0 + strips_each * kStrip);
-  for (int r = wave; r < kRowsPerBlock; r += 4) {
-    const int64_t v = v0 + r;
-    if (v >= vocab) break;
-    const int a = __builtin_amdgcn_readfirstlane(start[r]), b = __builtin_amdgcn_readfirstlane(start[r + 1]);
-    if (accumulate && a == b) continue;
-    const int ga = (a + kRun - 1) / kRun, gb = b / kRun;  // whole groups ga .. gb - 1
-    for (int base = c0; base < c1; base += kStrip) {
-      float acc[8] = {};
-      if (ga < gb) {
-        add_positions<ELT, C>(g, ld, pos, a, ga * kRun, base, lane, d, acc);
-        for (int j = ga; j < gb; ++j) {
-          float w[8];
-          load_cols<4, C>((const uint8_t*)(part + (int64_t)j * ld_part), base, lane, d, w);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) acc[e] += w[e];
-        }
-        add_positions<ELT, C>(g, ld, pos, gb * kRun, b, base, lane, d, acc);
-      } else {
-        add_positions<ELT, C>(g, ld, pos, a, b, base, lane, d, acc);
-      }
-      uint8_t* row = (uint8_t*)(out + v * ld_out);
-      float old[8] = {};
-      if (accumulate) load_cols<4, C>(row, base, lane, d, old);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] = fmaf(scale, acc[e], old[e]);
-      store_cols<4, C>(row, base, lane, d, acc);
-    }
+  b = __builtin_amdgcn_readfirstlane(b);
+  auto near = [&](int i) { return g + (int64_t)__builtin_amdgcn_readlane(at, i - a) * ld * ELT; };
+  auto far = [&](int i) { return g + (int64_t)pos[i] * ld * ELT; };
+  const int ga = a / kRun + (a % kRun != 0), gb = b / kRun;  // whole groups ga .. gb - 1
+  float acc[E] = {};
+  if (ga < gb) {
+    add_rows<ELT, C, F>(near, a, ga * kRun, base, lane, d, acc);
+    add_rows<4, C, F>([&](int j) { return (const uint8_t*)(part + (int64_t)j * ld_part); }, ga, gb, base, lane, d, acc);
+    add_rows<ELT, C, F>(far, gb * kRun, b, base, lane, d, acc);
+  } else {
+    add_rows<ELT, C, F>(near, a, b, base, lane, d, acc);
   }
+  uint8_t* to = (uint8_t*)(out + (int64_t)v * ld_out);
+  float old[E] = {};
+  if (accumulate) load_cols<4, C>(to, base, lane, d, old);
+#pragma unroll
+  for (int e = 0; e < E; ++e) acc[e] = fmaf(scale, acc[e], old[e]);
+  store_cols<4, C>(to, base, lane, d, acc);
 }
 
 namespace {
@@ -405,8 +519,17 @@ hipError_t launch_embedding_grad(int elt, const void* grad_out, int64_t ld_grad,
   uint32_t* key[2] = {(uint32_t*)(ws + L.off_key[0]), (uint32_t*)(ws + L.off_key[1])};
   int* pos[2] = {(int*)(ws + L.off_pos[0]), (int*)(ws + L.off_pos[1])};
   int cur = 0;
-  if (n > 0) {
-    const int bits = key_bits(vocab), passes = (bits + kMaxDigit - 1) / kMaxDigit, each = (bits + passes - 1) / passes;
+  const Fill f = {accumulate ? nullptr : grad_table, ld_table, vocab, (int)d};
+  // workgroups that zero the table: 64 KiB each at least, four rounds of the chip at most
+  const int64_t share = (vocab * d * 4 + 65535) / 65536;
+  auto fills = [&](int64_t most) { return accumulate ? 0u : (unsigned)std::min(share, most); };
+  const int bits = key_bits(vocab);
+  if (n <= kSmallSort && bits + kPosBits <= 32) {
+    const int passes = (bits + kMaxDigit - 1) / kMaxDigit;
+    hipLaunchKernelGGL(sort_small_kernel, dim3(1 + fills(1023)), dim3(1024), 0, s, tokens, token_bytes, vocab, (int)n,
+                       passes, (bits + passes - 1) / passes, key[0], pos[0], f);
+  } else {
+    const int passes = (bits + kMaxDigit - 1) / kMaxDigit, each = (bits + passes - 1) / passes;
     SortPass p = {};
     p.vocab = vocab;
     p.token_bytes = token_bytes;
@@ -422,37 +545,43 @@ hipError_t launch_embedding_grad(int elt, const void* grad_out, int64_t ld_grad,
       p.pos_out = pos[1 - cur];
       p.shift = k * each;
       p.bits = std::min(each, bits - k * each);
-      hipLaunchKernelGGL(sort_count_kernel, dim3(p.blocks), dim3(256), 0, s, p);
+      hipLaunchKernelGGL(sort_count_kernel, dim3(p.blocks + (k == 0 ? fills(4096) : 0u)), dim3(256), 0, s, p, f);
       hipLaunchKernelGGL(sort_scan_kernel, dim3(1), dim3(1024), 0, s, p.hist, p.blocks << p.bits);
       hipLaunchKernelGGL(sort_scatter_kernel, dim3(p.blocks), dim3(256), 0, s, p);
       cur = 1 - cur;
     }
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
   }
-  const int strips = (int)((d + kStrip - 1) / kStrip);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || n == 0) return e;
   const int64_t ldp = part_ld(d), n_groups = n / kRun;
   const bool al = (uintptr_t)grad_out % (4 * elt) == 0 && ld_grad % 4 == 0 && (uintptr_t)grad_table % 16 == 0 &&
                   ld_table % 4 == 0 && d % 4 == 0;
   float* part = (float*)(ws + L.off_part);
-  const int64_t blocks = (vocab + kRowsPerBlock - 1) / kRowsPerBlock;
-  if (blocks > INT32_MAX) return hipErrorInvalidValue;
-  auto go = [&](auto groups_kernel, auto rows_kernel) {
+  // 16 columns per lane while that leaves the chip 32 waves per CU (16384
+  // positions x 4096 columns: 74 us, 8 columns 84, 4 93), else 4 (509 x 769: 6 us, 16 11)
+  const bool wide = n * ((d + 1023) / 1024) >= 8192;
+  auto go = [&](auto groups_kernel, auto wide_kernel, auto narrow_kernel) {
+    const int row_cols = wide ? 16 : 4;
+    const int64_t gs = (d + 255) / 256, rs = (d + 64 * row_cols - 1) / (64 * row_cols);
+    const int64_t gb = (n_groups * gs + 3) / 4, rb = (n * rs + 3) / 4;
+    if (gb > INT32_MAX || rb > INT32_MAX) return hipErrorInvalidValue;
     if (n_groups > 0)
-      hipLaunchKernelGGL(groups_kernel, dim3((unsigned)((n_groups + 3) / 4), strips), dim3(256), 0, s,
-                         (const uint8_t*)grad_out, ld_grad, (int)d, key[cur], pos[cur], (int)n_groups, (uint32_t)vocab,
-                         part, ldp);
-    const int strips_each = 4, groups = (strips + strips_each - 1) / strips_each;
-    hipLaunchKernelGGL(rows_kernel, dim3((unsigned)blocks, groups), dim3(256), 0, s, (const uint8_t*)grad_out, ld_grad,
-                       (int)d, key[cur], pos[cur], (int)n, part, ldp, scale, vocab, strips_each, grad_table, ld_table,
-                       (int)accumulate);
+      hipLaunchKernelGGL(groups_kernel, dim3((unsigned)gb), dim3(256), 0, s, (const uint8_t*)grad_out, ld_grad, (int)d,
+                         key[cur], pos[cur], (int)n_groups, (uint32_t)vocab, part, ldp, (int)gs);
+    hipLaunchKernelGGL(wide ? wide_kernel : narrow_kernel, dim3((unsigned)rb), dim3(256), 0, s, (const uint8_t*)grad_out, ld_grad, (int)d,
+                       key[cur], pos[cur], (int)n, part, ldp, scale, (uint32_t)vocab, grad_table, ld_table,
+                       (int)accumulate, (int)rs);
     return hipGetLastError();
   };
   if (elt == 2)
-    return al ? go(embgrad_groups_kernel<2, kCols4>, embgrad_rows_kernel<2, kCols4>)
-              : go(embgrad_groups_kernel<2, kCols1>, embgrad_rows_kernel<2, kCols1>);
-  return al ? go(embgrad_groups_kernel<4, kCols4>, embgrad_rows_kernel<4, kCols4>)
-            : go(embgrad_groups_kernel<4, kCols1>, embgrad_rows_kernel<4, kCols1>);
+    return al ? go(embgrad_groups_kernel<2, kCols4>, embgrad_rows_kernel<2, kCols4, 16>,
+                    embgrad_rows_kernel<2, kCols4, 4>)
+              : go(embgrad_groups_kernel<2, kCols1>, embgrad_rows_kernel<2, kCols1, 16>,
+                    embgrad_rows_kernel<2, kCols1, 4>);
+  return al ? go(embgrad_groups_kernel<4, kCols4>, embgrad_rows_kernel<4, kCols4, 16>,
+                    embgrad_rows_kernel<4, kCols4, 4>)
+            : go(embgrad_groups_kernel<4, kCols1>, embgrad_rows_kernel<4, kCols1, 16>,
+                    embgrad_rows_kernel<4, kCols1, 4>);
 }
 
 }  // namespace dattri
