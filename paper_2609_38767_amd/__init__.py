@@ -9,6 +9,7 @@ no fallback: if libdattri.so is missing, every call raises.
 
 Build the library with ``python -m paper_2609_38767_amd.build``.
 """
+import array
 import ctypes
 import os
 
@@ -206,7 +207,9 @@ def _ptr(x):
 
 
 def _host(x):
-    """Address of a host array (ctypes or numpy), or None."""
+    """Address of a host array (array.array, ctypes or numpy), or None."""
+    if isinstance(x, array.array):
+        return x.buffer_info()[0]
     return ctypes.addressof(x) if isinstance(x, ctypes.Array) else _ptr(x)
 
 
@@ -623,7 +626,7 @@ def dattri_linear_weight_grad(G, ld_g, X, ld_x, dW, ld_dw, dbias, accumulate, ro
 
 
 def dattri_clip_workspace_bytes(sizes, n_tensors):
-    """sizes: a ctypes or numpy int64 array."""
+    """sizes: a host array of int64."""
     v = _sz()
     _check(load().dattri_clip_workspace_bytes(_host(sizes), n_tensors, ctypes.byref(v)), "dattri_clip_workspace_bytes")
     return v.value
@@ -631,7 +634,7 @@ def dattri_clip_workspace_bytes(sizes, n_tensors):
 
 def dattri_clip_gradients(grads, sizes, dtypes, outs, out_dtypes, n_tensors, max_norm, norm_coef, workspace, ws_bytes,
                           stream=None):
-    """grads, outs: ctypes or numpy arrays of device addresses; sizes int64, dtypes int32 likewise."""
+    """Host arrays: grads, outs of device addresses, sizes of int64, dtypes of int32."""
     _check(load().dattri_clip_gradients(_host(grads), _host(sizes), _host(dtypes), _host(outs), _host(out_dtypes),
                                         n_tensors, max_norm, _ptr(norm_coef), _ptr(workspace), ws_bytes,
                                         _stream(stream)), "dattri_clip_gradients")

@@ -11,7 +11,8 @@ using namespace dattri;
 
 namespace {
 
-constexpr int64_t kMaxWidth = (int64_t)1 << 24;  // columns of a row: grids and 32-bit offsets within a tile
+constexpr int64_t kClipStream = (int64_t)256 << 20;  // bytes (gradients and other buffers written) that no cache holds
+constexpr int64_t kMaxWidth = (int64_t)1 << 23;  // columns of a row: 256 of them stay below 4 GiB in any type
 
 dattri_status elt_of(dattri_dtype dtype, int* elt) {
   if (dtype != DATTRI_F32 && dtype != DATTRI_BF16)
@@ -22,7 +23,7 @@ dattri_status elt_of(dattri_dtype dtype, int* elt) {
 
 dattri_status check_width(const char* what, int64_t d) {
   if (d < 1) return fail(DATTRI_E_INVALID_ARG, "%s must be >= 1 (got %lld)", what, (long long)d);
-  if (d > kMaxWidth) return fail(DATTRI_E_UNSUPPORTED, "%s=%lld exceeds 2^24", what, (long long)d);
+  if (d > kMaxWidth) return fail(DATTRI_E_UNSUPPORTED, "%s=%lld exceeds 2^23", what, (long long)d);
   return DATTRI_OK;
 }
 
@@ -359,21 +360,21 @@ dattri_status dattri_clip_gradients(const void* const* grads, const int64_t* siz
   TRY(check_workspace(workspace, ws_bytes, align_up(std::max<size_t>((size_t)n_partials * 8, kAlign))));
   hipStream_t s = (hipStream_t)stream;
   double* partials = (double*)workspace;
+  int64_t bytes = 0;
+  for (int64_t i = 0; i < n_tensors; ++i)
+    bytes += sizes[i] * ((dtypes[i] == DATTRI_F32 ? 4 : 2) + (!outs || outs[i] == grads[i] ? 0 : out_dtypes[i] == DATTRI_F32 ? 4 : 2));
   int at = 0;
   TRY(clip_launches(grads, sizes, dtypes, outs, out_dtypes, n_tensors,
                     [&](const ClipList& l, int groups) -> dattri_status {
-                      HIP_TRY(launch_clip_squares(l, groups, partials + at, s));
+                      HIP_TRY(launch_clip_squares(l, groups, partials + at, bytes > kClipStream, s));
                       at += groups;
                       return DATTRI_OK;
                     }));
-  if (!outs || at == 0) {
-    HIP_TRY(launch_clip_norm(partials, at, max_norm, norm_coef, s));
-    return DATTRI_OK;
-  }
+  HIP_TRY(launch_clip_norm(partials, at, max_norm, norm_coef, s));
+  if (!outs) return DATTRI_OK;
   return clip_launches(grads, sizes, dtypes, outs, out_dtypes, n_tensors,
-                       [&](const ClipList& l, int groups) -> dattri_status {
-                         HIP_TRY(launch_clip_scale(l, groups, partials, at, max_norm, norm_coef, s));
-                         norm_coef = nullptr;  // written once
+                       [&](const ClipList& l, int) -> dattri_status {
+                         HIP_TRY(launch_clip_scale(l, norm_coef, bytes > kClipStream, s));
                          return DATTRI_OK;
                        });
 }

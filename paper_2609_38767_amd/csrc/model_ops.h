@@ -57,7 +57,7 @@ hipError_t launch_linear(dattri_linear_op op, int elt, bool aligned, GemmArgs a,
 // ------------------------------------------------------------------ clip
 constexpr int kClipTensors = 128;    // tensors per launch (their list is a kernel argument)
 constexpr int kClipChunk = 16384;    // elements per unit of work
-constexpr int kClipGroups = 2048;    // most workgroups of one launch, each writing one partial sum
+constexpr int kClipGroups = 2048;    // most workgroups of the norm's launch, each writing one partial sum
 struct ClipTensor {
   const void* src;
   void* dst;           // null: norm only
@@ -69,9 +69,9 @@ struct ClipList {
   int first[kClipTensors + 1];  // first chunk of each tensor, then the number of chunks
 };
 static_assert(sizeof(ClipList) <= 3840, "kernel argument size");
-hipError_t launch_clip_squares(const ClipList& l, int groups, double* partials, hipStream_t s);
-hipError_t launch_clip_scale(const ClipList& l, int groups, const double* partials, int n_partials, float max_norm,
-                             float* norm_coef, hipStream_t s);
+// stream: loads and stores past the caches
+hipError_t launch_clip_squares(const ClipList& l, int groups, double* partials, bool stream, hipStream_t s);
 hipError_t launch_clip_norm(const double* partials, int n_partials, float max_norm, float* norm_coef, hipStream_t s);
+hipError_t launch_clip_scale(const ClipList& l, const float* norm_coef, bool stream, hipStream_t s);
 
 }  // namespace dattri

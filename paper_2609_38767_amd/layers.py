@@ -12,7 +12,8 @@ between rows (a contiguous tensor, or a view of padded rows).  ``stream`` is a
 torch stream, a raw handle or None (the current one); outputs and workspaces
 are allocated on the stream that the call runs on.
 """
-import ctypes
+from array import array
+from operator import attrgetter
 
 import torch
 
@@ -25,6 +26,7 @@ from . import (DATTRI_BF16, DATTRI_F32, DATTRI_ACT_GELU, DATTRI_ACT_GELU_TANH, D
 ACTS = {"none": DATTRI_ACT_NONE, "relu": DATTRI_ACT_RELU, "gelu": DATTRI_ACT_GELU,
         "gelu_tanh": DATTRI_ACT_GELU_TANH, "silu": DATTRI_ACT_SILU}
 _CODES = {torch.float32: DATTRI_F32, torch.bfloat16: DATTRI_BF16}
+_dtype = attrgetter("dtype")
 
 
 def _elsewhere(t, stream):
@@ -253,36 +255,39 @@ def linear_weight_grad(g, x, bias=False, out=None, out_bias=None, accumulate=Fal
     return (out, out_bias) if bias else out
 
 
-def _host_list(tensors, what):
-    """Host arrays of the tensors' addresses, element counts and types."""
-    for t in tensors:
-        if not t.is_contiguous():
-            raise ValueError(f"{what} must be contiguous")
-    n = len(tensors)
+def _host_list(tensors, what, device):
+    """Host arrays of the tensors' addresses, element counts and types.  Whole
+    lists at a time: a training step hands over hundreds of small tensors."""
+    T, n = torch.Tensor, len(tensors)
+    if set(map(T.get_device, tensors)) != {device}:
+        raise ValueError(f"{what} must be on one GPU")
+    if not all(map(T.is_contiguous, tensors)):
+        raise ValueError(f"{what} must be contiguous")
     try:
-        types = (ctypes.c_int32 * n)(*[_CODES[t.dtype] for t in tensors])
+        types = array("i", map(_CODES.__getitem__, map(_dtype, tensors)))
     except KeyError:
         raise ValueError(f"{what} must be float32 or bfloat16") from None
-    return (ctypes.c_void_p * n)(*[t.data_ptr() for t in tensors]), \
-        (ctypes.c_int64 * n)(*[t.numel() for t in tensors]), types
+    return array("Q", map(T.data_ptr, tensors)), array("q", map(T.numel, tensors)), types
 
 
 def _clip(grads, max_norm, out, stream):
-    grads = list(grads)
+    grads = grads if isinstance(grads, list) else list(grads)
     if not grads:
         raise ValueError("no gradients")
-    out = None if out is None else list(out)
-    _on_gpu(*grads, *(out or ()))
+    _on_gpu(grads[0])
     ctx = _elsewhere(grads[0], stream)
     if ctx is not None:
         with ctx:
             return _clip(grads, max_norm, out, None)
-    src, sizes, types = _host_list(grads, "gradients")
+    device = grads[0].get_device()
+    src, sizes, types = _host_list(grads, "gradients", device)
     dst = otypes = None
-    if out is not None:
-        if [t.shape for t in out] != [t.shape for t in grads]:
-            raise ValueError("out must have the gradients' shapes")
-        dst, _, otypes = _host_list(out, "out")
+    if out is grads:
+        dst, otypes = src, types
+    elif out is not None:
+        dst, osizes, otypes = _host_list(list(out), "out", device)
+        if osizes != sizes:
+            raise ValueError("out must have the gradients' sizes")
     norm_coef = torch.empty(2, dtype=torch.float32, device=grads[0].device)
     n = len(grads)
     ws_bytes = dattri_clip_workspace_bytes(sizes, n)
@@ -298,7 +303,7 @@ def gradient_norm(grads, stream=None):
 
 def clip_gradients(grads, max_norm, out=None, stream=None):
     """Scales the gradients so that their 2-norm together is at most max_norm,
-    in place or into `out` (tensors of the same shapes, float32 or bfloat16).
+    in place or into `out` (tensors of the same sizes, float32 or bfloat16).
     Returns (norm before, coefficient), float32 scalars on the GPU."""
     grads = list(grads)
     return _clip(grads, max_norm, grads if out is None else out, stream)
