@@ -7,19 +7,21 @@
 // v_mfma_f32_32x32x16_bf16, float32 ones v_mfma_f32_32x32x2f32.  Operands come
 // to LDS by direct loads (16 bytes per lane) in stages of 128 bytes of k (64
 // bf16, 32 float32), in the order they have in memory:
-//   k contiguous: [row][128 bytes], 16-byte chunks XORed by row % 8; a fragment
+//   k contiguous: [row][128 bytes], 16-byte chunks XORed by row / 2 % 8; a fragment
 //     is one 16-byte read per lane: 8 bf16, or 4 float32 that serve four MFMA
 //     (slot j of half-wave h is k = 4h + j for both operands);
 //   k strided: [k][row], read across with the transposing LDS read (bf16) or
 //     by 4-byte reads of 32 neighbouring rows (float32); chunks XORed by k so
 //     that the k rows of one read lie in different banks.
-// Two stage buffers.  A stage's four K steps are read two steps ahead of their
-// products, so halfway through a stage all of it is in registers; the one
-// barrier per stage sits there, behind it the buffer takes the loads of the
-// stage after next, which then have a whole stage of products to arrive.
+// Two stage buffers.  A stage's four K steps are read during the two steps
+// before it and its own first; its buffer is then empty and takes the loads of
+// the stage after next, which have five of eight K steps to arrive (the wait
+// counts: those issued last may still be under way).  Reading each step two
+// steps ahead left them four at most, and the matrix cores half idle at 1000
+// TFLOP/s.
 //
-// Rows past M or N repeat the last row (their outputs are not stored); k past K
-// reads as zero on both sides, so no product meets what lies behind a row.
+// Rows past M or N and k past K read as zero, so no product meets what lies
+// behind a row.
 //
 // The accumulators leave through LDS, 32 columns of blocks at a time as float32
 // rows, so that the epilogue is one short loop over whole rows: its loads and
@@ -44,11 +46,8 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 __device__ inline void wait_all() {  // this wave's loads are in LDS, its LDS reads done
   __builtin_amdgcn_s_waitcnt(0x70);  // vmcnt 0, lgkmcnt 0, other counters untouched
 }
+__device__ inline void plain_barrier() { asm volatile("s_barrier" ::: "memory"); }
 __device__ inline void stage_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
-
-__device__ inline void direct_load(rsrc_t r, uint8_t* lds, uint32_t off) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, DATTRI_LDS_PTR(lds), 16, off, 0, 0, 0);
-}
 
 // Transposing LDS read: lane 4r + c of every 16 addresses four bf16 of k row r,
 // lane j receives the four k of column j.
@@ -66,52 +65,61 @@ struct Side {
   static constexpr int CH = R * ELT / 16;               // chunks per k row (strided)
   static constexpr int kReads = KC ? 1 : ELT == 2 ? 2 : 4;  // LDS reads per fragment
 
+  // A direct load moves 1 KiB, 64 chunks: kRows rows of a stage buffer (of the
+  // operand or of k).  Its rows lie kRows * j further than load 0's; the swizzle
+  // has two variants over j.
+  static constexpr int kRows = KC ? 8 : 64 / CH;
+  static constexpr int kShift = KC || ELT == 2 ? 0 : R == 256 ? 2 : 1;  // variant (j >> kShift) & 1
+
   const uint8_t* base;  // the tile's first row (KC) or column (strided) at k = 0
-  int64_t ld;           // bytes
+  uint32_t ld;          // bytes
   int rows, K;
-  rsrc_t rs;         // KC: the tile's rows
-  uint32_t off[kLoads];  // KC: this lane's chunk of each load at k = 0 of the stage; strided: from the stage's first k row
-  int kc;            // KC: k of this lane's chunk within the stage
+  uint32_t off[2];  // this lane's chunk of a load of each variant, from the load's first row
+  int kc[2];        // KC: its k within the stage
 
   __device__ static int swz(int k) { return ELT == 2 ? 2 * (k & 3) + 8 * (k & 1) : 8 * ((k >> 2) & 1); }
 
   __device__ void init(const void* p, int64_t ld_elts, int row0, int n_rows, int K_, int wave, int lane) {
-    ld = ld_elts * ELT;
+    ld = (uint32_t)(ld_elts * ELT);
     rows = min(R, n_rows - row0);
     K = K_;
-    if constexpr (KC) {
-      base = (const uint8_t*)p + (int64_t)row0 * ld;
-      // rows are whole 16-byte chunks (repacked rows end in zeros)
-      rs = make_rsrc(base, (uint32_t)((int64_t)(rows - 1) * ld + ((int64_t)K * ELT + 15) / 16 * 16));
-      const int r8 = lane >> 3;
-      kc = ((lane & 7) ^ r8) * EPL;
+    base = (const uint8_t*)p + (KC ? (int64_t)row0 * ld : (int64_t)row0 * ELT);
 #pragma unroll
-      for (int j = 0; j < kLoads; ++j) {
-        const int row = min((wave * kLoads + j) * 8 + r8, rows - 1);
-        off[j] = (uint32_t)((int64_t)row * ld + kc * ELT);
-      }
-    } else {
-      base = (const uint8_t*)p + (int64_t)row0 * ELT;
-#pragma unroll
-      for (int j = 0; j < kLoads; ++j) {
-        const int slot = (wave * kLoads + j) * 64 + lane, k = slot / CH, c = slot % CH;
-        off[j] = (uint32_t)((int64_t)k * ld + ((c ^ (swz(k) & (CH - 1))) << 4));
+    for (int v = 0; v < 2; ++v) {
+      const int j = wave * kLoads + (v << kShift);
+      if constexpr (KC) {
+        const int r = lane >> 3;
+        kc[v] = ((lane & 7) ^ (((j * 8 + r) >> 1) & 7)) * EPL;
+        off[v] = r * ld + kc[v] * ELT;
+      } else {
+        const int r = lane / CH, c = lane % CH;
+        off[v] = r * ld + ((c ^ (swz(j * kRows + r) & (CH - 1))) << 4);
+        kc[v] = 0;
       }
     }
   }
 
-  // The direct loads of stage st into `buf` (this side's part of a stage buffer).
-  __device__ void load(int st, uint8_t* buf, int wave, int j) const {
-    uint8_t* d = buf + (wave * kLoads + j) * 1024;
+  // What stage st may read: from its first k to the last row's end (rows are
+  // whole 16-byte chunks, repacked ones end in zeros); past the last k nothing.
+  // Fits 32 bits: 256 rows stay below 4 GiB, st * BK is past K by three stages at most.
+  __device__ rsrc_t range(int st) const {
+    const int left = (int)((uint32_t)K - (uint32_t)st * BK);
     if constexpr (KC) {
-      const int k0 = st * BK;
-      const uint32_t o = k0 + kc < K ? off[j] + (uint32_t)k0 * ELT : kOOB;
-      direct_load(rs, d, o);
+      const uint32_t bytes = (uint32_t)(rows - 1) * ld + ((uint32_t)left * ELT + 15) / 16 * 16;
+      return make_rsrc(base + (int64_t)st * 128, left > 0 ? bytes : 0);
     } else {
-      const int64_t left = K - (int64_t)st * BK;  // k rows that exist from here on; none: an empty range
-      const int64_t bytes = left > 0 ? (min(left, (int64_t)BK) - 1) * ld + ((int64_t)rows * ELT + 15) / 16 * 16 : 0;
-      direct_load(make_rsrc(base + (int64_t)st * BK * ld, (uint32_t)bytes), d, off[j]);
+      const uint32_t bytes = (uint32_t)(min(left, BK) - 1) * ld + ((uint32_t)rows * ELT + 15) / 16 * 16;
+      return make_rsrc(base + (int64_t)st * BK * ld, left > 0 ? bytes : 0);
     }
+  }
+  // Direct load j of stage st (r: its range) into `buf`, this side's part of a
+  // stage buffer.  Rows past the last (KC) and k past K read as zero; KC, where
+  // the next row lies behind K: by an offset out of range.
+  __device__ void load(rsrc_t r, int st, uint8_t* buf, int wave, int j) const {
+    const int v = (j >> kShift) & 1, at = wave * kLoads + j;
+    uint32_t o = off[v] + (uint32_t)(at * kRows) * ld;
+    if (KC && kc[v] >= (int)((uint32_t)K - (uint32_t)st * BK)) o = kOOB;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, DATTRI_LDS_PTR(buf + at * 1024), 16, o, 0, 0, 0);
   }
 
   // Fragment of K step s of the 32-row block at row w0 + 32 i: lane l holds row
@@ -120,7 +128,9 @@ struct Side {
   __device__ static void read(const uint8_t* buf, int s, int w0, int lane, i32x4 (&f)[NB]) {
     const int l32 = lane & 31, h = lane >> 5;
     if constexpr (KC) {
-      const uint8_t* p = buf + (w0 + l32) * 128 + (((2 * s + h) ^ (l32 & 7)) << 4);
+      uint32_t o = ((w0 + l32) * 128 + ((h ^ ((l32 >> 1) & 7)) << 4)) ^ (s << 5);
+      asm volatile("" : "+v"(o));  // formed where it is used: kept for every step and buffer they would not fit
+      const uint8_t* p = buf + o;
 #pragma unroll
       for (int i = 0; i < NB; ++i) f[i] = *(const i32x4*)(p + i * 4096);
     } else if constexpr (ELT == 2) {
@@ -172,19 +182,16 @@ __device__ inline void step_mma(const i32x4 (&b)[BN], const i32x4 (&a)[BM], f32x
   }
 }
 
-// Deals a step's LDS reads (first half) and direct loads (second half) out
-// between its MFMA.
+// Deals a step's LDS reads and direct loads out between the first half of its MFMA.
 template <int BLOCKS, int READS, int LOADS, int I = 0>
 __device__ inline void spread() {
-  constexpr int kFirst = (BLOCKS + 1) / 2, kRest = BLOCKS - kFirst;
+  constexpr int kFirst = (BLOCKS + 1) / 2;
   if constexpr (I < BLOCKS) {
     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
     if constexpr (I < kFirst) {
-      constexpr int n = READS * (I + 1) / kFirst - READS * I / kFirst;
-      if constexpr (n > 0) __builtin_amdgcn_sched_group_barrier(0x100, n, 0);
-    } else {
-      constexpr int n = LOADS * (I - kFirst + 1) / kRest - LOADS * (I - kFirst) / kRest;
-      if constexpr (n > 0) __builtin_amdgcn_sched_group_barrier(0x020, n, 0);
+      constexpr int r = READS * (I + 1) / kFirst - READS * I / kFirst, l = LOADS * (I + 1) / kFirst - LOADS * I / kFirst;
+      if constexpr (r > 0) __builtin_amdgcn_sched_group_barrier(0x100, r, 0);
+      if constexpr (l > 0) __builtin_amdgcn_sched_group_barrier(0x020, l, 0);
     }
     spread<BLOCKS, READS, LOADS, I + 1>();
   }
@@ -239,44 +246,48 @@ __global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void gemm_kernel(GemmAr
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
 
-  i32x4 fb[4][BN], fa[4][BM];
+  i32x4 fb[4][BN], fa[4][BM];  // fragments of a stage's K steps
   auto read = [&](const uint8_t* x, int s) {
     SA::template read<BM>(x, s, wm * BM * 32, lane, fa[s]);
     SB::template read<BN>(x + SA::kBytes, s, wn * BN * 32, lane, fb[s]);
   };
-  auto issue = [&](int st, uint8_t* x, int half) {  // loads half, half + 2, ... of each side
+  auto issue = [&](int st, uint8_t* x) {
+    const rsrc_t ra = sa.range(s0 + st), rb = sb.range(s0 + st);
 #pragma unroll
-    for (int j = half; j < SA::kLoads; j += 2) sa.load(s0 + st, x, wave, j);
+    for (int j = 0; j < SA::kLoads; ++j) sa.load(ra, s0 + st, x, wave, j);
 #pragma unroll
-    for (int j = half; j < SB::kLoads; j += 2) sb.load(s0 + st, x + SA::kBytes, wave, j);
+    for (int j = 0; j < SB::kLoads; ++j) sb.load(rb, s0 + st, x + SA::kBytes, wave, j);
   };
+  constexpr int kLoads = SA::kLoads + SB::kLoads, kReads = SA::kReads * BM + SB::kReads * BN;
+  constexpr int kMma = BN * BM * (ELT == 2 ? 1 : 4);
   if (ns > 0) {
-    issue(0, x0, 0);
-    issue(0, x0, 1);
-    issue(1, x1, 0);
-    issue(1, x1, 1);
-    wait_all();
-    stage_barrier();
+    issue(0, x0);
+    issue(1, x1);
+    wait_vmcnt_dma<kLoads>();
+    plain_barrier();
     read(x0, 0);
     read(x0, 1);
-    // loads past the last stage fetch nothing (their k is past the sides' K) and fill with zeros
+    read(x0, 2);
+    // K steps 0 .. 2 of stage st are in registers or asked for, st + 1 is on its
+    // way to nx.  Loads past the last stage fetch nothing (their k is past the
+    // sides' K) and fill with zeros.
     auto stage = [&](int st, uint8_t* cx, const uint8_t* nx) {
-      read(cx, 2);
-      step_mma<ELT, BN, BM>(fb[0], fa[0], acc);
-      spread<BN * BM * (ELT == 2 ? 1 : 4), SA::kReads * BM + SB::kReads * BN, 0>();
       read(cx, 3);
+      step_mma<ELT, BN, BM>(fb[0], fa[0], acc);
+      spread<kMma, kReads, 0>();
+      stage_barrier();  // the stage is in registers, its buffer free
+      issue(st + 2, cx);
       step_mma<ELT, BN, BM>(fb[1], fa[1], acc);
-      spread<BN * BM * (ELT == 2 ? 1 : 4), SA::kReads * BM + SB::kReads * BN, 0>();
-      wait_all();  // stage st + 1 has landed, this stage is in registers
-      stage_barrier();
-      issue(st + 2, cx, 0);
+      spread<kMma, 0, kLoads>();
+      wait_vmcnt_dma<kLoads>();  // all but the loads just issued: stage st + 1 has landed
+      plain_barrier();
       read(nx, 0);
-      step_mma<ELT, BN, BM>(fb[2], fa[2], acc);
-      spread<BN * BM * (ELT == 2 ? 1 : 4), SA::kReads * BM + SB::kReads * BN, (SA::kLoads + 1) / 2 + (SB::kLoads + 1) / 2>();
-      issue(st + 2, cx, 1);
       read(nx, 1);
+      step_mma<ELT, BN, BM>(fb[2], fa[2], acc);
+      spread<kMma, 2 * kReads, 0>();
+      read(nx, 2);
       step_mma<ELT, BN, BM>(fb[3], fa[3], acc);
-      spread<BN * BM * (ELT == 2 ? 1 : 4), SA::kReads * BM + SB::kReads * BN, SA::kLoads / 2 + SB::kLoads / 2>();
+      spread<kMma, kReads, 0>();
     };
     for (int st = 0; st < ns; st += 2) {  // an odd last stage is followed by one of zeros
       stage(st, x0, x1);
