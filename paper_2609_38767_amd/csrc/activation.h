@@ -12,6 +12,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "dattri.h"
 
 namespace dattri {
@@ -69,6 +71,23 @@ __device__ inline float act_slope(float z, int act) {
     }
     default:
       return 1.f;
+  }
+}
+
+// f(activation as a constant)
+template <class F>
+__device__ inline void with_act(int act, F f) {
+  switch (act) {
+    case DATTRI_ACT_RELU:
+      return f(std::integral_constant<int, DATTRI_ACT_RELU>{});
+    case DATTRI_ACT_GELU:
+      return f(std::integral_constant<int, DATTRI_ACT_GELU>{});
+    case DATTRI_ACT_GELU_TANH:
+      return f(std::integral_constant<int, DATTRI_ACT_GELU_TANH>{});
+    case DATTRI_ACT_SILU:
+      return f(std::integral_constant<int, DATTRI_ACT_SILU>{});
+    default:
+      return;
   }
 }
 

@@ -56,6 +56,27 @@ __device__ inline void store4_elt(void* p, int64_t i, f32x4 v, bool vec, int cnt
     if (e < cnt) store_elt<ELT>(p, i + e, v[e]);
 }
 
+// v = act(v); v *= act'(z).  One choice of activation for four values.
+template <int ELT>
+__device__ inline void act_values(f32x4& v, int act) {
+  auto each = [&](auto kind) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = act_value<ELT>(v[e], decltype(kind)::value);
+  };
+  with_act(act, each);
+}
+template <int ELT>
+__device__ inline void slope_values(f32x4& v, f32x4 z, int act) {
+  auto each = [&](auto kind) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float s = act_slope<ELT>(z[e], decltype(kind)::value);
+      v[e] = decltype(kind)::value == DATTRI_ACT_RELU && s == 0.f ? 0.f : v[e] * s;  // a closed relu passes nothing, not 0 * inf
+    }
+  };
+  with_act(act, each);
+}
+
 // m < M and n < N; a.vec: every row of the epilogue's buffers starts on four elements.
 template <int OP, int ELT>
 __device__ inline void epilogue4(const GemmArgs& a, int m, int n, f32x4 v) {
@@ -66,8 +87,7 @@ __device__ inline void epilogue4(const GemmArgs& a, int m, int n, f32x4 v) {
     if (a.Z) store4_elt<ELT>(a.Z, m * a.ldz + n, v, vec, cnt);
     f32x4 r = {0.f, 0.f, 0.f, 0.f};
     if (a.R) r = load4_elt<ELT>(a.R, m * a.ldr + n, vec, cnt);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = act_value<ELT>(v[e], a.act);
+    act_values<ELT>(v, a.act);
     if (a.R) v += r;
     store4_elt<ELT>(a.out, m * a.ldo + n, v, vec, cnt);
   } else if constexpr (OP == DATTRI_LINEAR_INPUT_GRAD) {
@@ -77,19 +97,119 @@ __device__ inline void epilogue4(const GemmArgs& a, int m, int n, f32x4 v) {
     if (a.R) v += load4_elt<ELT>(a.R, m * a.ldr + n, vec, cnt);
     if (a.out) store4_elt<ELT>(a.out, m * a.ldo + n, v, vec, cnt);
     if (!a.out2) return;
-    if (slope) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float s = act_slope<ELT>(z[e], a.act);
-        v[e] = a.act == DATTRI_ACT_RELU && s == 0.f ? 0.f : v[e] * s;  // a closed relu passes nothing, not 0 * inf
-      }
-    }
+    if (slope) slope_values<ELT>(v, z, a.act);
     store4_elt<ELT>(a.out2, m * a.ldo2 + n, v, vec, cnt);
   } else {
     if (a.accumulate) v += load4_elt<4>(a.out, m * a.ldo + n, vec, cnt);
     store4_elt<4>(a.out, m * a.ldo + n, v, vec, cnt);
   }
 }
+
+// Four elements of a buffer at byte offset `off` (range checked).
+template <int ELT>
+__device__ inline f32x4 buffer_load4(rsrc_t r, uint32_t off) {
+  if constexpr (ELT == 2) {
+    const i32x2 w = load8(r, off);
+    const uint32_t a = (uint32_t)w.x, b = (uint32_t)w.y;
+    return f32x4{__builtin_bit_cast(float, a << 16), __builtin_bit_cast(float, a & 0xFFFF0000u),
+                 __builtin_bit_cast(float, b << 16), __builtin_bit_cast(float, b & 0xFFFF0000u)};
+  } else {
+    return __builtin_bit_cast(f32x4, load16(r, off));
+  }
+}
+template <int ELT>
+__device__ inline void buffer_store4(rsrc_t r, uint32_t off, f32x4 v) {
+  if constexpr (ELT == 2)
+    __builtin_amdgcn_raw_buffer_store_b64(i32x2{(int)pack_bf16(v.x, v.y), (int)pack_bf16(v.z, v.w)}, r, off, 0, 0);
+  else
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(i32x4, v), r, off, 0, 0);
+}
+
+// A buffer of the epilogue seen from a tile: rows m0 .. (rows of them exist),
+// columns n0 .. n0 + width - 1.  Rows past the last are out of its range.
+template <int ELT>
+struct TileRows {
+  rsrc_t r;
+  uint32_t ld;
+  __device__ TileRows(const void* p, int64_t ld_elts, int m0, int n0, int rows, int width) {
+    ld = (uint32_t)(ld_elts * ELT);
+    r = make_rsrc((const uint8_t*)p + ((int64_t)m0 * ld_elts + n0) * ELT,
+                  p ? (uint32_t)(rows - 1) * ld + (uint32_t)width * ELT : 0u);
+  }
+};
+
+// epilogue4 for U rows at once: v[u] are elements (rows at[u], columns n .. n + 3)
+// of the tile at (m0, n0), all buffers on four elements.  Rows past the
+// tile's may be passed: what they store is dropped by the range checks.
+template <int OP, int ELT, int U>
+struct TileEpilogue {
+  static constexpr int OELT = OP == DATTRI_LINEAR_WEIGHT_GRAD ? 4 : ELT;
+  const GemmArgs& a;
+  TileRows<OELT> out;
+  TileRows<ELT> out2, z, r;
+  f32x4 bias;
+  uint32_t n;
+  __device__ TileEpilogue(const GemmArgs& a_, int m0, int n0, int rows, int width, int col)
+      : a(a_), out(a_.out, a_.ldo, m0, n0, rows, width), out2(a_.out2, a_.ldo2, m0, n0, rows, width),
+        z(a_.Z, a_.ldz, m0, n0, rows, width), r(a_.R, a_.ldr, m0, n0, rows, width), bias{0.f, 0.f, 0.f, 0.f},
+        n((uint32_t)col) {
+    if (OP == DATTRI_LINEAR_FORWARD && a.bias) bias = load4_elt<ELT>(a.bias, n0 + col, true, 4);
+  }
+  __device__ void run(const int (&at)[U], f32x4 (&v)[U]) const {
+    f32x4 x[U], y[U];
+    if (OP != DATTRI_LINEAR_WEIGHT_GRAD && a.R) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) x[u] = buffer_load4<ELT>(r.r, at[u] * r.ld + n * ELT);
+    }
+    if constexpr (OP == DATTRI_LINEAR_FORWARD) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] += bias;
+      if (a.Z) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) buffer_store4<ELT>(z.r, at[u] * z.ld + n * ELT, v[u]);
+      }
+      if (a.act != DATTRI_ACT_NONE) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) act_values<ELT>(v[u], a.act);
+      }
+      if (a.R) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] += x[u];
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) buffer_store4<ELT>(out.r, at[u] * out.ld + n * ELT, v[u]);
+    } else if constexpr (OP == DATTRI_LINEAR_INPUT_GRAD) {
+      const bool slope = a.out2 && a.act != DATTRI_ACT_NONE;
+      if (slope) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) y[u] = buffer_load4<ELT>(z.r, at[u] * z.ld + n * ELT);
+      }
+      if (a.R) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] += x[u];
+      }
+      if (a.out) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) buffer_store4<ELT>(out.r, at[u] * out.ld + n * ELT, v[u]);
+      }
+      if (slope) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) slope_values<ELT>(v[u], y[u], a.act);
+      }
+      if (a.out2) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) buffer_store4<ELT>(out2.r, at[u] * out2.ld + n * ELT, v[u]);
+      }
+    } else {
+      if (a.accumulate) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] += buffer_load4<4>(out.r, at[u] * out.ld + n * 4);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) buffer_store4<4>(out.r, at[u] * out.ld + n * 4, v[u]);
+    }
+  }
+};
 
 }  // namespace dev
 }  // namespace dattri

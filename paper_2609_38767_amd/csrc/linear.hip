@@ -300,6 +300,9 @@ __global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void gemm_kernel(GemmAr
   // row so that the lanes' writes (32 rows of one chunk) spread over the banks.
   const int l32 = lane & 31, h = lane >> 5;
   constexpr int LPR = TN / 4;  // lanes per row in the epilogue
+  constexpr int kRows = 4;     // rows a thread takes at once (a slab holds whole rounds of them)
+  static_assert(WM * 32 % (256 / LPR * kRows) == 0, "slab rows");
+  const int c = tid % LPR;
 #pragma unroll
   for (int j = 0; j < BM; ++j) {
     uint8_t* x = j & 1 ? x1 : x0;
@@ -313,16 +316,37 @@ __global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void gemm_kernel(GemmAr
             f32x4{acc[i][j][4 * v], acc[i][j][4 * v + 1], acc[i][j][4 * v + 2], acc[i][j][4 * v + 3]};
       }
     stage_barrier();
-    const int c = tid % LPR, n = n0 + 4 * c;
-#pragma unroll 2
-    for (int row = tid / LPR; row < WM * 32; row += 256 / LPR) {
-      const int m = m0 + (row >> 5) * (BM * 32) + 32 * j + (row & 31);
-      const f32x4 v = *(const f32x4*)(x + row * (TN * 4) + ((c ^ (row & 15)) << 4));
-      if (m < a.M && n < a.N) {
-        if constexpr (OP == kPartial)
-          *(f32x4*)(part + ((int64_t)blockIdx.y * a.M + m) * ld_part + n) = v;
-        else
-          epilogue4<OP, ELT>(a, m, n, v);
+    // row r of the slab is row (r / 32) * 32 BM + 32 j + r % 32 of the tile
+    auto tile_row = [&](int row) { return (row >> 5) * (BM * 32) + 32 * j + (row & 31); };
+    auto value = [&](int row) { return *(const f32x4*)(x + row * (TN * 4) + ((c ^ (row & 15)) << 4)); };
+    if constexpr (OP == kPartial) {
+      const TileRows<4> out(part + (int64_t)blockIdx.y * a.M * ld_part, ld_part, m0, n0, min(TM, a.M - m0),
+                            min((int64_t)TN, ld_part - n0));
+      if (n0 + 4 * c < ld_part)
+#pragma unroll 4
+        for (int row = tid / LPR; row < WM * 32; row += 256 / LPR)
+          buffer_store4<4>(out.r, tile_row(row) * out.ld + 16 * c, value(row));
+    } else if (a.vec && (a.N - n0 >= TN || a.N % 4 == 0)) {  // whole fours
+      const int width = min(TN, a.N - n0);
+      if (4 * c < width) {
+        const TileEpilogue<OP, ELT, kRows> e(a, m0, n0, min(TM, a.M - m0), width, 4 * c);
+#pragma unroll 1
+        for (int row = tid / LPR; row < WM * 32; row += 256 / LPR * kRows) {
+          int at[kRows];
+          f32x4 v[kRows];
+#pragma unroll
+          for (int u = 0; u < kRows; ++u) {
+            at[u] = tile_row(row + u * (256 / LPR));
+            v[u] = value(row + u * (256 / LPR));
+          }
+          e.run(at, v);
+        }
+      }
+    } else {
+#pragma unroll 1
+      for (int row = tid / LPR; row < WM * 32; row += 256 / LPR) {
+        const int m = m0 + tile_row(row), n = n0 + 4 * c;
+        if (m < a.M && n < a.N) epilogue4<OP, ELT>(a, m, n, value(row));
       }
     }
   }
