@@ -5,20 +5,20 @@
 // outputs; the blocks' rows run along n and their columns along m, so a lane
 // holds four neighbouring n of one m.  bf16 products are
 // v_mfma_f32_32x32x16_bf16, float32 ones v_mfma_f32_32x32x2f32.  Operands come
-// to LDS by direct loads (16 bytes per lane) in stages of 128 bytes of k (64
-// bf16, 32 float32), in the order they have in memory:
-//   k contiguous: [row][128 bytes], 16-byte chunks XORed by row / 2 % 8; a fragment
+// to LDS by direct loads (16 bytes per lane) in stages of 64 bytes of k (32
+// bf16, 16 float32: two K steps), in the order they have in memory:
+//   k contiguous: [row][64 bytes], 16-byte chunks XORed by row / 4 % 4; a fragment
 //     is one 16-byte read per lane: 8 bf16, or 4 float32 that serve four MFMA
 //     (slot j of half-wave h is k = 4h + j for both operands);
 //   k strided: [k][row], read across with the transposing LDS read (bf16) or
 //     by 4-byte reads of 32 neighbouring rows (float32); chunks XORed by k so
 //     that the k rows of one read lie in different banks.
-// Two stage buffers.  A stage's four K steps are read during the two steps
-// before it and its own first; its buffer is then empty and takes the loads of
-// the stage after next, which have five of eight K steps to arrive (the wait
-// counts: those issued last may still be under way).  Reading each step two
-// steps ahead left them four at most, and the matrix cores half idle at 1000
-// TFLOP/s.
+// A ring of kBuffers stage buffers.  Fragments are read one K step ahead; the
+// one barrier of a stage sits between its two steps, where the stage is in
+// registers: its buffer then takes the loads of the stage kBuffers further on,
+// half of them in each of the next two steps.  A load so has four to six K
+// steps to arrive, and the loads come evenly (the wait counts them, those of
+// two stages may be under way).
 //
 // Rows past M or N and k past K read as zero, so no product meets what lies
 // behind a row.
@@ -27,6 +27,8 @@
 // rows, so that the epilogue is one short loop over whole rows: its loads and
 // stores of Z, R and the outputs are contiguous per wave.
 #include <algorithm>
+#include <type_traits>
+#include <utility>
 
 #include "api_common.h"
 #include "device_common.h"
@@ -39,6 +41,7 @@ using namespace dev;
 
 namespace {
 
+constexpr int kBuffers = 4;  // stage buffers (and stages unrolled)
 constexpr int kPartial = 3;  // epilogue of a split product: float32 partial tile
 
 typedef short i16x4 __attribute__((ext_vector_type(4)));
@@ -49,64 +52,100 @@ __device__ inline void wait_all() {  // this wave's loads are in LDS, its LDS re
 __device__ inline void plain_barrier() { asm volatile("s_barrier" ::: "memory"); }
 __device__ inline void stage_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
+// Fragment halves that an LDS read written out below puts in place behind the
+// compiler's back: only touched after landed() has waited for them.
+struct Raw {
+  i16x4 lo, hi;
+};
 // Transposing LDS read: lane 4r + c of every 16 addresses four bf16 of k row r,
-// lane j receives the four k of column j.
-__device__ inline i16x4 read_across(const uint8_t* p) {
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)p);
+// lane j receives the four k of column j.  Written out because the compiler,
+// which cannot tell what bytes the builtin reads, waits for every direct load
+// in flight (vmcnt 0) before it: 654 TFLOP/s where this reaches 1300.
+template <int OFF>
+__device__ inline i16x4 read_across(uint32_t lds) {
+  i16x4 v;
+  asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(v) : "v"(lds), "i"(OFF));
+  return v;
+}
+// All LDS reads of this wave are done; the fragments may be used.
+__device__ inline void landed(Raw (&f)[4]) {
+  asm volatile("s_waitcnt lgkmcnt(0)"
+               : "+v"(f[0].lo), "+v"(f[0].hi), "+v"(f[1].lo), "+v"(f[1].hi), "+v"(f[2].lo), "+v"(f[2].hi),
+                 "+v"(f[3].lo), "+v"(f[3].hi));
+}
+__device__ inline void landed(Raw (&f)[2]) {
+  asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(f[0].lo), "+v"(f[0].hi), "+v"(f[1].lo), "+v"(f[1].hi));
+}
+__device__ inline void landed(Raw (&f)[1]) {
+  asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(f[0].lo), "+v"(f[0].hi));
+}
+template <int N>
+__device__ inline void landed(i32x4 (&)[N]) {}  // the compiler waits by itself
+__device__ inline i32x4 operand(i32x4 f) { return f; }
+__device__ inline i32x4 operand(const Raw& f) {
+  const i32x2 x = __builtin_bit_cast(i32x2, f.lo), y = __builtin_bit_cast(i32x2, f.hi);
+  return i32x4{x.x, x.y, y.x, y.y};
+}
+
+// The main loop's pieces keep accumulators and fragments in registers only if
+// every one of them is inlined, whatever its size.
+#define DATTRI_INLINE __attribute__((always_inline))
+
+// f(0), ..., f(N - 1) with constants for arguments
+template <class F, int... I>
+__device__ DATTRI_INLINE inline void unrolled(F& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ DATTRI_INLINE inline void unrolled(F f) {
+  unrolled(f, std::make_integer_sequence<int, N>{});
 }
 
 // One operand's share of a tile: R rows (of the operand's own index) of which
 // `rows` exist, k contiguous (KC) or strided.
 template <int ELT, bool KC, int R>
 struct Side {
-  static constexpr int EPL = 16 / ELT, BK = 128 / ELT;  // elements per chunk, k per stage
-  static constexpr int kBytes = R * 128;                // of a stage
-  static constexpr int kLoads = R / 32;                 // direct loads per wave and stage
-  static constexpr int CH = R * ELT / 16;               // chunks per k row (strided)
-  static constexpr int kReads = KC ? 1 : ELT == 2 ? 2 : 4;  // LDS reads per fragment
+  static constexpr int EPL = 16 / ELT, BK = 64 / ELT;    // elements per chunk, k per stage
+  static constexpr int kBytes = R * 64;                  // of a stage
+  static constexpr int kPieces = kBytes / 1024;          // direct loads of 1 KiB
+  static constexpr int kLoads = kPieces > 4 ? kPieces / 4 : 1;  // per wave; two pieces: each loaded by two waves
+  static constexpr int CH = R * ELT / 16;                // chunks per k row (strided)
 
-  // A direct load moves 1 KiB, 64 chunks: kRows rows of a stage buffer (of the
-  // operand or of k).  Its rows lie kRows * j further than load 0's; the swizzle
-  // has two variants over j.
-  static constexpr int kRows = KC ? 8 : 64 / CH;
-  static constexpr int kShift = KC || ELT == 2 ? 0 : R == 256 ? 2 : 1;  // variant (j >> kShift) & 1
+  // A direct load moves 64 chunks: kRows rows of a stage buffer (of the operand
+  // or of k).  The chunks of row r are XORed by swz(r), which has two variants
+  // over the loads where a load is two k rows.
+  static constexpr int kRows = KC ? 16 : 64 / CH;
 
   const uint8_t* base;  // the tile's first row (KC) or column (strided) at k = 0
   uint32_t ld;          // bytes
   int rows, K;
-  uint32_t off[2];  // this lane's chunk of a load of each variant, from the load's first row
-  int kc[2];        // KC: its k within the stage
+  uint32_t off[2];  // this lane's chunk of an even and an odd load, from the load's first row
+  int kc;           // KC: its k within the stage
 
-  __device__ static int swz(int k) { return ELT == 2 ? 2 * (k & 3) + 8 * (k & 1) : 8 * ((k >> 2) & 1); }
+  __device__ static int swz(int r) {
+    return KC ? (r >> 2) & 3 : (ELT == 2 ? 2 * (r & 3) + 8 * (r & 1) : 8 * ((r >> 2) & 1)) & (CH - 1);
+  }
 
   __device__ void init(const void* p, int64_t ld_elts, int row0, int n_rows, int K_, int wave, int lane) {
     ld = (uint32_t)(ld_elts * ELT);
     rows = min(R, n_rows - row0);
     K = K_;
     base = (const uint8_t*)p + (KC ? (int64_t)row0 * ld : (int64_t)row0 * ELT);
+    constexpr int kPer = KC ? 4 : CH;  // chunks per row
+    const int r = lane / kPer, c = lane % kPer;
 #pragma unroll
-    for (int v = 0; v < 2; ++v) {
-      const int j = wave * kLoads + (v << kShift);
-      if constexpr (KC) {
-        const int r = lane >> 3;
-        kc[v] = ((lane & 7) ^ (((j * 8 + r) >> 1) & 7)) * EPL;
-        off[v] = r * ld + kc[v] * ELT;
-      } else {
-        const int r = lane / CH, c = lane % CH;
-        off[v] = r * ld + ((c ^ (swz(j * kRows + r) & (CH - 1))) << 4);
-        kc[v] = 0;
-      }
-    }
+    for (int v = 0; v < 2; ++v) off[v] = r * ld + ((c ^ swz((wave * kLoads + v) * kRows + r)) << 4);
+    kc = (c ^ swz(r)) * EPL;
   }
 
   // What stage st may read: from its first k to the last row's end (rows are
   // whole 16-byte chunks, repacked ones end in zeros); past the last k nothing.
-  // Fits 32 bits: 256 rows stay below 4 GiB, st * BK is past K by three stages at most.
+  // Fits 32 bits: 256 rows stay below 4 GiB, st * BK is past K by a few stages at most.
   __device__ rsrc_t range(int st) const {
     const int left = (int)((uint32_t)K - (uint32_t)st * BK);
     if constexpr (KC) {
       const uint32_t bytes = (uint32_t)(rows - 1) * ld + ((uint32_t)left * ELT + 15) / 16 * 16;
-      return make_rsrc(base + (int64_t)st * 128, left > 0 ? bytes : 0);
+      return make_rsrc(base + (int64_t)st * 64, left > 0 ? bytes : 0);
     } else {
       const uint32_t bytes = (uint32_t)(min(left, BK) - 1) * ld + ((uint32_t)rows * ELT + 15) / 16 * 16;
       return make_rsrc(base + (int64_t)st * BK * ld, left > 0 ? bytes : 0);
@@ -116,84 +155,53 @@ struct Side {
   // stage buffer.  Rows past the last (KC) and k past K read as zero; KC, where
   // the next row lies behind K: by an offset out of range.
   __device__ void load(rsrc_t r, int st, uint8_t* buf, int wave, int j) const {
-    const int v = (j >> kShift) & 1, at = wave * kLoads + j;
-    uint32_t o = off[v] + (uint32_t)(at * kRows) * ld;
-    if (KC && kc[v] >= (int)((uint32_t)K - (uint32_t)st * BK)) o = kOOB;
+    const int at = (wave * kLoads + j) % kPieces;
+    uint32_t o = off[j & 1] + (uint32_t)(at * kRows) * ld;
+    if (KC && kc >= (int)((uint32_t)K - (uint32_t)st * BK)) o = kOOB;
     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, DATTRI_LDS_PTR(buf + at * 1024), 16, o, 0, 0, 0);
   }
 
+  typedef std::conditional_t<!KC && ELT == 2, Raw, i32x4> Frag;
+
   // Fragment of K step s of the 32-row block at row w0 + 32 i: lane l holds row
   // l % 32 and the step's k of half-wave l / 32.
-  template <int NB>
-  __device__ static void read(const uint8_t* buf, int s, int w0, int lane, i32x4 (&f)[NB]) {
+  template <int S>
+  __device__ static Frag read(const uint8_t* buf, int w0, int lane, int i) {
     const int l32 = lane & 31, h = lane >> 5;
     if constexpr (KC) {
-      uint32_t o = ((w0 + l32) * 128 + ((h ^ ((l32 >> 1) & 7)) << 4)) ^ (s << 5);
-      asm volatile("" : "+v"(o));  // formed where it is used: kept for every step and buffer they would not fit
-      const uint8_t* p = buf + o;
-#pragma unroll
-      for (int i = 0; i < NB; ++i) f[i] = *(const i32x4*)(p + i * 4096);
+      return *(const i32x4*)(buf + (w0 + l32) * 64 + (((2 * S + h) ^ swz(l32)) << 4) + i * 2048);
     } else if constexpr (ELT == 2) {
       const int q = lane >> 4, rr = (lane >> 2) & 3, aa = lane & 3;
-      const uint8_t* p = buf + (16 * s + 8 * (q >> 1) + rr) * (CH * 16) + (aa & 1) * 8;
-#pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        const int c = (w0 >> 3) + 4 * i + 2 * (q & 1) + (aa >> 1);
-        const uint8_t* a = p + ((c ^ (swz(rr) & (CH - 1))) << 4);
-        const i16x4 lo = read_across(a), hi = read_across(a + 4 * CH * 16);
-        const i32x2 x = __builtin_bit_cast(i32x2, lo), y = __builtin_bit_cast(i32x2, hi);
-        f[i] = i32x4{x.x, x.y, y.x, y.y};
-      }
+      const int c = (w0 >> 3) + 4 * i + 2 * (q & 1) + (aa >> 1);
+      const uint32_t at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)buf +
+                          (8 * (q >> 1) + rr) * (CH * 16) + (aa & 1) * 8 + ((c ^ swz(rr)) << 4);
+      return Raw{read_across<16 * S * CH * 16>(at), read_across<(16 * S + 4) * CH * 16>(at)};
     } else {
-      const uint8_t* p = buf + (8 * s + 4 * h) * (CH * 16) + (l32 & 3) * 4;
-#pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        const int c = (w0 >> 2) + 8 * i + (l32 >> 2);
-        const uint8_t* a = p + ((c ^ ((8 * h) & (CH - 1))) << 4);
-        f[i] = i32x4{*(const int*)a, *(const int*)(a + CH * 16), *(const int*)(a + 2 * CH * 16),
-                     *(const int*)(a + 3 * CH * 16)};
-      }
+      const int c = (w0 >> 2) + 8 * i + (l32 >> 2);
+      const uint8_t* a = buf + (8 * S + 4 * h) * (CH * 16) + (l32 & 3) * 4 + ((c ^ swz(4 * h)) << 4);
+      return i32x4{*(const int*)a, *(const int*)(a + CH * 16), *(const int*)(a + 2 * CH * 16),
+                   *(const int*)(a + 3 * CH * 16)};
     }
   }
 };
 
-template <int ELT, int BN, int BM>
-__device__ inline void step_mma(const i32x4 (&b)[BN], const i32x4 (&a)[BM], f32x16 (&acc)[BN][BM]) {
+// acc[j] += block row b times the blocks a[j]
+template <int ELT, int BM>
+__device__ inline void row_mma(i32x4 b, const i32x4 (&a)[BM], f32x16 (&acc)[BM]) {
   if constexpr (ELT == 2) {
 #pragma unroll
-    for (int i = 0; i < BN; ++i)
-#pragma unroll
-      for (int j = 0; j < BM; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b[i]),
-                                                           __builtin_bit_cast(bf16x8, a[j]), acc[i][j], 0, 0, 0);
+    for (int j = 0; j < BM; ++j)
+      acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a[j]),
+                                                       acc[j], 0, 0, 0);
   } else {
-    f32x4 fb[BN], fa[BM];
-#pragma unroll
-    for (int i = 0; i < BN; ++i) fb[i] = __builtin_bit_cast(f32x4, b[i]);
+    const f32x4 fb = __builtin_bit_cast(f32x4, b);
+    f32x4 fa[BM];
 #pragma unroll
     for (int j = 0; j < BM; ++j) fa[j] = __builtin_bit_cast(f32x4, a[j]);
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
-      for (int i = 0; i < BN; ++i)
-#pragma unroll
-        for (int j = 0; j < BM; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(fb[i][e], fa[j][e], acc[i][j], 0, 0, 0);
-  }
-}
-
-// Deals a step's LDS reads and direct loads out between the first half of its MFMA.
-template <int BLOCKS, int READS, int LOADS, int I = 0>
-__device__ inline void spread() {
-  constexpr int kFirst = (BLOCKS + 1) / 2;
-  if constexpr (I < BLOCKS) {
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-    if constexpr (I < kFirst) {
-      constexpr int r = READS * (I + 1) / kFirst - READS * I / kFirst, l = LOADS * (I + 1) / kFirst - LOADS * I / kFirst;
-      if constexpr (r > 0) __builtin_amdgcn_sched_group_barrier(0x100, r, 0);
-      if constexpr (l > 0) __builtin_amdgcn_sched_group_barrier(0x020, l, 0);
-    }
-    spread<BLOCKS, READS, LOADS, I + 1>();
+      for (int j = 0; j < BM; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(fb[e], fa[j][e], acc[j], 0, 0, 0);
   }
 }
 
@@ -218,14 +226,14 @@ __device__ inline void tile_of(int b, int nm, int nn, int* mt, int* nt) {
 template <int OP, bool AC, bool BC, int ELT, int WM, int WN, int BM, int BN>
 __global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void gemm_kernel(GemmArgs a, int nm, int nn, int sps,
                                                                           float* __restrict__ part, int64_t ld_part) {
-  static_assert(WM * WN == 4, "four waves");
+  static_assert(WM * WN == 4 && WM <= 2, "four waves");
   constexpr int TM = WM * BM * 32, TN = WN * BN * 32;
   typedef Side<ELT, AC, TM> SA;
   typedef Side<ELT, BC, TN> SB;
   constexpr int kStage = SA::kBytes + SB::kBytes;
-  constexpr int kSlab = WM * 32 * TN * 4;  // epilogue: one block column of every wave
+  constexpr int kSlab = 32 * TN * 4;  // epilogue: one block column of a row of waves
   constexpr int kBuf = kStage > kSlab ? kStage : kSlab;
-  __shared__ __align__(1024) uint8_t x0[kBuf], x1[kBuf];
+  __shared__ __align__(1024) uint8_t x0[kBuf], x1[kBuf], x2[kBuf], x3[kBuf];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WN, wn = wave % WN;
   int mt, nt;
@@ -246,52 +254,83 @@ __global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void gemm_kernel(GemmAr
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
 
-  i32x4 fb[4][BN], fa[4][BM];  // fragments of a stage's K steps
-  auto read = [&](const uint8_t* x, int s) {
-    SA::template read<BM>(x, s, wm * BM * 32, lane, fa[s]);
-    SB::template read<BN>(x + SA::kBytes, s, wn * BN * 32, lane, fb[s]);
+  typename SB::Frag fb[2][BN];  // fragments of a stage's two K steps
+  typename SA::Frag fa[2][BM];
+  // fragment J of K step S, A's first
+  auto read = [&](auto S, auto J, const uint8_t* x) DATTRI_INLINE {
+    constexpr int s = decltype(S)::value, j = decltype(J)::value;
+    if constexpr (j < BM)
+      fa[s][j] = SA::template read<s>(x, wm * BM * 32, lane, j);
+    else
+      fb[s][j - BM] = SB::template read<s>(x + SA::kBytes, wn * BN * 32, lane, j - BM);
   };
-  auto issue = [&](int st, uint8_t* x) {
+  constexpr int kLoads = SA::kLoads + SB::kLoads, kHalf = kLoads / 2;
+  // loads From .. To - 1 of stage st, A's first
+  auto issue = [&](int st, uint8_t* x, auto From, auto To) DATTRI_INLINE {
     const rsrc_t ra = sa.range(s0 + st), rb = sb.range(s0 + st);
-#pragma unroll
-    for (int j = 0; j < SA::kLoads; ++j) sa.load(ra, s0 + st, x, wave, j);
-#pragma unroll
-    for (int j = 0; j < SB::kLoads; ++j) sb.load(rb, s0 + st, x + SA::kBytes, wave, j);
+    unrolled<kLoads>([&](auto J) DATTRI_INLINE {
+      constexpr int j = decltype(J)::value;
+      if constexpr (j >= decltype(From)::value && j < decltype(To)::value) {
+        if constexpr (j < SA::kLoads)
+          sa.load(ra, s0 + st, x, wave, j);
+        else
+          sb.load(rb, s0 + st, x + SA::kBytes, wave, j - SA::kLoads);
+      }
+    });
   };
-  constexpr int kLoads = SA::kLoads + SB::kLoads, kReads = SA::kReads * BM + SB::kReads * BN;
-  constexpr int kMma = BN * BM * (ELT == 2 ? 1 : 4);
+  // K step S: its products, and between them the reads of the step after it
+  // (from rx, in the first half) and loads From .. To - 1 of stage lst.
+  auto step = [&](auto S, const uint8_t* rx, int lst, uint8_t* lx, auto From, auto To) DATTRI_INLINE {
+    constexpr int s = decltype(S)::value, kFirst = (BN + 1) / 2, from = decltype(From)::value,
+                  to = decltype(To)::value;
+    i32x4 oa[BM];
+#pragma unroll
+    for (int j = 0; j < BM; ++j) oa[j] = operand(fa[s][j]);
+    unrolled<BN>([&](auto I) DATTRI_INLINE {
+      constexpr int i = decltype(I)::value;
+      unrolled<BM + BN>([&](auto J) DATTRI_INLINE {
+        constexpr int j = decltype(J)::value;
+        if constexpr (i < kFirst && j >= (BM + BN) * i / kFirst && j < (BM + BN) * (i + 1) / kFirst)
+          read(std::integral_constant<int, 1 - s>{}, J, rx);
+      });
+      issue(lst, lx, std::integral_constant<int, from + (to - from) * i / BN>{},
+            std::integral_constant<int, from + (to - from) * (i + 1) / BN>{});
+      row_mma<ELT, BM>(operand(fb[s][i]), oa, acc[i]);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    landed(fa[1 - s]);
+    landed(fb[1 - s]);
+  };
+  typedef std::integral_constant<int, 0> zero_t;
+  typedef std::integral_constant<int, 1> one_t;
+  typedef std::integral_constant<int, kHalf> half_t;
+  typedef std::integral_constant<int, kLoads> all_t;
   if (ns > 0) {
-    issue(0, x0);
-    issue(1, x1);
-    wait_vmcnt_dma<kLoads>();
+    issue(0, x0, zero_t{}, all_t{});
+    issue(1, x1, zero_t{}, all_t{});
+    issue(2, x2, zero_t{}, all_t{});
+    issue(3, x3, zero_t{}, half_t{});
+    wait_vmcnt_dma<2 * kLoads + kHalf>();  // stage 0 has landed
     plain_barrier();
-    read(x0, 0);
-    read(x0, 1);
-    read(x0, 2);
-    // K steps 0 .. 2 of stage st are in registers or asked for, st + 1 is on its
-    // way to nx.  Loads past the last stage fetch nothing (their k is past the
-    // sides' K) and fill with zeros.
-    auto stage = [&](int st, uint8_t* cx, const uint8_t* nx) {
-      read(cx, 3);
-      step_mma<ELT, BN, BM>(fb[0], fa[0], acc);
-      spread<kMma, kReads, 0>();
-      stage_barrier();  // the stage is in registers, its buffer free
-      issue(st + 2, cx);
-      step_mma<ELT, BN, BM>(fb[1], fa[1], acc);
-      spread<kMma, 0, kLoads>();
-      wait_vmcnt_dma<kLoads>();  // all but the loads just issued: stage st + 1 has landed
-      plain_barrier();
-      read(nx, 0);
-      read(nx, 1);
-      step_mma<ELT, BN, BM>(fb[2], fa[2], acc);
-      spread<kMma, 2 * kReads, 0>();
-      read(nx, 2);
-      step_mma<ELT, BN, BM>(fb[3], fa[3], acc);
-      spread<kMma, kReads, 0>();
+    unrolled<BM + BN>([&](auto J) DATTRI_INLINE { read(zero_t{}, J, x0); });
+    landed(fa[0]);
+    landed(fb[0]);
+    // On entry step 0 of stage st (in cx) is in registers, and stages st + 1 ..
+    // st + kBuffers - 1 are on their way, the last but for its second half.
+    // Loads past the last stage fetch nothing (their k is past the sides' K) and
+    // fill with zeros.
+    auto stage = [&](int st, uint8_t* cx, const uint8_t* nx, uint8_t* px) DATTRI_INLINE {
+      step(zero_t{}, cx, st + kBuffers - 1, px, half_t{}, all_t{});
+      // stage st is in registers, st + 1 has landed: two stages may still be under way
+      wait_vmcnt_dma<(kBuffers - 2) * kLoads>();
+      stage_barrier();
+      step(one_t{}, nx, st + kBuffers, cx, zero_t{}, half_t{});
     };
-    for (int st = 0; st < ns; st += 2) {  // an odd last stage is followed by one of zeros
-      stage(st, x0, x1);
-      stage(st + 1, x1, x0);
+    for (int st = 0; st < ns; st += kBuffers) {  // a last round that is not full ends in stages of zeros
+      stage(st, x0, x1, x3);
+      stage(st + 1, x1, x2, x0);
+      stage(st + 2, x2, x3, x1);
+      stage(st + 3, x3, x0, x2);
     }
     wait_all();
   }
@@ -305,20 +344,24 @@ __global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void gemm_kernel(GemmAr
   const int c = tid % LPR;
 #pragma unroll
   for (int j = 0; j < BM; ++j) {
-    uint8_t* x = j & 1 ? x1 : x0;
-    if (j < 2) stage_barrier();  // the last stage's reads are done (j = 0); later ones are ordered by the barrier below
+    // the rows of waves: in one buffer each
+    uint8_t* const y0 = j & 1 ? x2 : x0;
+    uint8_t* const y1 = j & 1 ? x3 : x1;
+    if (j == 0) stage_barrier();  // the last stage's reads are done; the buffers of j - 2 are by the barrier below
 #pragma unroll
     for (int i = 0; i < BN; ++i)
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
-        const int row = wm * 32 + l32, c = (wn * BN + i) * 8 + 2 * v + h;
-        *(f32x4*)(x + row * (TN * 4) + ((c ^ (row & 15)) << 4)) =
+        const int c = (wn * BN + i) * 8 + 2 * v + h;
+        *(f32x4*)((wm ? y1 : y0) + l32 * (TN * 4) + ((c ^ (l32 & 15)) << 4)) =
             f32x4{acc[i][j][4 * v], acc[i][j][4 * v + 1], acc[i][j][4 * v + 2], acc[i][j][4 * v + 3]};
       }
     stage_barrier();
     // row r of the slab is row (r / 32) * 32 BM + 32 j + r % 32 of the tile
     auto tile_row = [&](int row) { return (row >> 5) * (BM * 32) + 32 * j + (row & 31); };
-    auto value = [&](int row) { return *(const f32x4*)(x + row * (TN * 4) + ((c ^ (row & 15)) << 4)); };
+    auto value = [&](int row) {
+      return *(const f32x4*)((row & 32 ? y1 : y0) + (row & 31) * (TN * 4) + ((c ^ (row & 15)) << 4));
+    };
     if constexpr (OP == kPartial) {
       const TileRows<4> out(part + (int64_t)blockIdx.y * a.M * ld_part, ld_part, m0, n0, min(TM, a.M - m0),
                             min((int64_t)TN, ld_part - n0));
@@ -455,10 +498,11 @@ GemmShape gemm_shape(int64_t M, int64_t N, int64_t K, int elt, bool a_contiguous
   g.tn = g.v == kBig ? 256 : 128;
   g.nm = (M + g.tm - 1) / g.tm;
   g.nn = (N + g.tn - 1) / g.tn;
-  const int64_t stages = std::max<int64_t>(1, (K * elt + 127) / 128), tiles = g.nm * g.nn;
+  const int64_t stages = std::max<int64_t>(1, (K * elt + 63) / 64), tiles = g.nm * g.nn;
   const int64_t target = g.v == kBig ? 256 : g.v == kMid ? 512 : 1024;  // workgroups that fill the chip
-  int64_t splits = std::max<int64_t>(1, std::min<int64_t>({target / std::max<int64_t>(tiles, 1), stages / 4, 64}));
+  int64_t splits = std::max<int64_t>(1, std::min<int64_t>({target / std::max<int64_t>(tiles, 1), stages / 8, 64}));
   g.sps = (int)((stages + splits - 1) / splits);
+  if (splits > 1) g.sps = (g.sps + kBuffers - 1) / kBuffers * kBuffers;  // whole rounds of the buffers
   g.splits = (int)((stages + g.sps - 1) / g.sps);
   return g;
 }
