@@ -5,20 +5,24 @@
 // outputs; the blocks' rows run along n and their columns along m, so a lane
 // holds four neighbouring n of one m.  bf16 products are
 // v_mfma_f32_32x32x16_bf16, float32 ones v_mfma_f32_32x32x2f32.  Operands come
-// to LDS by direct loads (16 bytes per lane) in stages of 64 bytes of k (32
-// bf16, 16 float32: two K steps), in the order they have in memory:
-//   k contiguous: [row][64 bytes], 16-byte chunks XORed by row / 4 % 4; a fragment
-//     is one 16-byte read per lane: 8 bf16, or 4 float32 that serve four MFMA
+// to LDS by direct loads (16 bytes per lane) in stages of KW bytes of k, in the
+// order they have in memory:
+//   k contiguous: [row][KW bytes], 16-byte chunks XORed by row; a fragment is
+//     one 16-byte read per lane: 8 bf16, or 4 float32 that serve four MFMA
 //     (slot j of half-wave h is k = 4h + j for both operands);
 //   k strided: [k][row], read across with the transposing LDS read (bf16) or
-//     by 4-byte reads of 32 neighbouring rows (float32); chunks XORed by k so
-//     that the k rows of one read lie in different banks.
-// A ring of kBuffers stage buffers.  Fragments are read one K step ahead; the
-// one barrier of a stage sits between its two steps, where the stage is in
-// registers: its buffer then takes the loads of the stage kBuffers further on,
-// half of them in each of the next two steps.  A load so has four to six K
-// steps to arrive, and the loads come evenly (the wait counts them, those of
-// two stages may be under way).
+//     by 4-byte reads of 32 neighbouring rows (float32); chunks XORed by k.
+// Every read then meets each bank once.
+//
+// A ring of 256 / KW stage buffers, 32 bytes of k per K step.  Fragments are
+// read one step ahead; the one barrier of a stage sits before its last step,
+// where the stage is in registers: its buffer then takes the loads of the stage
+// a ring further on, half of them in that step and half in the next, dealt out
+// evenly (the wait counts: with four buffers the loads of two stages may still be
+// under way).  Four buffers of 64 bytes give a load four to six steps to arrive.
+// Where both operands of a 256 x 256 bf16 tile have k contiguous, 64 bytes are
+// half a cache line and double the requests to L2 (8192 x 4096 -> 14336: 827 us);
+// there two buffers of 128 bytes, two to four steps for a load, take 739.
 //
 // Rows past M or N and k past K read as zero, so no product meets what lies
 // behind a row.
@@ -41,7 +45,7 @@ using namespace dev;
 
 namespace {
 
-constexpr int kBuffers = 4;  // stage buffers (and stages unrolled)
+constexpr int buffers_of(int kw) { return 256 / kw; }  // stage buffers (and stages unrolled)
 constexpr int kPartial = 3;  // epilogue of a split product: float32 partial tile
 
 typedef short i16x4 __attribute__((ext_vector_type(4)));
@@ -102,28 +106,29 @@ __device__ DATTRI_INLINE inline void unrolled(F f) {
 }
 
 // One operand's share of a tile: R rows (of the operand's own index) of which
-// `rows` exist, k contiguous (KC) or strided.
-template <int ELT, bool KC, int R>
+// `rows` exist, k contiguous (KC) or strided; KW bytes of k per stage.
+template <int ELT, bool KC, int R, int KW>
 struct Side {
-  static constexpr int EPL = 16 / ELT, BK = 64 / ELT;    // elements per chunk, k per stage
-  static constexpr int kBytes = R * 64;                  // of a stage
+  static constexpr int EPL = 16 / ELT, BK = KW / ELT;    // elements per chunk, k per stage
+  static constexpr int kBytes = R * KW;                  // of a stage
   static constexpr int kPieces = kBytes / 1024;          // direct loads of 1 KiB
   static constexpr int kLoads = kPieces > 4 ? kPieces / 4 : 1;  // per wave; two pieces: each loaded by two waves
   static constexpr int CH = R * ELT / 16;                // chunks per k row (strided)
 
   // A direct load moves 64 chunks: kRows rows of a stage buffer (of the operand
-  // or of k).  The chunks of row r are XORed by swz(r), which has two variants
-  // over the loads where a load is two k rows.
-  static constexpr int kRows = KC ? 16 : 64 / CH;
+  // or of k).  The chunks of row r are XORed by swz(r), which differs between
+  // even and odd loads at most.
+  static constexpr int kPer = KC ? KW / 16 : CH, kRows = 64 / kPer;  // chunks per row
 
   const uint8_t* base;  // the tile's first row (KC) or column (strided) at k = 0
   uint32_t ld;          // bytes
   int rows, K;
   uint32_t off[2];  // this lane's chunk of an even and an odd load, from the load's first row
-  int kc;           // KC: its k within the stage
+  int kc[2];        // KC: its k within the stage
 
   __device__ static int swz(int r) {
-    return KC ? (r >> 2) & 3 : (ELT == 2 ? 2 * (r & 3) + 8 * (r & 1) : 8 * ((r >> 2) & 1)) & (CH - 1);
+    if constexpr (KC) return KW == 128 ? (r >> 1) & 7 : (r >> 2) & 3;
+    return (ELT == 2 ? 2 * (r & 3) + 8 * (r & 1) : 8 * ((r >> 2) & 1)) & (CH - 1);
   }
 
   __device__ void init(const void* p, int64_t ld_elts, int row0, int n_rows, int K_, int wave, int lane) {
@@ -131,11 +136,13 @@ struct Side {
     rows = min(R, n_rows - row0);
     K = K_;
     base = (const uint8_t*)p + (KC ? (int64_t)row0 * ld : (int64_t)row0 * ELT);
-    constexpr int kPer = KC ? 4 : CH;  // chunks per row
     const int r = lane / kPer, c = lane % kPer;
 #pragma unroll
-    for (int v = 0; v < 2; ++v) off[v] = r * ld + ((c ^ swz((wave * kLoads + v) * kRows + r)) << 4);
-    kc = (c ^ swz(r)) * EPL;
+    for (int v = 0; v < 2; ++v) {
+      const int x = c ^ swz((wave * kLoads + v) * kRows + r);
+      off[v] = r * ld + (x << 4);
+      kc[v] = x * EPL;
+    }
   }
 
   // What stage st may read: from its first k to the last row's end (rows are
@@ -145,7 +152,7 @@ struct Side {
     const int left = (int)((uint32_t)K - (uint32_t)st * BK);
     if constexpr (KC) {
       const uint32_t bytes = (uint32_t)(rows - 1) * ld + ((uint32_t)left * ELT + 15) / 16 * 16;
-      return make_rsrc(base + (int64_t)st * 64, left > 0 ? bytes : 0);
+      return make_rsrc(base + (int64_t)st * KW, left > 0 ? bytes : 0);
     } else {
       const uint32_t bytes = (uint32_t)(min(left, BK) - 1) * ld + ((uint32_t)rows * ELT + 15) / 16 * 16;
       return make_rsrc(base + (int64_t)st * BK * ld, left > 0 ? bytes : 0);
@@ -157,7 +164,7 @@ struct Side {
   __device__ void load(rsrc_t r, int st, uint8_t* buf, int wave, int j) const {
     const int at = (wave * kLoads + j) % kPieces;
     uint32_t o = off[j & 1] + (uint32_t)(at * kRows) * ld;
-    if (KC && kc >= (int)((uint32_t)K - (uint32_t)st * BK)) o = kOOB;
+    if (KC && kc[j & 1] >= (int)((uint32_t)K - (uint32_t)st * BK)) o = kOOB;
     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, DATTRI_LDS_PTR(buf + at * 1024), 16, o, 0, 0, 0);
   }
 
@@ -169,7 +176,7 @@ struct Side {
   __device__ static Frag read(const uint8_t* buf, int w0, int lane, int i) {
     const int l32 = lane & 31, h = lane >> 5;
     if constexpr (KC) {
-      return *(const i32x4*)(buf + (w0 + l32) * 64 + (((2 * S + h) ^ swz(l32)) << 4) + i * 2048);
+      return *(const i32x4*)(buf + (w0 + l32) * KW + (((2 * S + h) ^ swz(l32)) << 4) + i * 32 * KW);
     } else if constexpr (ELT == 2) {
       const int q = lane >> 4, rr = (lane >> 2) & 3, aa = lane & 3;
       const int c = (w0 >> 3) + 4 * i + 2 * (q & 1) + (aa >> 1);
@@ -185,24 +192,15 @@ struct Side {
   }
 };
 
-// acc[j] += block row b times the blocks a[j]
-template <int ELT, int BM>
-__device__ inline void row_mma(i32x4 b, const i32x4 (&a)[BM], f32x16 (&acc)[BM]) {
-  if constexpr (ELT == 2) {
+template <int ELT>
+__device__ inline f32x16 block_mma(i32x4 b, i32x4 a, f32x16 c) {
+  if constexpr (ELT == 2)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a), c, 0, 0,
+                                                   0);
+  const f32x4 fb = __builtin_bit_cast(f32x4, b), fa = __builtin_bit_cast(f32x4, a);
 #pragma unroll
-    for (int j = 0; j < BM; ++j)
-      acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a[j]),
-                                                       acc[j], 0, 0, 0);
-  } else {
-    const f32x4 fb = __builtin_bit_cast(f32x4, b);
-    f32x4 fa[BM];
-#pragma unroll
-    for (int j = 0; j < BM; ++j) fa[j] = __builtin_bit_cast(f32x4, a[j]);
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-#pragma unroll
-      for (int j = 0; j < BM; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(fb[e], fa[j][e], acc[j], 0, 0, 0);
-  }
+  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(fb[e], fa[e], c, 0, 0, 0);
+  return c;
 }
 
 // Tile (mt, nt) of launch index b: every XCD takes a contiguous run of tiles,
@@ -223,17 +221,17 @@ __device__ inline void tile_of(int b, int nm, int nn, int* mt, int* nt) {
 // WM x WN waves; BM x BN blocks of 32 x 32 each.  Grid (tiles, splits of k):
 // split y runs stages [y * sps, min((y + 1) * sps, all)); with several splits
 // (OP kPartial) part holds them as [split][M][ld_part].
-template <int OP, bool AC, bool BC, int ELT, int WM, int WN, int BM, int BN>
+template <int OP, bool AC, bool BC, int ELT, int KW, int WM, int WN, int BM, int BN>
 __global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void gemm_kernel(GemmArgs a, int nm, int nn, int sps,
                                                                           float* __restrict__ part, int64_t ld_part) {
   static_assert(WM * WN == 4 && WM <= 2, "four waves");
   constexpr int TM = WM * BM * 32, TN = WN * BN * 32;
-  typedef Side<ELT, AC, TM> SA;
-  typedef Side<ELT, BC, TN> SB;
-  constexpr int kStage = SA::kBytes + SB::kBytes;
-  constexpr int kSlab = 32 * TN * 4;  // epilogue: one block column of a row of waves
-  constexpr int kBuf = kStage > kSlab ? kStage : kSlab;
-  __shared__ __align__(1024) uint8_t x0[kBuf], x1[kBuf], x2[kBuf], x3[kBuf];
+  typedef Side<ELT, AC, TM, KW> SA;
+  typedef Side<ELT, BC, TN, KW> SB;
+  constexpr int kStage = SA::kBytes + SB::kBytes, kBuffers = buffers_of(KW), kSteps = KW / 32;
+  constexpr int kSlab = 32 * TN * 4;  // epilogue: one block column of a row of waves, four of them
+  constexpr int kBuf = std::max(kStage, kSlab * 4 / kBuffers);
+  __shared__ __align__(1024) uint8_t x0[kBuf], x1[kBuf], x2[kBuffers == 4 ? kBuf : 16], x3[kBuffers == 4 ? kBuf : 16];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WN, wn = wave % WN;
   int mt, nt;
@@ -254,17 +252,18 @@ __global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void gemm_kernel(GemmAr
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
 
-  typename SB::Frag fb[2][BN];  // fragments of a stage's two K steps
+  typename SB::Frag fb[2][BN];  // fragments of even and odd K steps
   typename SA::Frag fa[2][BM];
   // fragment J of K step S, A's first
   auto read = [&](auto S, auto J, const uint8_t* x) DATTRI_INLINE {
     constexpr int s = decltype(S)::value, j = decltype(J)::value;
     if constexpr (j < BM)
-      fa[s][j] = SA::template read<s>(x, wm * BM * 32, lane, j);
+      fa[s & 1][j] = SA::template read<s>(x, wm * BM * 32, lane, j);
     else
-      fb[s][j - BM] = SB::template read<s>(x + SA::kBytes, wn * BN * 32, lane, j - BM);
+      fb[s & 1][j - BM] = SB::template read<s>(x + SA::kBytes, wn * BN * 32, lane, j - BM);
   };
-  constexpr int kLoads = SA::kLoads + SB::kLoads, kHalf = kLoads / 2;
+  constexpr int kLoads = SA::kLoads + SB::kLoads;
+  constexpr int kHalf = kLoads / 2;  // in the step behind the barrier, the others in the next
   // loads From .. To - 1 of stage st, A's first
   auto issue = [&](int st, uint8_t* x, auto From, auto To) DATTRI_INLINE {
     const rsrc_t ra = sa.range(s0 + st), rb = sb.range(s0 + st);
@@ -279,58 +278,69 @@ __global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void gemm_kernel(GemmAr
     });
   };
   // K step S: its products, and between them the reads of the step after it
-  // (from rx, in the first half) and loads From .. To - 1 of stage lst.
+  // (from rx) and loads From .. To - 1 of stage lst.  One wave
+  // has a SIMD to itself, so what stands between two MFMA delays the second once
+  // it takes longer than the first: the order is fixed, a read or two at a time.
   auto step = [&](auto S, const uint8_t* rx, int lst, uint8_t* lx, auto From, auto To) DATTRI_INLINE {
-    constexpr int s = decltype(S)::value, kFirst = (BN + 1) / 2, from = decltype(From)::value,
-                  to = decltype(To)::value;
-    i32x4 oa[BM];
-#pragma unroll
-    for (int j = 0; j < BM; ++j) oa[j] = operand(fa[s][j]);
-    unrolled<BN>([&](auto I) DATTRI_INLINE {
-      constexpr int i = decltype(I)::value;
+    constexpr int s = decltype(S)::value & 1, kBlocks = BN * BM, kFirst = (7 * kBlocks + 7) / 8,
+                  from = decltype(From)::value, to = decltype(To)::value;
+    unrolled<kBlocks>([&](auto M) DATTRI_INLINE {
+      constexpr int m = decltype(M)::value, i = m / BM, j = m % BM;
       unrolled<BM + BN>([&](auto J) DATTRI_INLINE {
-        constexpr int j = decltype(J)::value;
-        if constexpr (i < kFirst && j >= (BM + BN) * i / kFirst && j < (BM + BN) * (i + 1) / kFirst)
-          read(std::integral_constant<int, 1 - s>{}, J, rx);
+        constexpr int q = decltype(J)::value;
+        if constexpr (m < kFirst && q >= (BM + BN) * m / kFirst && q < (BM + BN) * (m + 1) / kFirst)
+          read(std::integral_constant<int, (decltype(S)::value + 1) % kSteps>{}, J, rx);
       });
-      issue(lst, lx, std::integral_constant<int, from + (to - from) * i / BN>{},
-            std::integral_constant<int, from + (to - from) * (i + 1) / BN>{});
-      row_mma<ELT, BM>(operand(fb[s][i]), oa, acc[i]);
+      issue(lst, lx, std::integral_constant<int, from + (to - from) * m / kBlocks>{},
+            std::integral_constant<int, from + (to - from) * (m + 1) / kBlocks>{});
+      acc[i][j] = block_mma<ELT>(operand(fb[s][i]), operand(fa[s][j]), acc[i][j]);
       __builtin_amdgcn_sched_barrier(0);
     });
     landed(fa[1 - s]);
     landed(fb[1 - s]);
   };
   typedef std::integral_constant<int, 0> zero_t;
-  typedef std::integral_constant<int, 1> one_t;
   typedef std::integral_constant<int, kHalf> half_t;
   typedef std::integral_constant<int, kLoads> all_t;
   if (ns > 0) {
     issue(0, x0, zero_t{}, all_t{});
-    issue(1, x1, zero_t{}, all_t{});
-    issue(2, x2, zero_t{}, all_t{});
-    issue(3, x3, zero_t{}, half_t{});
-    wait_vmcnt_dma<2 * kLoads + kHalf>();  // stage 0 has landed
+    if constexpr (kBuffers == 4) {
+      issue(1, x1, zero_t{}, all_t{});
+      issue(2, x2, zero_t{}, all_t{});
+      issue(3, x3, zero_t{}, half_t{});
+    } else {
+      issue(1, x1, zero_t{}, half_t{});
+    }
+    wait_vmcnt_dma<(kBuffers - 2) * kLoads + kHalf>();  // stage 0 has landed
     plain_barrier();
     unrolled<BM + BN>([&](auto J) DATTRI_INLINE { read(zero_t{}, J, x0); });
     landed(fa[0]);
     landed(fb[0]);
     // On entry step 0 of stage st (in cx) is in registers, and stages st + 1 ..
-    // st + kBuffers - 1 are on their way, the last but for its second half.
+    // st + kBuffers - 1 are on their way, the last but for its second part.
     // Loads past the last stage fetch nothing (their k is past the sides' K) and
     // fill with zeros.
     auto stage = [&](int st, uint8_t* cx, const uint8_t* nx, uint8_t* px) DATTRI_INLINE {
       step(zero_t{}, cx, st + kBuffers - 1, px, half_t{}, all_t{});
-      // stage st is in registers, st + 1 has landed: two stages may still be under way
+      if constexpr (kSteps == 4) {
+        step(std::integral_constant<int, 1>{}, cx, 0, cx, zero_t{}, zero_t{});
+        step(std::integral_constant<int, 2>{}, cx, 0, cx, zero_t{}, zero_t{});
+      }
+      // stage st is in registers, st + 1 has landed: the stages after it may still be under way
       wait_vmcnt_dma<(kBuffers - 2) * kLoads>();
       stage_barrier();
-      step(one_t{}, nx, st + kBuffers, cx, zero_t{}, half_t{});
+      step(std::integral_constant<int, kSteps - 1>{}, nx, st + kBuffers, cx, zero_t{}, half_t{});
     };
     for (int st = 0; st < ns; st += kBuffers) {  // a last round that is not full ends in stages of zeros
-      stage(st, x0, x1, x3);
-      stage(st + 1, x1, x2, x0);
-      stage(st + 2, x2, x3, x1);
-      stage(st + 3, x3, x0, x2);
+      if constexpr (kBuffers == 4) {
+        stage(st, x0, x1, x3);
+        stage(st + 1, x1, x2, x0);
+        stage(st + 2, x2, x3, x1);
+        stage(st + 3, x3, x0, x2);
+      } else {
+        stage(st, x0, x1, x1);
+        stage(st + 1, x1, x0, x0);
+      }
     }
     wait_all();
   }
@@ -345,8 +355,8 @@ __global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void gemm_kernel(GemmAr
 #pragma unroll
   for (int j = 0; j < BM; ++j) {
     // the rows of waves: in one buffer each
-    uint8_t* const y0 = j & 1 ? x2 : x0;
-    uint8_t* const y1 = j & 1 ? x3 : x1;
+    uint8_t* const y0 = kBuffers == 4 ? (j & 1 ? x2 : x0) : (j & 1 ? x1 : x0);
+    uint8_t* const y1 = kBuffers == 4 ? (j & 1 ? x3 : x1) : y0 + kSlab;
     if (j == 0) stage_barrier();  // the last stage's reads are done; the buffers of j - 2 are by the barrier below
 #pragma unroll
     for (int i = 0; i < BN; ++i)
@@ -483,12 +493,13 @@ namespace {
 enum Variant { kBig, kMid, kFew };
 struct GemmShape {
   Variant v;
+  int kw;  // bytes of k per stage
   int tm, tn;
   int64_t nm, nn;
   int splits, sps;
 };
 
-GemmShape gemm_shape(int64_t M, int64_t N, int64_t K, int elt, bool a_contiguous) {
+GemmShape gemm_shape(int64_t M, int64_t N, int64_t K, int elt, bool a_contiguous, bool b_contiguous) {
   GemmShape g;
   const int64_t big = ((M + 255) / 256) * ((N + 255) / 256);
   if (a_contiguous && M <= 32) g.v = kFew;
@@ -498,11 +509,12 @@ GemmShape gemm_shape(int64_t M, int64_t N, int64_t K, int elt, bool a_contiguous
   g.tn = g.v == kBig ? 256 : 128;
   g.nm = (M + g.tm - 1) / g.tm;
   g.nn = (N + g.tn - 1) / g.tn;
-  const int64_t stages = std::max<int64_t>(1, (K * elt + 63) / 64), tiles = g.nm * g.nn;
+  g.kw = g.v == kBig && elt == 2 && a_contiguous && b_contiguous ? 128 : 64;
+  const int64_t stages = std::max<int64_t>(1, (K * elt + g.kw - 1) / g.kw), tiles = g.nm * g.nn;
   const int64_t target = g.v == kBig ? 256 : g.v == kMid ? 512 : 1024;  // workgroups that fill the chip
-  int64_t splits = std::max<int64_t>(1, std::min<int64_t>({target / std::max<int64_t>(tiles, 1), stages / 8, 64}));
+  int64_t splits = std::max<int64_t>(1, std::min<int64_t>({target / std::max<int64_t>(tiles, 1), stages * g.kw / 512, 64}));
   g.sps = (int)((stages + splits - 1) / splits);
-  if (splits > 1) g.sps = (g.sps + kBuffers - 1) / kBuffers * kBuffers;  // whole rounds of the buffers
+  if (splits > 1) g.sps = (g.sps + buffers_of(g.kw) - 1) / buffers_of(g.kw) * buffers_of(g.kw);  // whole rounds of the buffers
   g.splits = (int)((stages + g.sps - 1) / g.sps);
   return g;
 }
@@ -545,7 +557,7 @@ LinearLayout linear_layout(dattri_linear_op op, int64_t rows, int64_t d_in, int6
   auto packed = [&](int64_t r, int64_t w) { return (size_t)r * (size_t)((w * elt + 15) / 16 * 16); };
   L.off_a = take(L.pack_a ? packed(L.a_rows, L.a_w) : 0);
   L.off_b = take(L.pack_b ? packed(L.b_rows, L.b_w) : 0);
-  L.g = gemm_shape(std::max<int64_t>(L.M, 1), L.N, L.K, elt, L.ac);
+  L.g = gemm_shape(std::max<int64_t>(L.M, 1), L.N, L.K, elt, L.ac, L.bc);
   L.off_part = take(L.g.splits > 1 ? (size_t)L.g.splits * L.M * ((L.N + 3) / 4 * 4) * 4 : 0);
   L.off_cols = off;
   if (op == DATTRI_LINEAR_WEIGHT_GRAD) {
@@ -568,14 +580,14 @@ hipError_t repack(int elt, const void* src, int64_t ld, int64_t w, int64_t rows,
   return hipGetLastError();
 }
 
-template <int OP, bool AC, bool BC, int ELT, int WM, int WN, int BM, int BN>
+template <int OP, bool AC, bool BC, int ELT, int KW, int WM, int WN, int BM, int BN>
 hipError_t launch_tiles(const GemmArgs& a, const GemmShape& g, float* part, int64_t ldp, hipStream_t s) {
   const dim3 grid((unsigned)(g.nm * g.nn), g.splits);
   if (g.splits > 1)
-    hipLaunchKernelGGL((gemm_kernel<kPartial, AC, BC, ELT, WM, WN, BM, BN>), grid, dim3(256), 0, s, a, (int)g.nm,
+    hipLaunchKernelGGL((gemm_kernel<kPartial, AC, BC, ELT, KW, WM, WN, BM, BN>), grid, dim3(256), 0, s, a, (int)g.nm,
                        (int)g.nn, g.sps, part, ldp);
   else
-    hipLaunchKernelGGL((gemm_kernel<OP, AC, BC, ELT, WM, WN, BM, BN>), grid, dim3(256), 0, s, a, (int)g.nm, (int)g.nn,
+    hipLaunchKernelGGL((gemm_kernel<OP, AC, BC, ELT, KW, WM, WN, BM, BN>), grid, dim3(256), 0, s, a, (int)g.nm, (int)g.nn,
                        g.sps, part, ldp);
   return hipGetLastError();
 }
@@ -587,11 +599,11 @@ hipError_t launch_product(const GemmArgs& a, const GemmShape& g, float* part, hi
   const int64_t ldp = (a.N + 3) / 4 * 4;
   hipError_t e = hipErrorInvalidValue;
   if (g.v == kBig)
-    e = launch_tiles<OP, AC, BC, ELT, 2, 2, 4, 4>(a, g, part, ldp, s);
+    e = launch_tiles<OP, AC, BC, ELT, AC && BC && ELT == 2 ? 128 : 64, 2, 2, 4, 4>(a, g, part, ldp, s);
   else if (g.v == kMid)
-    e = launch_tiles<OP, AC, BC, ELT, 2, 2, 2, 2>(a, g, part, ldp, s);
+    e = launch_tiles<OP, AC, BC, ELT, 64, 2, 2, 2, 2>(a, g, part, ldp, s);
   else if constexpr (AC)
-    e = launch_tiles<OP, AC, BC, ELT, 1, 4, 1, 1>(a, g, part, ldp, s);
+    e = launch_tiles<OP, AC, BC, ELT, 64, 1, 4, 1, 1>(a, g, part, ldp, s);
   if (e != hipSuccess || g.splits == 1) return e;
   hipLaunchKernelGGL((gemm_join_kernel<OP, ELT>), dim3(flat_grid((int64_t)a.M * (ldp / 4))), dim3(256), 0, s, a, part,
                      ldp, g.splits);

@@ -12,10 +12,12 @@ import pytest
 
 from test_host_waitcounts import _asm
 
-# (op, A contiguous, B contiguous, bytes per element, WM, WN, BM, BN): loads per wave and stage
+# (op, A contiguous, B contiguous, bytes per element, bytes of k per stage, WM, WN, BM, BN); loads per wave
+# and 64 bytes of k by the last four
 SHAPES = {(2, 2, 4, 4): 8, (2, 2, 2, 2): 4, (1, 4, 1, 1): 3}
 OPS = {0: (1, 1), 1: (1, 0), 2: (0, 0)}
-KERNELS = [(op, a, b, e) + shape for real, (a, b) in OPS.items() for op in (real, 3) for e in (2, 4)
+KERNELS = [(op, a, b, e, 128 if a and b and e == 2 and shape[2] == 4 else 64) + shape
+           for real, (a, b) in OPS.items() for op in (real, 3) for e in (2, 4)
            for shape in SHAPES if not (real == 2 and shape[0] == 1)]
 
 
@@ -25,8 +27,8 @@ def asm():
 
 
 def _kernel(lines, key):
-    op, a, b, e, *shape = key
-    name = f"_ZN6dattri11gemm_kernelILi{op}ELb{a}ELb{b}ELi{e}E" + "".join(f"Li{v}E" for v in shape)
+    op, a, b, e, kw, *shape = key
+    name = f"_ZN6dattri11gemm_kernelILi{op}ELb{a}ELb{b}ELi{e}ELi{kw}E" + "".join(f"Li{v}E" for v in shape)
     start = next(i for i, l in enumerate(lines) if l.startswith(name) and ":" in l)
     end = next(i for i in range(start, len(lines)) if lines[i].startswith(".Lfunc_end"))
     body = [l.split(";")[0].strip() for l in lines[start:end]]
@@ -56,16 +58,18 @@ def _registers(text):
 def test_ring_waits(asm, key):
     body = _kernel(asm, key)
     assert not any(t.startswith("scratch_") for t in body)
-    loop, loads = _loop(body), SHAPES[key[4:]]
+    buffers = 256 // key[4]
+    loop, loads = _loop(body), SHAPES[key[5:]] * key[4] // 64
     memory = [t for t in loop if t.startswith(("buffer_", "global_", "flat_"))]
-    assert len(memory) == 4 * loads and all(t.startswith("buffer_load_dwordx4") and t.endswith(" lds") for t in memory)
+    assert len(memory) == buffers * loads and all(t.startswith("buffer_load_dwordx4") and t.endswith(" lds") for t in memory)
     waits = [int(m[1]) for t in loop for m in [re.match(r"s_waitcnt vmcnt\((\d+)\)", t)] if m]
-    assert waits and all(w >= 2 * loads for w in waits) and waits.count(2 * loads) == 4, waits
-    # each wait stands where exactly the loads of two stages follow the awaited one's: between waits one stage's loads
-    at = [i for i, t in enumerate(loop) if t == f"s_waitcnt vmcnt({2 * loads})"]
+    left = (buffers - 2) * loads  # that may be under way at a barrier
+    assert waits == [left] * buffers, waits
+    # between two waits one stage's loads, so exactly the awaited stage's are the older ones
+    at = [i for i, t in enumerate(loop) if re.match(r"s_waitcnt vmcnt", t)]
     for i, j in zip(at, at[1:]):
         assert sum(t.endswith(" lds") for t in loop[i:j]) == loads
-    assert loop.count("s_barrier") == 4
+    assert loop.count("s_barrier") == buffers
 
 
 @pytest.mark.parametrize("key", [k for k in KERNELS if k[3] == 2 and not k[2]], ids=lambda k: "".join(map(str, k)))
