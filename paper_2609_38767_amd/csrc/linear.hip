@@ -31,6 +31,7 @@
 // rows, so that the epilogue is one short loop over whole rows: its loads and
 // stores of Z, R and the outputs are contiguous per wave.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 #include <utility>
 
@@ -426,21 +427,30 @@ __global__ __launch_bounds__(256) void gemm_join_kernel(GemmArgs a, const float*
   }
 }
 
-// Rows of `w` elements copied to rows of `ld_out` (a multiple of 16 bytes), zeros behind.
+// Rows of `w` elements copied to rows of `ld_out` (a multiple of 16 bytes),
+// zeros behind; both operands in one launch (rows 0: nothing).
+struct Repack {
+  const uint8_t* src;
+  uint8_t* dst;
+  int64_t ld, rows;
+  int w, ld_out;
+};
 template <int ELT>
-__global__ __launch_bounds__(256) void repack_kernel(const uint8_t* __restrict__ src, int64_t ld, int w, int64_t rows,
-                                                     uint8_t* __restrict__ dst, int ld_out) {
+__global__ __launch_bounds__(256) void repack_kernel(Repack a, Repack b) {
   constexpr int EPL = 16 / ELT;
-  const int chunks = ld_out / EPL;
-  const int64_t total = rows * chunks;
+  const int64_t na = a.rows * (a.ld_out / EPL), total = na + b.rows * (b.ld_out / EPL);
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / chunks;
-    const int c = (int)(i - r * chunks) * EPL;
+    const Repack& p = i < na ? a : b;
+    const int64_t at = i < na ? i : i - na;
+    const int chunks = p.ld_out / EPL;
+    const int64_t r = at / chunks;
+    const int c = (int)(at - r * chunks) * EPL;
     uint32_t v[EPL];
 #pragma unroll
     for (int e = 0; e < EPL; ++e) {
       v[e] = 0;
-      if (c + e < w) v[e] = ELT == 2 ? ((const uint16_t*)src)[r * ld + c + e] : ((const uint32_t*)src)[r * ld + c + e];
+      if (c + e < p.w)
+        v[e] = ELT == 2 ? ((const uint16_t*)p.src)[r * p.ld + c + e] : ((const uint32_t*)p.src)[r * p.ld + c + e];
     }
     i32x4 o;
     if (ELT == 2)
@@ -448,7 +458,7 @@ __global__ __launch_bounds__(256) void repack_kernel(const uint8_t* __restrict__
                 (int)(v[6 % EPL] | v[7 % EPL] << 16)};
     else
       o = i32x4{(int)v[0], (int)v[1], (int)v[2], (int)v[3]};
-    *(i32x4*)(dst + i * 16) = o;
+    *(i32x4*)(p.dst + at * 16) = o;
   }
 }
 
@@ -490,33 +500,65 @@ __global__ __launch_bounds__(256) void column_join_kernel(const float* __restric
 namespace {
 
 // How a product is cut: tile variant, splits of k, stages per split.
-enum Variant { kBig, kMid, kFew };
+enum Variant { kBig, kMid, kSlim, kFew };  // 256 x 256, 128 x 128, 64 x 128, 32 x 128
 struct GemmShape {
   Variant v;
   int kw;  // bytes of k per stage
-  int tm, tn;
   int64_t nm, nn;
   int splits, sps;
 };
 
-GemmShape gemm_shape(int64_t M, int64_t N, int64_t K, int elt, bool a_contiguous, bool b_contiguous) {
-  GemmShape g;
-  const int64_t big = ((M + 255) / 256) * ((N + 255) / 256);
-  if (a_contiguous && M <= 32) g.v = kFew;
-  else if (big >= 192) g.v = kBig;
-  else g.v = kMid;
-  g.tm = g.v == kBig ? 256 : g.v == kMid ? 128 : 32;
-  g.tn = g.v == kBig ? 256 : 128;
-  g.nm = (M + g.tm - 1) / g.tm;
-  g.nn = (N + g.tn - 1) / g.tn;
-  g.kw = g.v == kBig && elt == 2 && a_contiguous && b_contiguous ? 128 : 64;
-  const int64_t stages = std::max<int64_t>(1, (K * elt + g.kw - 1) / g.kw), tiles = g.nm * g.nn;
-  const int64_t target = g.v == kBig ? 256 : g.v == kMid ? 512 : 1024;  // workgroups that fill the chip
-  int64_t splits = std::max<int64_t>(1, std::min<int64_t>({target / std::max<int64_t>(tiles, 1), stages * g.kw / 512, 64}));
-  g.sps = (int)((stages + splits - 1) / splits);
-  if (splits > 1) g.sps = (g.sps + buffers_of(g.kw) - 1) / buffers_of(g.kw) * buffers_of(g.kw);  // whole rounds of the buffers
-  g.splits = (int)((stages + g.sps - 1) / g.sps);
-  return g;
+// Bytes of k per stage: 128 where both operands have k contiguous (whole cache
+// lines) and nothing else hides the loads: bf16, one workgroup per CU.  Else 64,
+// twice the buffers (128 x 128 tiles, 2048^3: 24 us, 27 with 128 bytes).
+constexpr int stage_bytes(bool ac, bool bc, int elt, int tm) { return ac && bc && elt == 2 && tm == 256 ? 128 : 64; }
+
+GemmShape gemm_shape(int64_t M, int64_t N, int64_t K, int elt, bool ac, bool bc) {
+  auto cut = [&](Variant v, int64_t splits) {
+    GemmShape g;
+    const int tm = v == kBig ? 256 : v == kMid ? 128 : v == kSlim ? 64 : 32, tn = v == kBig ? 256 : 128;
+    g.v = v;
+    g.kw = stage_bytes(ac, bc, elt, tm);
+    g.nm = (M + tm - 1) / tm;
+    g.nn = (N + tn - 1) / tn;
+    const int64_t stages = std::max<int64_t>(1, (K * elt + g.kw - 1) / g.kw), round = buffers_of(g.kw);
+    splits = std::max<int64_t>(1, std::min(splits, stages * g.kw / 512));
+    g.sps = (int)((stages + splits - 1) / splits);
+    if (splits > 1) g.sps = (int)((g.sps + round - 1) / round * round);  // whole rounds of the buffers
+    g.splits = (int)((stages + g.sps - 1) / g.sps);
+    return g;
+  };
+  // Few rows: the other operand is what there is to read, by as many workgroups
+  // as keep its loads in flight.
+  if (ac && M <= 64) {
+    const Variant v = M <= 32 ? kFew : kSlim;
+    const int64_t tiles = (N + 127) / 128;
+    return cut(v, std::min<int64_t>(64, (v == kFew ? 1024 : 768) / std::max<int64_t>(tiles, 1)));
+  }
+  // Else the cut with the least time as modelled, in us: the CU with most tiles
+  // (FLOP at the rate one CU reaches on a large product, plus what a tile costs
+  // besides), and the partial tiles of a split written, read and joined.  1531 x 1024 -> 4096 float32: 128 x
+  // 128 whole 123 us, in two splits 110, 256 x 256 244.
+  const double rate[2] = {elt == 2 ? 5.2e6 : 0.58e6, elt == 2 ? 4.0e6 : 0.565e6}, fixed[2] = {12., 3.};
+  const int64_t all = (K * elt + 63) / 64 * 64;
+  GemmShape best = {};
+  double best_us = 0.;
+  for (int v = kBig; v <= kMid; ++v)
+    for (int64_t splits = 1; splits <= 32; ++splits) {
+      const GemmShape g = cut((Variant)v, splits);
+      if (g.splits != splits) continue;
+      // in tiles of sps stages: the last split may be short
+      const double tiles = (double)g.nm * g.nn * (splits > 1 ? (double)all / ((int64_t)g.sps * g.kw) : 1.);
+      const int64_t side = v == kBig ? 256 : 128;
+      const double flop = 2. * side * side * g.sps * (g.kw / elt);
+      double us = std::ceil(tiles / 256.) * (flop / rate[v] + fixed[v]);
+      if (g.splits > 1) us += 3. + 8. * g.splits * M * N / 6.0e6;
+      if (best_us == 0. || us < best_us) {
+        best = g;
+        best_us = us;
+      }
+    }
+  return best;
 }
 
 // Column sums: rows per part, parts.
@@ -571,13 +613,13 @@ LinearLayout linear_layout(dattri_linear_op op, int64_t rows, int64_t d_in, int6
 
 unsigned flat_grid(int64_t n) { return (unsigned)std::min<int64_t>((n + 255) / 256, 16384); }
 
-hipError_t repack(int elt, const void* src, int64_t ld, int64_t w, int64_t rows, uint8_t* dst, hipStream_t s) {
+// An operand and where its repacked rows go; updates pointer and stride.
+Repack repack_of(const void** src, int64_t* ld, int64_t w, int64_t rows, int elt, uint8_t* dst) {
   const int ld_out = (int)((w * elt + 15) / 16 * 16 / elt);
-  const int64_t n = rows * (ld_out * elt / 16);
-  if (n == 0) return hipSuccess;
-  hipLaunchKernelGGL(elt == 2 ? repack_kernel<2> : repack_kernel<4>, dim3(flat_grid(n)), dim3(256), 0, s,
-                     (const uint8_t*)src, ld, (int)w, rows, dst, ld_out);
-  return hipGetLastError();
+  const Repack r = {(const uint8_t*)*src, dst, *ld, rows, (int)w, ld_out};
+  *src = dst;
+  *ld = ld_out;
+  return r;
 }
 
 template <int OP, bool AC, bool BC, int ELT, int KW, int WM, int WN, int BM, int BN>
@@ -599,11 +641,15 @@ hipError_t launch_product(const GemmArgs& a, const GemmShape& g, float* part, hi
   const int64_t ldp = (a.N + 3) / 4 * 4;
   hipError_t e = hipErrorInvalidValue;
   if (g.v == kBig)
-    e = launch_tiles<OP, AC, BC, ELT, AC && BC && ELT == 2 ? 128 : 64, 2, 2, 4, 4>(a, g, part, ldp, s);
+    e = launch_tiles<OP, AC, BC, ELT, stage_bytes(AC, BC, ELT, 256), 2, 2, 4, 4>(a, g, part, ldp, s);
   else if (g.v == kMid)
-    e = launch_tiles<OP, AC, BC, ELT, 64, 2, 2, 2, 2>(a, g, part, ldp, s);
-  else if constexpr (AC)
-    e = launch_tiles<OP, AC, BC, ELT, 64, 1, 4, 1, 1>(a, g, part, ldp, s);
+    e = launch_tiles<OP, AC, BC, ELT, stage_bytes(AC, BC, ELT, 128), 2, 2, 2, 2>(a, g, part, ldp, s);
+  else if constexpr (AC) {
+    if (g.v == kSlim)
+      e = launch_tiles<OP, AC, BC, ELT, 64, 2, 2, 1, 2>(a, g, part, ldp, s);
+    else
+      e = launch_tiles<OP, AC, BC, ELT, 64, 1, 4, 1, 1>(a, g, part, ldp, s);
+  }
   if (e != hipSuccess || g.splits == 1) return e;
   hipLaunchKernelGGL((gemm_join_kernel<OP, ELT>), dim3(flat_grid((int64_t)a.M * (ldp / 4))), dim3(256), 0, s, a, part,
                      ldp, g.splits);
@@ -641,17 +687,16 @@ hipError_t launch_linear(dattri_linear_op op, int elt, bool aligned, GemmArgs a,
     e = launch_column_sums(elt, a.A, a.lda, rows, d_out, dbias, a.accumulate, (float*)(ws + L.off_cols), s);
     if (e != hipSuccess || !a.out) return e;
   }
-  if (L.pack_a) {
-    e = repack(elt, a.A, a.lda, L.a_w, L.a_rows, ws + L.off_a, s);
-    if (e != hipSuccess) return e;
-    a.A = ws + L.off_a;
-    a.lda = (L.a_w * elt + 15) / 16 * 16 / elt;
-  }
-  if (L.pack_b) {
-    e = repack(elt, a.B, a.ldb, L.b_w, L.b_rows, ws + L.off_b, s);
-    if (e != hipSuccess) return e;
-    a.B = ws + L.off_b;
-    a.ldb = (L.b_w * elt + 15) / 16 * 16 / elt;
+  if (L.pack_a || L.pack_b) {
+    Repack ra = {}, rb = {};
+    if (L.pack_a) ra = repack_of(&a.A, &a.lda, L.a_w, L.a_rows, elt, ws + L.off_a);
+    if (L.pack_b) rb = repack_of(&a.B, &a.ldb, L.b_w, L.b_rows, elt, ws + L.off_b);
+    const int64_t n = (ra.rows * ra.ld_out + rb.rows * rb.ld_out) * elt / 16;
+    if (n > 0) {
+      hipLaunchKernelGGL(elt == 2 ? repack_kernel<2> : repack_kernel<4>, dim3(flat_grid(n)), dim3(256), 0, s, ra, rb);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
   }
   const int oelt = wgrad ? 4 : elt;
   auto on4 = [](const void* p, int64_t ld, int e) { return !p || ((uintptr_t)p % (4 * e) == 0 && ld % 4 == 0); };
