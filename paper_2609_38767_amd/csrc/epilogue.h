@@ -105,10 +105,19 @@ __device__ inline void epilogue4(const GemmArgs& a, int m, int n, f32x4 v) {
   }
 }
 
-// Four elements of a buffer at byte offset `off` (range checked).
-template <int ELT>
-__device__ inline f32x4 buffer_load4(rsrc_t r, uint32_t off) {
-  if constexpr (ELT == 2) {
+// Four elements of a buffer from byte offset `off` (range checked): neighbours
+// (APART 1), or APART elements from each other, of which the first `cnt` exist.
+template <int ELT, int APART>
+__device__ inline f32x4 buffer_load4(rsrc_t r, uint32_t off, int cnt) {
+  if constexpr (APART > 1) {
+    f32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t o = e < cnt ? off + e * APART * ELT : kOOB;
+      v[e] = ELT == 2 ? bf16_bits_to_f32(load2(r, o)) : __builtin_bit_cast(float, load4(r, o));
+    }
+    return v;
+  } else if constexpr (ELT == 2) {
     const i32x2 w = load8(r, off);
     const uint32_t a = (uint32_t)w.x, b = (uint32_t)w.y;
     return f32x4{__builtin_bit_cast(float, a << 16), __builtin_bit_cast(float, a & 0xFFFF0000u),
@@ -117,12 +126,22 @@ __device__ inline f32x4 buffer_load4(rsrc_t r, uint32_t off) {
     return __builtin_bit_cast(f32x4, load16(r, off));
   }
 }
-template <int ELT>
-__device__ inline void buffer_store4(rsrc_t r, uint32_t off, f32x4 v) {
-  if constexpr (ELT == 2)
+template <int ELT, int APART>
+__device__ inline void buffer_store4(rsrc_t r, uint32_t off, f32x4 v, int cnt) {
+  if constexpr (APART > 1) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t o = e < cnt ? off + e * APART * ELT : kOOB;
+      if constexpr (ELT == 2)
+        __builtin_amdgcn_raw_buffer_store_b16((short)pack_bf16(v[e], 0.f), r, o, 0, 0);
+      else
+        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(int, (float)v[e]), r, o, 0, 0);
+    }
+  } else if constexpr (ELT == 2) {
     __builtin_amdgcn_raw_buffer_store_b64(i32x2{(int)pack_bf16(v.x, v.y), (int)pack_bf16(v.z, v.w)}, r, off, 0, 0);
-  else
+  } else {
     __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(i32x4, v), r, off, 0, 0);
+  }
 }
 
 // A buffer of the epilogue seen from a tile: rows m0 .. (rows of them exist),
@@ -138,10 +157,11 @@ struct TileRows {
   }
 };
 
-// epilogue4 for U rows at once: v[u] are elements (rows at[u], columns n .. n + 3)
-// of the tile at (m0, n0), all buffers on four elements.  Rows past the
-// tile's may be passed: what they store is dropped by the range checks.
-template <int OP, int ELT, int U>
+// epilogue4 for U rows at once: v[u] are the elements of rows at[u] and columns
+// col, col + APART, ... of the tile at (m0, n0); APART 1: all buffers' rows on
+// four elements and four columns left.  Rows past the tile's may be passed: what
+// they store is dropped by the range checks.
+template <int OP, int ELT, int U, int APART>
 struct TileEpilogue {
   static constexpr int OELT = OP == DATTRI_LINEAR_WEIGHT_GRAD ? 4 : ELT;
   const GemmArgs& a;
@@ -149,24 +169,33 @@ struct TileEpilogue {
   TileRows<ELT> out2, z, r;
   f32x4 bias;
   uint32_t n;
+  int cnt;  // columns that exist
   __device__ TileEpilogue(const GemmArgs& a_, int m0, int n0, int rows, int width, int col)
       : a(a_), out(a_.out, a_.ldo, m0, n0, rows, width), out2(a_.out2, a_.ldo2, m0, n0, rows, width),
         z(a_.Z, a_.ldz, m0, n0, rows, width), r(a_.R, a_.ldr, m0, n0, rows, width), bias{0.f, 0.f, 0.f, 0.f},
-        n((uint32_t)col) {
-    if (OP == DATTRI_LINEAR_FORWARD && a.bias) bias = load4_elt<ELT>(a.bias, n0 + col, true, 4);
+        n((uint32_t)col), cnt(APART > 1 ? min(4, (width - col + APART - 1) / APART) : 4) {
+    if (OP == DATTRI_LINEAR_FORWARD && a.bias) {
+      if constexpr (APART == 1) {
+        bias = load4_elt<ELT>(a.bias, n0 + col, true, 4);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (e < cnt) bias[e] = load_elt<ELT>(a.bias, n0 + col + e * APART);
+      }
+    }
   }
   __device__ void run(const int (&at)[U], f32x4 (&v)[U]) const {
     f32x4 x[U], y[U];
     if (OP != DATTRI_LINEAR_WEIGHT_GRAD && a.R) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) x[u] = buffer_load4<ELT>(r.r, at[u] * r.ld + n * ELT);
+      for (int u = 0; u < U; ++u) x[u] = buffer_load4<ELT, APART>(r.r, at[u] * r.ld + n * ELT, cnt);
     }
     if constexpr (OP == DATTRI_LINEAR_FORWARD) {
 #pragma unroll
       for (int u = 0; u < U; ++u) v[u] += bias;
       if (a.Z) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) buffer_store4<ELT>(z.r, at[u] * z.ld + n * ELT, v[u]);
+        for (int u = 0; u < U; ++u) buffer_store4<ELT, APART>(z.r, at[u] * z.ld + n * ELT, v[u], cnt);
       }
       if (a.act != DATTRI_ACT_NONE) {
 #pragma unroll
@@ -177,12 +206,12 @@ struct TileEpilogue {
         for (int u = 0; u < U; ++u) v[u] += x[u];
       }
 #pragma unroll
-      for (int u = 0; u < U; ++u) buffer_store4<ELT>(out.r, at[u] * out.ld + n * ELT, v[u]);
+      for (int u = 0; u < U; ++u) buffer_store4<ELT, APART>(out.r, at[u] * out.ld + n * ELT, v[u], cnt);
     } else if constexpr (OP == DATTRI_LINEAR_INPUT_GRAD) {
       const bool slope = a.out2 && a.act != DATTRI_ACT_NONE;
       if (slope) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) y[u] = buffer_load4<ELT>(z.r, at[u] * z.ld + n * ELT);
+        for (int u = 0; u < U; ++u) y[u] = buffer_load4<ELT, APART>(z.r, at[u] * z.ld + n * ELT, cnt);
       }
       if (a.R) {
 #pragma unroll
@@ -190,7 +219,7 @@ struct TileEpilogue {
       }
       if (a.out) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) buffer_store4<ELT>(out.r, at[u] * out.ld + n * ELT, v[u]);
+        for (int u = 0; u < U; ++u) buffer_store4<ELT, APART>(out.r, at[u] * out.ld + n * ELT, v[u], cnt);
       }
       if (slope) {
 #pragma unroll
@@ -198,15 +227,15 @@ struct TileEpilogue {
       }
       if (a.out2) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) buffer_store4<ELT>(out2.r, at[u] * out2.ld + n * ELT, v[u]);
+        for (int u = 0; u < U; ++u) buffer_store4<ELT, APART>(out2.r, at[u] * out2.ld + n * ELT, v[u], cnt);
       }
     } else {
       if (a.accumulate) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) v[u] += buffer_load4<4>(out.r, at[u] * out.ld + n * 4);
+        for (int u = 0; u < U; ++u) v[u] += buffer_load4<4, APART>(out.r, at[u] * out.ld + n * 4, cnt);
       }
 #pragma unroll
-      for (int u = 0; u < U; ++u) buffer_store4<4>(out.r, at[u] * out.ld + n * 4, v[u]);
+      for (int u = 0; u < U; ++u) buffer_store4<4, APART>(out.r, at[u] * out.ld + n * 4, v[u], cnt);
     }
   }
 };

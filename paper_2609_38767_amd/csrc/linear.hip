@@ -379,28 +379,39 @@ __global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void gemm_kernel(GemmAr
       if (n0 + 4 * c < ld_part)
 #pragma unroll 4
         for (int row = tid / LPR; row < WM * 32; row += 256 / LPR)
-          buffer_store4<4>(out.r, tile_row(row) * out.ld + 16 * c, value(row));
-    } else if (a.vec && (a.N - n0 >= TN || a.N % 4 == 0)) {  // whole fours
-      const int width = min(TN, a.N - n0);
-      if (4 * c < width) {
-        const TileEpilogue<OP, ELT, kRows> e(a, m0, n0, min(TM, a.M - m0), width, 4 * c);
+          buffer_store4<4, 1>(out.r, tile_row(row) * out.ld + 16 * c, value(row), 4);
+    } else {
+      const int rows = min(TM, a.M - m0), width = min(TN, a.N - n0);
+      auto finish = [&](auto take, const auto& e, auto get) {  // `take` rows at once
+        constexpr int U = decltype(take)::value;
 #pragma unroll 1
-        for (int row = tid / LPR; row < WM * 32; row += 256 / LPR * kRows) {
-          int at[kRows];
-          f32x4 v[kRows];
+        for (int row = tid / LPR; row < WM * 32; row += 256 / LPR * U) {
+          int at[U];
+          f32x4 v[U];
 #pragma unroll
-          for (int u = 0; u < kRows; ++u) {
+          for (int u = 0; u < U; ++u) {
             at[u] = tile_row(row + u * (256 / LPR));
-            v[u] = value(row + u * (256 / LPR));
+            v[u] = get(row + u * (256 / LPR));
           }
           e.run(at, v);
         }
-      }
-    } else {
-#pragma unroll 1
-      for (int row = tid / LPR; row < WM * 32; row += 256 / LPR) {
-        const int m = m0 + tile_row(row), n = n0 + 4 * c;
-        if (m < a.M && n < a.N) epilogue4<OP, ELT>(a, m, n, value(row));
+      };
+      if (a.vec && width % 4 == 0) {  // four neighbours per lane
+        if (4 * c < width)
+          finish(std::integral_constant<int, kRows>{}, TileEpilogue<OP, ELT, kRows, 1>(a, m0, n0, rows, width, 4 * c), value);
+      } else {  // rows on any element: every LPR-th column, so that lanes are neighbours
+        auto apart = [&](int row) {
+          f32x4 v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int n = c + e * LPR;
+            v[e] = *(const float*)((row & 32 ? y1 : y0) + (row & 31) * (TN * 4) + (((n >> 2) ^ (row & 15)) << 4) +
+                                   (n & 3) * 4);
+          }
+          return v;
+        };
+        if (c < width)
+          finish(std::integral_constant<int, 2>{}, TileEpilogue<OP, ELT, 2, LPR>(a, m0, n0, rows, width, c), apart);
       }
     }
   }
@@ -673,6 +684,7 @@ hipError_t launch_column_sums(int elt, const void* G, int64_t ld_g, int64_t rows
 }  // namespace
 
 size_t linear_workspace_need(dattri_linear_op op, int64_t rows, int64_t d_in, int64_t d_out, int elt, bool aligned) {
+  if (linear_few(op, rows, d_out)) return 0;
   return linear_layout(op, rows, d_in, d_out, elt, aligned).total;
 }
 
@@ -681,6 +693,11 @@ hipError_t launch_linear(dattri_linear_op op, int elt, bool aligned, GemmArgs a,
   const bool wgrad = op == DATTRI_LINEAR_WEIGHT_GRAD;
   const int64_t rows = wgrad ? a.K : a.M, d_out = op == DATTRI_LINEAR_FORWARD ? a.N : wgrad ? a.M : a.K,
                 d_in = op == DATTRI_LINEAR_FORWARD ? a.K : a.N;
+  const int oelt = wgrad ? 4 : elt;
+  auto on4 = [](const void* p, int64_t ld, int e) { return !p || ((uintptr_t)p % (4 * e) == 0 && ld % 4 == 0); };
+  a.vec = on4(a.bias, 0, elt) && on4(a.R, a.ldr, elt) && on4(a.Z, a.ldz, elt) && on4(a.out, a.ldo, oelt) &&
+          on4(a.out2, a.ldo2, elt);
+  if (linear_few(op, rows, d_out)) return launch_linear_few(elt, a, aligned && (d_in * elt) % 16 == 0, s);
   const LinearLayout L = linear_layout(op, rows, d_in, d_out, elt, aligned);
   hipError_t e;
   if (dbias) {
@@ -698,10 +715,6 @@ hipError_t launch_linear(dattri_linear_op op, int elt, bool aligned, GemmArgs a,
       if (e != hipSuccess) return e;
     }
   }
-  const int oelt = wgrad ? 4 : elt;
-  auto on4 = [](const void* p, int64_t ld, int e) { return !p || ((uintptr_t)p % (4 * e) == 0 && ld % 4 == 0); };
-  a.vec = on4(a.bias, 0, elt) && on4(a.R, a.ldr, elt) && on4(a.Z, a.ldz, elt) && on4(a.out, a.ldo, oelt) &&
-          on4(a.out2, a.ldo2, elt);
   float* part = (float*)(ws + L.off_part);
   if (op == DATTRI_LINEAR_FORWARD)
     return elt == 2 ? launch_product<DATTRI_LINEAR_FORWARD, 2>(a, L.g, part, s)

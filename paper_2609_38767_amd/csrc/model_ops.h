@@ -54,6 +54,11 @@ size_t linear_workspace_need(dattri_linear_op op, int64_t rows, int64_t d_in, in
 hipError_t launch_linear(dattri_linear_op op, int elt, bool aligned, GemmArgs a, float* dbias, uint8_t* ws,
                          hipStream_t s);
 
+// The form for a few rows (linear_few.hip): whether a call takes it, its launch
+// (aligned: rows of X and W on 16 bytes).
+bool linear_few(dattri_linear_op op, int64_t rows, int64_t d_out);
+hipError_t launch_linear_few(int elt, const GemmArgs& a, bool aligned, hipStream_t s);
+
 // ------------------------------------------------------------------ clip
 constexpr int kClipTensors = 128;    // tensors per launch (their list is a kernel argument)
 constexpr int kClipChunk = 16384;    // elements per unit of work
