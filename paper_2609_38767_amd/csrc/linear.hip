@@ -449,19 +449,19 @@ struct Repack {
 template <int ELT>
 __global__ __launch_bounds__(256) void repack_kernel(Repack a, Repack b) {
   constexpr int EPL = 16 / ELT;
-  const int64_t na = a.rows * (a.ld_out / EPL), total = na + b.rows * (b.ld_out / EPL);
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const Repack& p = i < na ? a : b;
-    const int64_t at = i < na ? i : i - na;
-    const int chunks = p.ld_out / EPL;
-    const int64_t r = at / chunks;
-    const int c = (int)(at - r * chunks) * EPL;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t at = (int64_t)blockIdx.x * 4 + wave;  // a wave per row
+  if (at >= a.rows + b.rows) return;
+  const Repack& p = at < a.rows ? a : b;
+  const int64_t r = at < a.rows ? at : at - a.rows;
+  const uint8_t* src = p.src + r * p.ld * ELT;
+  uint8_t* dst = p.dst + r * p.ld_out * ELT;
+  for (int c = lane * EPL; c < p.ld_out; c += 64 * EPL) {
     uint32_t v[EPL];
 #pragma unroll
     for (int e = 0; e < EPL; ++e) {
       v[e] = 0;
-      if (c + e < p.w)
-        v[e] = ELT == 2 ? ((const uint16_t*)p.src)[r * p.ld + c + e] : ((const uint32_t*)p.src)[r * p.ld + c + e];
+      if (c + e < p.w) v[e] = ELT == 2 ? ((const uint16_t*)src)[c + e] : ((const uint32_t*)src)[c + e];
     }
     i32x4 o;
     if (ELT == 2)
@@ -469,43 +469,68 @@ __global__ __launch_bounds__(256) void repack_kernel(Repack a, Repack b) {
                 (int)(v[6 % EPL] | v[7 % EPL] << 16)};
     else
       o = i32x4{(int)v[0], (int)v[1], (int)v[2], (int)v[3]};
-    *(i32x4*)(p.dst + at * 16) = o;
+    *(i32x4*)(dst + c * ELT) = o;
   }
 }
 
-// Column sums over rows [y * per, (y + 1) * per): a wave owns 64 columns and
-// every fourth row of the range; the waves' sums are added in wave order.
-template <int ELT>
+// Column sums over rows [y * per, (y + 1) * per): a wave owns 64 C columns, C
+// neighbours per lane, and every fourth row of the range; the waves' sums are
+// added in wave order.  8192 x 14336 bf16 (235 MB): one column per lane took 80
+// us, two bytes per lane and load.
+template <int ELT, int C>
 __global__ __launch_bounds__(256) void column_sums_kernel(const void* __restrict__ G, int64_t ld, int64_t rows,
                                                           int cols, int64_t per, float* __restrict__ out,
                                                           int accumulate) {
-  __shared__ float red[4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+  constexpr int kAhead = 8;
+  __shared__ float red[4][64 * C];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (blockIdx.x * 64 + lane) * C;
   const int64_t r0 = blockIdx.y * per, r1 = min(rows, r0 + per);
-  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  f32x4 s[2] = {};
+  auto get = [&](int64_t r) {
+    if constexpr (C == 4) return load4_elt<ELT>(G, r * ld + c, true, 4);
+    return f32x4{load_elt<ELT>(G, r * ld + c), 0.f, 0.f, 0.f};
+  };
   if (c < cols) {
     int64_t r = r0 + wave;
-    for (; r + 12 < r1; r += 16)
+    for (; r + 4 * (kAhead - 1) < r1; r += 4 * kAhead) {
+      f32x4 v[kAhead];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) s[u] += load_elt<ELT>(G, (r + 4 * u) * ld + c);
-    for (; r < r1; r += 4) s[0] += load_elt<ELT>(G, r * ld + c);
+      for (int u = 0; u < kAhead; ++u) v[u] = get(r + 4 * u);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) s[u & 1] += v[u];
+    }
+    for (; r < r1; r += 4) s[0] += get(r);
   }
-  red[wave][lane] = (s[0] + s[1]) + (s[2] + s[3]);
+  s[0] += s[1];
+#pragma unroll
+  for (int e = 0; e < C; ++e) red[wave][e * 64 + lane] = s[0][e];
   __syncthreads();
   if (wave == 0 && c < cols) {
-    const float v = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
-    float* o = out + (int64_t)blockIdx.y * cols + c;
-    *o = accumulate ? *o + v : v;
+#pragma unroll
+    for (int e = 0; e < C; ++e) {
+      const int i = e * 64 + lane;
+      const float v = (red[0][i] + red[1][i]) + (red[2][i] + red[3][i]);
+      float* o = out + (int64_t)blockIdx.y * cols + c + e;
+      *o = accumulate ? *o + v : v;
+    }
   }
 }
 
+// A wave per 64 columns and four interleaved runs of the parts.
 __global__ __launch_bounds__(256) void column_join_kernel(const float* __restrict__ part, int n_parts, int cols,
                                                           float* __restrict__ out, int accumulate) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= cols) return;
+  __shared__ float red[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
   float s = 0.f;
-  for (int y = 0; y < n_parts; ++y) s += part[(int64_t)y * cols + c];
-  out[c] = accumulate ? out[c] + s : s;
+  if (c < cols)
+#pragma unroll 4
+    for (int y = wave; y < n_parts; y += 4) s += part[(int64_t)y * cols + c];
+  red[wave][lane] = s;
+  __syncthreads();
+  if (wave == 0 && c < cols) {
+    s = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
+    out[c] = accumulate ? out[c] + s : s;
+  }
 }
 
 namespace {
@@ -572,10 +597,11 @@ GemmShape gemm_shape(int64_t M, int64_t N, int64_t K, int elt, bool ac, bool bc)
   return best;
 }
 
-// Column sums: rows per part, parts.
+// Column sums: rows per part, parts.  Parts of at least 64 rows until there are
+// eight workgroups per CU.
 void column_shape(int64_t rows, int64_t cols, int64_t* per, int64_t* parts) {
-  const int64_t strips = (cols + 63) / 64;
-  int64_t p = std::max<int64_t>(1, std::min<int64_t>(1024 / strips, rows / 64));
+  const int64_t strips = (cols + 255) / 256;
+  const int64_t p = std::max<int64_t>(1, std::min<int64_t>(2048 / strips, rows / 64));
   *per = std::max<int64_t>(1, (rows + p - 1) / p);
   *parts = std::max<int64_t>(1, (rows + *per - 1) / *per);
 }
@@ -671,12 +697,15 @@ hipError_t launch_column_sums(int elt, const void* G, int64_t ld_g, int64_t rows
                               bool accumulate, float* part, hipStream_t s) {
   int64_t per, parts;
   column_shape(rows, cols, &per, &parts);
-  auto k = elt == 2 ? column_sums_kernel<2> : column_sums_kernel<4>;
-  hipLaunchKernelGGL(k, dim3((unsigned)((cols + 63) / 64), (unsigned)parts), dim3(256), 0, s, G, ld_g, rows, (int)cols,
+  const bool four = (uintptr_t)G % (4 * elt) == 0 && ld_g % 4 == 0 && cols % 4 == 0;
+  auto k = elt == 2 ? (four ? column_sums_kernel<2, 4> : column_sums_kernel<2, 1>)
+                    : (four ? column_sums_kernel<4, 4> : column_sums_kernel<4, 1>);
+  const int64_t wide = four ? 256 : 64;
+  hipLaunchKernelGGL(k, dim3((unsigned)((cols + wide - 1) / wide), (unsigned)parts), dim3(256), 0, s, G, ld_g, rows, (int)cols,
                      per, parts > 1 ? part : out, parts > 1 ? 0 : (int)accumulate);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || parts == 1) return e;
-  hipLaunchKernelGGL(column_join_kernel, dim3((unsigned)((cols + 255) / 256)), dim3(256), 0, s, part, (int)parts,
+  hipLaunchKernelGGL(column_join_kernel, dim3((unsigned)((cols + 63) / 64)), dim3(256), 0, s, part, (int)parts,
                      (int)cols, out, (int)accumulate);
   return hipGetLastError();
 }
@@ -708,9 +737,10 @@ hipError_t launch_linear(dattri_linear_op op, int elt, bool aligned, GemmArgs a,
     Repack ra = {}, rb = {};
     if (L.pack_a) ra = repack_of(&a.A, &a.lda, L.a_w, L.a_rows, elt, ws + L.off_a);
     if (L.pack_b) rb = repack_of(&a.B, &a.ldb, L.b_w, L.b_rows, elt, ws + L.off_b);
-    const int64_t n = (ra.rows * ra.ld_out + rb.rows * rb.ld_out) * elt / 16;
+    const int64_t n = ra.rows + rb.rows;
     if (n > 0) {
-      hipLaunchKernelGGL(elt == 2 ? repack_kernel<2> : repack_kernel<4>, dim3(flat_grid(n)), dim3(256), 0, s, ra, rb);
+      hipLaunchKernelGGL(elt == 2 ? repack_kernel<2> : repack_kernel<4>, dim3((unsigned)((n + 3) / 4)), dim3(256), 0, s,
+                         ra, rb);
       e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
