@@ -56,25 +56,28 @@ __device__ inline void store4_elt(void* p, int64_t i, f32x4 v, bool vec, int cnt
     if (e < cnt) store_elt<ELT>(p, i + e, v[e]);
 }
 
-// v = act(v); v *= act'(z).  One choice of activation for four values.
-template <int ELT>
-__device__ inline void act_values(f32x4& v, int act) {
-  auto each = [&](auto kind) {
+// v = act(v) and v *= act'(z) for U times four values, one choice of activation for all.
+template <int ELT, int U>
+__device__ inline void act_values(f32x4 (&v)[U], int act) {
+  with_act(act, [&](auto kind) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = act_value<ELT>(v[e], decltype(kind)::value);
-  };
-  with_act(act, each);
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[u][e] = act_value<ELT>(v[u][e], decltype(kind)::value);
+  });
 }
-template <int ELT>
-__device__ inline void slope_values(f32x4& v, f32x4 z, int act) {
-  auto each = [&](auto kind) {
+template <int ELT, int U>
+__device__ inline void slope_values(f32x4 (&v)[U], const f32x4 (&z)[U], int act) {
+  with_act(act, [&](auto kind) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float s = act_slope<ELT>(z[e], decltype(kind)::value);
-      v[e] = decltype(kind)::value == DATTRI_ACT_RELU && s == 0.f ? 0.f : v[e] * s;  // a closed relu passes nothing, not 0 * inf
-    }
-  };
-  with_act(act, each);
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float s = act_slope<ELT>(z[u][e], decltype(kind)::value);
+        // a closed relu passes nothing, not 0 * inf
+        v[u][e] = decltype(kind)::value == DATTRI_ACT_RELU && s == 0.f ? 0.f : v[u][e] * s;
+      }
+  });
 }
 
 // m < M and n < N; a.vec: every row of the epilogue's buffers starts on four elements.
@@ -87,7 +90,9 @@ __device__ inline void epilogue4(const GemmArgs& a, int m, int n, f32x4 v) {
     if (a.Z) store4_elt<ELT>(a.Z, m * a.ldz + n, v, vec, cnt);
     f32x4 r = {0.f, 0.f, 0.f, 0.f};
     if (a.R) r = load4_elt<ELT>(a.R, m * a.ldr + n, vec, cnt);
-    act_values<ELT>(v, a.act);
+    f32x4 y[1] = {v};
+    act_values<ELT, 1>(y, a.act);
+    v = y[0];
     if (a.R) v += r;
     store4_elt<ELT>(a.out, m * a.ldo + n, v, vec, cnt);
   } else if constexpr (OP == DATTRI_LINEAR_INPUT_GRAD) {
@@ -97,7 +102,12 @@ __device__ inline void epilogue4(const GemmArgs& a, int m, int n, f32x4 v) {
     if (a.R) v += load4_elt<ELT>(a.R, m * a.ldr + n, vec, cnt);
     if (a.out) store4_elt<ELT>(a.out, m * a.ldo + n, v, vec, cnt);
     if (!a.out2) return;
-    if (slope) slope_values<ELT>(v, z, a.act);
+    if (slope) {
+      f32x4 p[1] = {v};
+      const f32x4 at[1] = {z};
+      slope_values<ELT, 1>(p, at, a.act);
+      v = p[0];
+    }
     store4_elt<ELT>(a.out2, m * a.ldo2 + n, v, vec, cnt);
   } else {
     if (a.accumulate) v += load4_elt<4>(a.out, m * a.ldo + n, vec, cnt);
@@ -197,10 +207,7 @@ struct TileEpilogue {
 #pragma unroll
         for (int u = 0; u < U; ++u) buffer_store4<ELT, APART>(z.r, at[u] * z.ld + n * ELT, v[u], cnt);
       }
-      if (a.act != DATTRI_ACT_NONE) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) act_values<ELT>(v[u], a.act);
-      }
+      act_values<ELT, U>(v, a.act);
       if (a.R) {
 #pragma unroll
         for (int u = 0; u < U; ++u) v[u] += x[u];
@@ -221,10 +228,7 @@ struct TileEpilogue {
 #pragma unroll
         for (int u = 0; u < U; ++u) buffer_store4<ELT, APART>(out.r, at[u] * out.ld + n * ELT, v[u], cnt);
       }
-      if (slope) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) slope_values<ELT>(v[u], y[u], a.act);
-      }
+      if (slope) slope_values<ELT, U>(v, y, a.act);
       if (a.out2) {
 #pragma unroll
         for (int u = 0; u < U; ++u) buffer_store4<ELT, APART>(out2.r, at[u] * out2.ld + n * ELT, v[u], cnt);
