@@ -448,7 +448,6 @@ struct Repack {
 };
 template <int ELT>
 __global__ __launch_bounds__(256) void repack_kernel(Repack a, Repack b) {
-  constexpr int EPL = 16 / ELT;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t at = (int64_t)blockIdx.x * 4 + wave;  // a wave per row
   if (at >= a.rows + b.rows) return;
@@ -456,20 +455,12 @@ __global__ __launch_bounds__(256) void repack_kernel(Repack a, Repack b) {
   const int64_t r = at < a.rows ? at : at - a.rows;
   const uint8_t* src = p.src + r * p.ld * ELT;
   uint8_t* dst = p.dst + r * p.ld_out * ELT;
-  for (int c = lane * EPL; c < p.ld_out; c += 64 * EPL) {
-    uint32_t v[EPL];
-#pragma unroll
-    for (int e = 0; e < EPL; ++e) {
-      v[e] = 0;
-      if (c + e < p.w) v[e] = ELT == 2 ? ((const uint16_t*)src)[c + e] : ((const uint32_t*)src)[c + e];
-    }
-    i32x4 o;
-    if (ELT == 2)
-      o = i32x4{(int)(v[0] | v[1] << 16), (int)(v[2] | v[3] << 16), (int)(v[4 % EPL] | v[5 % EPL] << 16),
-                (int)(v[6 % EPL] | v[7 % EPL] << 16)};
+#pragma unroll 8
+  for (int c = lane; c < p.ld_out; c += 64) {
+    if constexpr (ELT == 2)
+      ((uint16_t*)dst)[c] = c < p.w ? ((const uint16_t*)src)[c] : (uint16_t)0;
     else
-      o = i32x4{(int)v[0], (int)v[1], (int)v[2], (int)v[3]};
-    *(i32x4*)(dst + c * ELT) = o;
+      ((uint32_t*)dst)[c] = c < p.w ? ((const uint32_t*)src)[c] : 0u;
   }
 }
 
@@ -572,8 +563,9 @@ GemmShape gemm_shape(int64_t M, int64_t N, int64_t K, int elt, bool ac, bool bc)
     return cut(v, std::min<int64_t>(64, (v == kFew ? 1024 : 768) / std::max<int64_t>(tiles, 1)));
   }
   // Else the cut with the least time as modelled, in us: the CU with most tiles
-  // (FLOP at the rate one CU reaches on a large product, plus what a tile costs
-  // besides), and the partial tiles of a split written, read and joined.  1531 x 1024 -> 4096 float32: 128 x
+  // (FLOP at the rate one CU reaches on a large product, 12% less where it has one
+  // workgroup of 128 x 128 only; plus what a tile costs besides), and the partial
+  // tiles of a split written, read and joined.  1531 x 1024 -> 4096 float32: 128 x
   // 128 whole 123 us, in two splits 110, 256 x 256 244.
   const double rate[2] = {elt == 2 ? 5.2e6 : 0.58e6, elt == 2 ? 4.0e6 : 0.565e6}, fixed[2] = {12., 3.};
   const int64_t all = (K * elt + 63) / 64 * 64;
@@ -583,11 +575,13 @@ GemmShape gemm_shape(int64_t M, int64_t N, int64_t K, int elt, bool ac, bool bc)
     for (int64_t splits = 1; splits <= 32; ++splits) {
       const GemmShape g = cut((Variant)v, splits);
       if (g.splits != splits) continue;
-      // in tiles of sps stages: the last split may be short
-      const double tiles = (double)g.nm * g.nn * (splits > 1 ? (double)all / ((int64_t)g.sps * g.kw) : 1.);
+      // the CU with most tiles; the last split's may be short
+      const double each = (double)g.nm * g.nn, last = splits > 1 ? (double)all / ((int64_t)g.sps * g.kw) - (splits - 1) : 1.;
+      const bool alone = each * splits <= 256.;
+      const double rounds = alone ? 1. : std::max(1. + last, std::ceil(each * (splits - 1 + last) / 256.));
       const int64_t side = v == kBig ? 256 : 128;
       const double flop = 2. * side * side * g.sps * (g.kw / elt);
-      double us = std::ceil(tiles / 256.) * (flop / rate[v] + fixed[v]);
+      double us = rounds * (flop / (rate[v] * (alone && v == kMid ? 0.88 : 1.)) + fixed[v]);
       if (g.splits > 1) us += 3. + 8. * g.splits * M * N / 6.0e6;
       if (best_us == 0. || us < best_us) {
         best = g;
