@@ -12,7 +12,9 @@
 // took 14 us where nothing was to be scaled).
 //
 // What bounds it: memory.  The norm has to be known before the first gradient
-// is scaled, so what the caches do not hold is read twice.
+// is scaled, so what the caches do not hold is read twice.  872 M elements, bf16
+// into float32: squares 323-345 us (5.1-5.4 TB/s), scaling 943 us (5.6 TB/s read
+// and written).
 #include "api_common.h"
 #include "device_common.h"
 #include "model_ops.h"

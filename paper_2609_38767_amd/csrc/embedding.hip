@@ -15,7 +15,10 @@
 // sort's first kernel: the sort is a few waves' latency, the zeros are bandwidth.
 //
 // What bounds it: the lookup and the sums read and write each row once; for a
-// whole table the zeros of rows without tokens are most of the bytes.
+// whole table the zeros of rows without tokens are most of the bytes.  16384
+// tokens, 128000 x 4096 bf16: lookup 32 us by itself, 45 with its operands out of
+// the caches; gradient: sort and 2.1 GB of zeros in one launch 338 us (6.2 TB/s),
+// groups 18, rows 74.
 #include <algorithm>
 
 #include "api_common.h"

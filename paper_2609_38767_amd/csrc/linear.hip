@@ -1,7 +1,7 @@
 // Linear layers with a fused epilogue and their backward products:
 //   C[m][n] = sum_k A(m, k) B(n, k), then epilogue4.
 //
-// Tile kernel.  Four waves (one per SIMD) each own BI x BJ blocks of 32 x 32
+// Tile kernel.  Four waves (one per SIMD) each own BN x BM blocks of 32 x 32
 // outputs; the blocks' rows run along n and their columns along m, so a lane
 // holds four neighbouring n of one m.  bf16 products are
 // v_mfma_f32_32x32x16_bf16, float32 ones v_mfma_f32_32x32x2f32.  Operands come
@@ -30,6 +30,12 @@
 // The accumulators leave through LDS, 32 columns of blocks at a time as float32
 // rows, so that the epilogue is one short loop over whole rows: its loads and
 // stores of Z, R and the outputs are contiguous per wave.
+//
+// What bounds it: 8192 x 4096 -> 14336 bf16, medians of five: forward 780 us
+// (1230 TFLOP/s; the vendor library 665), input gradient 735 (1310; 734), weight
+// gradient 776 (1240; 979).  The matrix cores are 70, 73 and 67% busy, at a
+// clock that the load holds at 1.7 GHz.  The weight gradient's 896 tiles are 3.5 rounds
+// of 256 CUs.  Float32, 4096 cubed: 144-150 TFLOP/s (the library 148-150).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
