@@ -13,7 +13,7 @@
 //
 // What bounds it: memory.  The norm has to be known before the first gradient
 // is scaled, so what the caches do not hold is read twice.  872 M elements, bf16
-// into float32: squares 323-345 us (5.1-5.4 TB/s), scaling 943 us (5.6 TB/s read
+// into float32: squares 252-262 us (6.7-6.9 TB/s), scaling 973 us (5.4 TB/s read
 // and written).
 #include "api_common.h"
 #include "device_common.h"
@@ -65,14 +65,22 @@ __device__ inline float load_one(const uint8_t* p, int i) {
 
 constexpr int kBatch = 8;  // 16-byte loads in flight per thread
 
-// stream: past the caches, for sets that no cache holds until the second pass
-// (1.7 GB of bf16: squares 255 us, 325 through the caches).
-__device__ inline i32x4 load_piece(const uint8_t* p, bool stream) {
-  return stream ? __builtin_nontemporal_load((const i32x4*)p) : *(const i32x4*)p;
+// STREAM: loads past the caches, for sets that no cache holds until the second
+// pass.  bf16, norm alone: 288 MB 49 us, 50 through the caches; 480 MB 78 and 88;
+// 1.74 GB 267 and 302.  Scaled into float32: 220 and 239, 359 and 381, 1275 and
+// 1321 us.  Stores past the caches instead are slower (1.74 GB: 1927).  A
+// template argument: under a run-time flag the compiler merges both loads into
+// a plain one.
+template <bool STREAM>
+__device__ inline i32x4 load_piece(const uint8_t* p) {
+  if constexpr (STREAM)
+    return __builtin_nontemporal_load((const i32x4*)p);
+  else
+    return *(const i32x4*)p;
 }
 
-template <int ELT>
-__device__ inline double chunk_squares(const uint8_t* p, int count, bool stream) {
+template <int ELT, bool STREAM>
+__device__ inline double chunk_squares(const uint8_t* p, int count) {
   constexpr int EPL = 16 / ELT, kStep = 256 * EPL * kBatch;
   double s[2] = {0., 0.};
   int done = 0;
@@ -81,7 +89,7 @@ __device__ inline double chunk_squares(const uint8_t* p, int count, bool stream)
       i32x4 w[kBatch];
 #pragma unroll
       for (int u = 0; u < kBatch; ++u)
-        w[u] = load_piece(p + (int64_t)(done + (u * 256 + threadIdx.x) * EPL) * ELT, stream);
+        w[u] = load_piece<STREAM>(p + (int64_t)(done + (u * 256 + threadIdx.x) * EPL) * ELT);
 #pragma unroll
       for (int u = 0; u < kBatch; ++u) {
         float v[EPL];
@@ -118,7 +126,8 @@ __device__ inline double block_sum(double s) {
   return s;
 }
 
-__global__ __launch_bounds__(256) void clip_squares_kernel(ClipList l, double* __restrict__ partials, int stream) {
+template <bool STREAM>
+__global__ __launch_bounds__(256) void clip_squares_kernel(ClipList l, double* __restrict__ partials) {
   double s = 0.;
   const int chunks = l.first[l.n];
   for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
@@ -126,7 +135,7 @@ __global__ __launch_bounds__(256) void clip_squares_kernel(ClipList l, double* _
     const ClipTensor& t = l.t[k.tensor];
     const int elt = t.size_flags & 1 ? 4 : 2;
     const uint8_t* p = (const uint8_t*)t.src + k.begin * elt;
-    s += elt == 4 ? chunk_squares<4>(p, k.count, stream) : chunk_squares<2>(p, k.count, stream);
+    s += elt == 4 ? chunk_squares<4, STREAM>(p, k.count) : chunk_squares<2, STREAM>(p, k.count);
   }
   s = block_sum<4>(s);
   if (threadIdx.x == 0) partials[blockIdx.x] = s;
@@ -147,18 +156,13 @@ __global__ __launch_bounds__(1024) void clip_norm_kernel(const double* __restric
 
 // One thread's 16 bytes of gradients, scaled, at element i of the output.
 template <int ELT, int OELT>
-__device__ inline void scale_piece(i32x4 w, float coef, uint8_t* q, int i, bool stream) {
+__device__ inline void scale_piece(i32x4 w, float coef, uint8_t* q, int i) {
   constexpr int EPL = 16 / ELT;
   float v[EPL];
   unpack<ELT>(w, v);
 #pragma unroll
   for (int e = 0; e < EPL; ++e) v[e] *= coef;
-  auto put = [&](auto x, uint8_t* at) {
-    if (stream)
-      __builtin_nontemporal_store(x, (decltype(x)*)at);
-    else
-      *(decltype(x)*)at = x;
-  };
+  auto put = [&](auto x, uint8_t* at) { *(decltype(x)*)at = x; };
   if constexpr (OELT == 4) {
 #pragma unroll
     for (int e = 0; e < EPL; e += 4) put(f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]}, q + (int64_t)(i + e) * 4);
@@ -170,8 +174,8 @@ __device__ inline void scale_piece(i32x4 w, float coef, uint8_t* q, int i, bool 
   }
 }
 
-template <int ELT, int OELT>
-__device__ inline void scale_chunk(const uint8_t* p, uint8_t* q, int count, float coef, bool stream) {
+template <int ELT, int OELT, bool STREAM>
+__device__ inline void scale_chunk(const uint8_t* p, uint8_t* q, int count, float coef) {
   constexpr int EPL = 16 / ELT, kStep = 256 * EPL * kBatch;
   int done = 0;
   if ((uintptr_t)p % 16 == 0 && (uintptr_t)q % 16 == 0) {
@@ -179,14 +183,14 @@ __device__ inline void scale_chunk(const uint8_t* p, uint8_t* q, int count, floa
       i32x4 w[kBatch];
 #pragma unroll
       for (int u = 0; u < kBatch; ++u)
-        w[u] = load_piece(p + (int64_t)(done + (u * 256 + threadIdx.x) * EPL) * ELT, stream);
+        w[u] = load_piece<STREAM>(p + (int64_t)(done + (u * 256 + threadIdx.x) * EPL) * ELT);
 #pragma unroll
       for (int u = 0; u < kBatch; ++u)
-        scale_piece<ELT, OELT>(w[u], coef, q, done + (u * 256 + threadIdx.x) * EPL, stream);
+        scale_piece<ELT, OELT>(w[u], coef, q, done + (u * 256 + threadIdx.x) * EPL);
     }
     const int end = count / EPL * EPL;
     for (int i = done + threadIdx.x * EPL; i < end; i += 256 * EPL)
-      scale_piece<ELT, OELT>(*(const i32x4*)(p + (int64_t)i * ELT), coef, q, i, stream);
+      scale_piece<ELT, OELT>(*(const i32x4*)(p + (int64_t)i * ELT), coef, q, i);
     done = end;
   }
 #pragma unroll 4
@@ -202,7 +206,8 @@ __device__ inline void scale_chunk(const uint8_t* p, uint8_t* q, int count, floa
 // One workgroup per chunk (872 M elements of bf16 to float32: 976 us, 1066 by
 // 2048 workgroups of many chunks), from the last chunk to the first: the norm's
 // pass has left the last ones in the caches.
-__global__ __launch_bounds__(256) void clip_scale_kernel(ClipList l, const float* __restrict__ norm_coef, int stream) {
+template <bool STREAM>
+__global__ __launch_bounds__(256) void clip_scale_kernel(ClipList l, const float* __restrict__ norm_coef) {
   const float coef = norm_coef[1];
   const Chunk k = find_chunk(l, (int)(gridDim.x - 1 - blockIdx.x));
   const ClipTensor& t = l.t[k.tensor];
@@ -210,14 +215,17 @@ __global__ __launch_bounds__(256) void clip_scale_kernel(ClipList l, const float
   const bool f = t.size_flags & 1, of = t.size_flags & 2;
   const uint8_t* p = (const uint8_t*)t.src + k.begin * (f ? 4 : 2);
   uint8_t* q = (uint8_t*)t.dst + k.begin * (of ? 4 : 2);
-  if (f && of) scale_chunk<4, 4>(p, q, k.count, coef, stream);
-  else if (f) scale_chunk<4, 2>(p, q, k.count, coef, stream);
-  else if (of) scale_chunk<2, 4>(p, q, k.count, coef, stream);
-  else scale_chunk<2, 2>(p, q, k.count, coef, stream);
+  if (f && of) scale_chunk<4, 4, STREAM>(p, q, k.count, coef);
+  else if (f) scale_chunk<4, 2, STREAM>(p, q, k.count, coef);
+  else if (of) scale_chunk<2, 4, STREAM>(p, q, k.count, coef);
+  else scale_chunk<2, 2, STREAM>(p, q, k.count, coef);
 }
 
 hipError_t launch_clip_squares(const ClipList& l, int groups, double* partials, bool stream, hipStream_t s) {
-  hipLaunchKernelGGL(clip_squares_kernel, dim3(groups), dim3(256), 0, s, l, partials, (int)stream);
+  if (stream)
+    hipLaunchKernelGGL(clip_squares_kernel<true>, dim3(groups), dim3(256), 0, s, l, partials);
+  else
+    hipLaunchKernelGGL(clip_squares_kernel<false>, dim3(groups), dim3(256), 0, s, l, partials);
   return hipGetLastError();
 }
 hipError_t launch_clip_norm(const double* partials, int n_partials, float max_norm, float* norm_coef, hipStream_t s) {
@@ -225,7 +233,10 @@ hipError_t launch_clip_norm(const double* partials, int n_partials, float max_no
   return hipGetLastError();
 }
 hipError_t launch_clip_scale(const ClipList& l, const float* norm_coef, bool stream, hipStream_t s) {
-  hipLaunchKernelGGL(clip_scale_kernel, dim3(l.first[l.n]), dim3(256), 0, s, l, norm_coef, (int)stream);
+  if (stream)
+    hipLaunchKernelGGL(clip_scale_kernel<true>, dim3(l.first[l.n]), dim3(256), 0, s, l, norm_coef);
+  else
+    hipLaunchKernelGGL(clip_scale_kernel<false>, dim3(l.first[l.n]), dim3(256), 0, s, l, norm_coef);
   return hipGetLastError();
 }
 
