@@ -196,6 +196,9 @@ __device__ inline void fill_zero(const Fill& f, int64_t b, int64_t nb) {
     for (int c = t % 64; c < f.d; c += 64) f.out[r * f.ld + c] = 0.f;
 }
 
+// Zeros alone: no token points anywhere, so there is nothing to sort.
+__global__ __launch_bounds__(1024) void zero_table_kernel(Fill f) { fill_zero<1024>(f, blockIdx.x, gridDim.x); }
+
 struct SortPass {
   const void* tokens;  // first pass: keys from the tokens, positions in order
   int token_bytes;
@@ -526,6 +529,10 @@ hipError_t launch_embedding_grad(int elt, const void* grad_out, int64_t ld_grad,
   // workgroups that zero the table: 64 KiB each at least, four rounds of the chip at most
   const int64_t share = (vocab * d * 4 + 65535) / 65536;
   auto fills = [&](int64_t most) { return accumulate ? 0u : (unsigned)std::min(share, most); };
+  if (n <= 0) {
+    hipLaunchKernelGGL(zero_table_kernel, dim3(fills(1024)), dim3(1024), 0, s, f);
+    return hipGetLastError();
+  }
   const int bits = key_bits(vocab);
   if (n <= kSmallSort && bits + kPosBits <= 32) {
     const int passes = (bits + kMaxDigit - 1) / kMaxDigit;
@@ -555,7 +562,7 @@ hipError_t launch_embedding_grad(int elt, const void* grad_out, int64_t ld_grad,
     }
   }
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || n == 0) return e;
+  if (e != hipSuccess) return e;
   const int64_t ldp = part_ld(d), n_groups = n / kRun;
   const bool al = (uintptr_t)grad_out % (4 * elt) == 0 && ld_grad % 4 == 0 && (uintptr_t)grad_table % 16 == 0 &&
                   ld_table % 4 == 0 && d % 4 == 0;
