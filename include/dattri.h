@@ -767,8 +767,10 @@ dattri_status dattri_token_scores(dattri_ctx* ctx, const void* phi_q, dattri_dty
  *
  * Common to the section: no context; row strides (ld) are in elements, 0 means
  * dense; products, sums and activations are float32 and every output is
- * rounded once to its type; all sums have a fixed order (bitwise
- * reproducible); buffers of one call must not overlap unless said otherwise.
+ * rounded once to its type (for bf16 results an activation, and each term of
+ * its slope, is within 2^-14 of itself before that, or zero where its exp is
+ * below 2^-126); all sums have a fixed order (bitwise reproducible); buffers of
+ * one call must not overlap unless said otherwise.
  * Row strides and widths of any size are accepted; rows on 16 bytes (pointer,
  * stride and width) are read without a repacking pass.  Row and token counts
  * of zero are allowed and widths are at least 1; every count and width fits
