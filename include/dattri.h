@@ -769,8 +769,9 @@ dattri_status dattri_token_scores(dattri_ctx* ctx, const void* phi_q, dattri_dty
  * dense; products, sums and activations are float32 and every output is
  * rounded once to its type (for bf16 results an activation, and each term of
  * its slope, is within 2^-14 of itself before that, or zero where its exp is
- * below 2^-126); all sums have a fixed order (bitwise reproducible); buffers of
- * one call must not overlap unless said otherwise.
+ * below 2^-126); all sums have a fixed order (bitwise reproducible).  What a
+ * call writes must not share a byte with what else it reads or writes unless
+ * said otherwise (INVALID_ARG); rows may lie between another buffer's rows.
  * Row strides and widths of any size are accepted; rows on 16 bytes (pointer,
  * stride and width) are read without a repacking pass.  Row and token counts
  * of zero are allowed and widths are at least 1; every count and width fits
@@ -885,7 +886,8 @@ dattri_status dattri_linear_weight_grad(const void* G, int64_t ld_g, const void*
  *   dtypes:     host array, F32 or BF16 per tensor
  *   outs:       NULL (norm only) or host array of device pointers; outs[i] may
  *               be grads[i] itself (in place, same type): such a tensor is not
- *               written when coef is 1.  Other overlaps are not allowed.
+ *               written when coef is 1.  No other output may overlap a
+ *               gradient or another output, so no tensor comes twice.
  *   out_dtypes: host array, F32 or BF16 per tensor; NULL with outs NULL
  *   norm_coef:  device float32 [2]: norm, coef
  *   max_norm:   >= 0, infinity allowed (coef 1)

@@ -2,6 +2,9 @@
 // launches of embedding, linear and clipping kernels.
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
+#include <memory>
+#include <new>
 
 #include "api_common.h"
 #include "dattri.h"
@@ -84,6 +87,52 @@ bool on_16(const void* a, int64_t lda, const void* b, int64_t ldb, int elt) {
   return (uintptr_t)a % 16 == 0 && (uintptr_t)b % 16 == 0 && (lda * elt) % 16 == 0 && (ldb * elt) % 16 == 0;
 }
 
+// The memory of an argument: `rows` pieces of `width` bytes, `stride` apart.
+struct Span {
+  const char* what;
+  int64_t at, rows, width, stride;
+  Span(const char* what_, const void* p, int64_t rows_, int64_t d, int64_t ld, int elt)
+      : what(what_), at((int64_t)p), rows(p ? rows_ : 0), width(d * elt), stride(ld * elt) {}
+  Span(const char* what_, const void* p, int64_t bytes) : Span(what_, p, bytes > 0, bytes, bytes, 1) {}
+  int64_t end() const { return at + (rows - 1) * stride + width; }
+  bool same(const Span& o) const { return at == o.at && width == o.width && (rows == 1 || stride == o.stride); }
+};
+
+// Whether two arguments share a byte.  Rows of one may lie between the other's
+// (column ranges of one matrix), so where the ranges meet the rows decide.
+bool overlap(const Span& a, const Span& b) {
+  if (a.rows == 0 || b.rows == 0 || a.at >= b.end() || b.at >= a.end()) return false;
+  if (a.rows == 1 && b.rows == 1) return true;
+  if (a.rows > 1 && b.rows > 1 && a.stride == b.stride) {
+    // b's row j starts `off` behind a's row j + k
+    const int64_t by = b.at - a.at, k = by >= 0 ? by / a.stride : -((a.stride - 1 - by) / a.stride), off = by - k * a.stride;
+    auto meet = [&](int64_t shift) { return std::max<int64_t>(0, shift) < std::min(a.rows, b.rows + shift); };
+    return (off < a.width && meet(k)) || (a.stride - off < b.width && meet(k + 1));
+  }
+  // every row of the one with fewer against the first row of the other that ends behind its start
+  const Span &f = a.rows <= b.rows ? a : b, &m = a.rows <= b.rows ? b : a;
+  const int64_t first = std::max<int64_t>(0, (m.at - f.at - f.width) / f.stride);
+  for (int64_t i = first; i < f.rows; ++i) {
+    const int64_t u = f.at + i * f.stride, past = u - m.at - m.width;  // m's rows that end at u or before
+    if (u >= m.end()) break;
+    const int64_t j = past < 0 ? 0 : past / m.stride + 1;
+    if (j < m.rows && m.at + j * m.stride < u + f.width) return true;
+  }
+  return false;
+}
+
+// What a call writes may not lie in what it reads or in what else it writes;
+// `in_place`, where given, may be `out` itself, element by element.
+dattri_status check_apart(const Span& out, std::initializer_list<Span> others, const Span* in_place = nullptr,
+                          const Span* in_place2 = nullptr) {
+  for (const Span& o : others)
+    if (overlap(out, o)) return fail(DATTRI_E_INVALID_ARG, "%s overlaps %s", out.what, o.what);
+  for (const Span* o : {in_place, in_place2})
+    if (o && !out.same(*o) && overlap(out, *o))
+      return fail(DATTRI_E_INVALID_ARG, "%s overlaps %s without being it", out.what, o->what);
+  return DATTRI_OK;
+}
+
 }  // namespace
 
 #define TRY(expr)                                   \
@@ -106,6 +155,8 @@ dattri_status dattri_embedding(const void* table, int64_t ld_table, int64_t voca
   TRY(check_rows("table", table, &ld_table, n > 0 ? vocab : 0, d, elt, true));
   TRY(check_rows("out", out, &ld_out, n, d, elt, true));
   TRY(check_tokens(tokens, token_bytes, n));
+  TRY(check_apart(Span("out", out, n, d, ld_out, elt),
+                  {Span("table", table, vocab, d, ld_table, elt), Span("tokens", tokens, n * token_bytes)}));
   if (n == 0) return DATTRI_OK;
   HIP_TRY(launch_embedding(elt, table, ld_table, vocab, d, tokens, token_bytes, n, scale, out, ld_out,
                            (hipStream_t)stream));
@@ -135,7 +186,14 @@ dattri_status dattri_embedding_grad(const void* grad_out, int64_t ld_grad, dattr
   TRY(check_rows("grad_out", grad_out, &ld_grad, n, d, elt, true));
   TRY(check_rows("grad_table", grad_table, &ld_table, vocab, d, 4, true));
   TRY(check_tokens(tokens, token_bytes, n));
-  TRY(check_workspace(workspace, ws_bytes, embedding_grad_layout(n, vocab, d).total));
+  const size_t need = embedding_grad_layout(n, vocab, d).total;
+  TRY(check_workspace(workspace, ws_bytes, need));
+  {
+    const Span g("grad_out", grad_out, n, d, ld_grad, elt), t("tokens", tokens, n * token_bytes),
+        out("grad_table", grad_table, vocab, d, ld_table, 4);
+    TRY(check_apart(out, {g, t}));
+    TRY(check_apart(Span("workspace", workspace, (int64_t)need), {g, t, out}));
+  }
   HIP_TRY(launch_embedding_grad(elt, grad_out, ld_grad, tokens, token_bytes, n, scale, vocab, d, grad_table, ld_table,
                                 accumulate != 0, (uint8_t*)workspace, (hipStream_t)stream));
   return DATTRI_OK;
@@ -169,7 +227,15 @@ dattri_status dattri_linear(const void* X, int64_t ld_x, const void* W, int64_t 
   if ((uintptr_t)bias % elt) return fail(DATTRI_E_INVALID_ARG, "bias is not aligned to its elements");
   if (R && R == Y && ld_r != ld_y) return fail(DATTRI_E_INVALID_ARG, "Y may be R only with the same row stride");
   const bool aligned = on_16(X, ld_x, W, ld_w, elt);
-  TRY(check_workspace(workspace, ws_bytes, linear_workspace_need(DATTRI_LINEAR_FORWARD, rows, d_in, d_out, elt, aligned)));
+  const size_t need = linear_workspace_need(DATTRI_LINEAR_FORWARD, rows, d_in, d_out, elt, aligned);
+  TRY(check_workspace(workspace, ws_bytes, need));
+  {
+    const Span x("X", X, rows, d_in, ld_x, elt), w("W", W, d_out, d_in, ld_w, elt), b("bias", bias, d_out * elt),
+        r("R", R, rows, d_out, ld_r, elt), y("Y", Y, rows, d_out, ld_y, elt), z("Z", Z, rows, d_out, ld_z, elt);
+    TRY(check_apart(y, {x, w, b, z}, &r));
+    TRY(check_apart(z, {x, w, b, r}));
+    TRY(check_apart(Span("workspace", workspace, (int64_t)need), {x, w, b, r, y, z}));
+  }
   if (rows == 0) return DATTRI_OK;
   GemmArgs a = {};
   a.A = X;
@@ -212,8 +278,16 @@ dattri_status dattri_linear_input_grad(const void* G, int64_t ld_g, const void* 
   if (Z && ((Z == P && ld_z != ld_p) || Z == D))
     return fail(DATTRI_E_INVALID_ARG, "P may be Z only with the same row stride, D may not");
   const bool aligned = on_16(G, ld_g, W, ld_w, elt);
-  TRY(check_workspace(workspace, ws_bytes,
-                      linear_workspace_need(DATTRI_LINEAR_INPUT_GRAD, rows, d_in, d_out, elt, aligned)));
+  const size_t need = linear_workspace_need(DATTRI_LINEAR_INPUT_GRAD, rows, d_in, d_out, elt, aligned);
+  TRY(check_workspace(workspace, ws_bytes, need));
+  {
+    const Span g("G", G, rows, d_out, ld_g, elt), w("W", W, d_out, d_in, ld_w, elt), r("R", R, rows, d_in, ld_r, elt),
+        z("Z", act == DATTRI_ACT_NONE || !P ? nullptr : Z, rows, d_in, ld_z, elt), d("D", D, rows, d_in, ld_d, elt),
+        p("P", P, rows, d_in, ld_p, elt);
+    TRY(check_apart(d, {g, w, z, p}, &r));
+    TRY(check_apart(p, {g, w}, &r, &z));
+    TRY(check_apart(Span("workspace", workspace, (int64_t)need), {g, w, r, z, d, p}));
+  }
   if (rows == 0) return DATTRI_OK;
   GemmArgs a = {};
   a.A = G;
@@ -250,8 +324,15 @@ dattri_status dattri_linear_weight_grad(const void* G, int64_t ld_g, const void*
   if ((uintptr_t)dbias % 4) return fail(DATTRI_E_INVALID_ARG, "dbias is not aligned to its elements");
   if (!dW && !dbias) return fail(DATTRI_E_INVALID_ARG, "nothing to compute: dW and dbias are NULL");
   const bool aligned = on_16(G, ld_g, X, ld_x, elt);
-  TRY(check_workspace(workspace, ws_bytes,
-                      linear_workspace_need(DATTRI_LINEAR_WEIGHT_GRAD, rows, d_in, d_out, elt, aligned)));
+  const size_t need = linear_workspace_need(DATTRI_LINEAR_WEIGHT_GRAD, rows, d_in, d_out, elt, aligned);
+  TRY(check_workspace(workspace, ws_bytes, need));
+  {
+    const Span g("G", G, rows, d_out, ld_g, elt), x("X", dW ? X : nullptr, rows, d_in, ld_x, elt),
+        w("dW", dW, d_out, d_in, ld_dw, 4), b("dbias", dbias, d_out * 4);
+    TRY(check_apart(w, {g, x, b}));
+    TRY(check_apart(b, {g, x}));
+    TRY(check_apart(Span("workspace", workspace, (int64_t)need), {g, x, w, b}));
+  }
   if (rows == 0 && accumulate) return DATTRI_OK;
   GemmArgs a = {};
   a.A = G;
@@ -321,6 +402,49 @@ dattri_status clip_sizes(const int64_t* sizes, int64_t n_tensors, int64_t* parti
   return st;
 }
 
+// A scaled tensor may lie in no other tensor of the call, and in its own source
+// only if it is that: sources and outputs in the order of their addresses, no
+// output in front of an end and nothing in front of an output's.
+dattri_status clip_apart(const void* const* grads, const int64_t* sizes, const dattri_dtype* dtypes, void* const* outs,
+                         const dattri_dtype* out_dtypes, int64_t n_tensors, const Span& norm_coef,
+                         const Span& workspace) {
+  TRY(check_apart(workspace, {norm_coef}));
+  struct Piece {
+    uintptr_t at, end;
+    int64_t tensor;
+    bool operator<(const Piece& o) const { return at < o.at; }
+  };
+  const std::unique_ptr<Piece[]> all(new (std::nothrow) Piece[2 * n_tensors + 1]);
+  if (!all) return fail(DATTRI_E_UNSUPPORTED, "no host memory for a list of %lld tensors", (long long)n_tensors);
+  Piece *src = all.get(), *src_end = src, *dst = src + n_tensors, *dst_end = dst;
+  for (int64_t i = 0; i < n_tensors; ++i) {
+    if (sizes[i] == 0) continue;
+    const uintptr_t p = (uintptr_t)grads[i], q = outs ? (uintptr_t)outs[i] : 0;
+    const int64_t bytes = sizes[i] * (dtypes[i] == DATTRI_F32 ? 4 : 2);
+    if (p != q) *src_end++ = Piece{p, p + bytes, i};
+    if (outs) *dst_end++ = Piece{q, q + sizes[i] * (out_dtypes[i] == DATTRI_F32 ? 4 : 2), i};
+    for (const Span* o : {&norm_coef, &workspace})
+      for (const Piece* e : {p != q ? src_end - 1 : nullptr, outs ? dst_end - 1 : nullptr})
+        if (e && e->at < (uintptr_t)o->end() && (uintptr_t)o->at < e->end)
+          return fail(DATTRI_E_INVALID_ARG, "tensor %lld overlaps %s", (long long)i, o->what);
+  }
+  if (!outs) return DATTRI_OK;
+  if (!std::is_sorted(src, src_end)) std::sort(src, src_end);
+  if (!std::is_sorted(dst, dst_end)) std::sort(dst, dst_end);
+  Piece read{0, 0, -1}, written{0, 0, -1};  // the ones that reach furthest
+  while (src != src_end || dst != dst_end) {
+    const bool w = src == src_end || (dst != dst_end && dst->at < src->at);
+    const Piece& e = w ? *dst++ : *src++;
+    const Piece* hit = e.at < written.end ? &written : w && e.at < read.end ? &read : nullptr;
+    if (hit)
+      return fail(DATTRI_E_INVALID_ARG, "tensors %lld and %lld overlap and one of them is written",
+                  (long long)hit->tensor, (long long)e.tensor);
+    Piece& reach = w ? written : read;
+    if (e.end > reach.end) reach = e;
+  }
+  return DATTRI_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -358,6 +482,8 @@ dattri_status dattri_clip_gradients(const void* const* grads, const int64_t* siz
       return fail(DATTRI_E_INVALID_ARG, "tensor %lld is scaled in place with another type", (long long)i);
   }
   TRY(check_workspace(workspace, ws_bytes, align_up(std::max<size_t>((size_t)n_partials * 8, kAlign))));
+  TRY(clip_apart(grads, sizes, dtypes, outs, out_dtypes, n_tensors, Span("norm_coef", norm_coef, 8),
+                 Span("workspace", workspace, n_partials * 8)));
   hipStream_t s = (hipStream_t)stream;
   double* partials = (double*)workspace;
   int64_t bytes = 0;

@@ -8,7 +8,9 @@ the rows that ``linear_input_grad`` returns are the blocks B that a
 kernels; nothing here is differentiated by autograd.
 
 Rows are the last axis: ``x [..., d]`` with unit stride along d and one stride
-between rows (a contiguous tensor, or a view of padded rows).  ``stream`` is a
+between rows (a contiguous tensor, or a view of padded rows).  An output may not
+share memory with what else the call reads or writes, except where a function
+says that it may be one of its inputs.  ``stream`` is a
 torch stream, a raw handle or None (the current one); outputs and workspaces
 are allocated on the stream that the call runs on.
 """
@@ -304,6 +306,7 @@ def gradient_norm(grads, stream=None):
 def clip_gradients(grads, max_norm, out=None, stream=None):
     """Scales the gradients so that their 2-norm together is at most max_norm,
     in place or into `out` (tensors of the same sizes, float32 or bfloat16).
+    No gradient may come twice (shared weights: once), nor overlap another.
     Returns (norm before, coefficient), float32 scalars on the GPU."""
     grads = list(grads)
     return _clip(grads, max_norm, grads if out is None else out, stream)

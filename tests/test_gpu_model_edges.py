@@ -24,3 +24,27 @@ def test_table_gradient_without_tokens(vocab, d, pad, dtype):
     assert (out == 7).all()
     layers().embedding_grad(g, t, vocab, out=out[:, :d])
     assert not out[:, :d].any() and (out[:, d:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_outputs_over_inputs_are_refused(dtype):
+    """An output in its own inputs raises and leaves them as they were; column ranges of one matrix are apart."""
+    from paper_2609_38767_amd import DattriError
+    m, g = layers(), gen(3)
+    buf = rand(g, 40, 3 * 64, dtype=dtype)
+    x, mid, w = buf[:, :64], buf[:, 64:128], rand(g, 64, 64, dtype=dtype)
+    was = buf.clone()
+    t = torch.arange(40, device="cuda") % 5
+    for bad in (lambda: m.linear(x, w, out=x), lambda: m.linear(x, w, out=buf[:, 32:96]),
+                lambda: m.linear_input_grad(x, w, out=x), lambda: m.embedding(x[:5], t, out=x),
+                lambda: m.linear(x, w, residual=mid, out=buf[:, 80:144]),
+                lambda: m.clip_gradients([buf.view(-1)[:100], buf.view(-1)[50:150]], 1.0),
+                lambda: m.clip_gradients([buf, buf], 1.0)):
+        with pytest.raises(DattriError, match="overlap"):
+            bad()
+    torch.cuda.synchronize()
+    assert torch.equal(buf, was)
+    want = m.linear(x.contiguous(), w, residual=mid.contiguous())
+    assert torch.equal(m.linear(x, w, residual=mid, out=buf[:, 128:]), want)
+    assert torch.equal(m.linear(x, w, residual=mid, out=mid), want) and torch.equal(x, was[:, :64])
+    assert m.gradient_norm([buf, buf]).item() > 0  # nothing is written
