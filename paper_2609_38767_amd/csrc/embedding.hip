@@ -126,7 +126,7 @@ __global__ __launch_bounds__(256) void embedding_kernel(const uint8_t* __restric
                                                         int token_bytes, int64_t units, int strips, float scale,
                                                         uint8_t* __restrict__ out, int64_t ld_out) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t u = (int64_t)blockIdx.x * 4 + wave;
+  const int64_t u = row_block() * 4 + wave;
   if (u >= units) return;
   const int64_t i = u / strips;
   const int base = (int)(u - i * strips) * kStrip;
@@ -144,12 +144,14 @@ hipError_t launch_embedding(int elt, const void* table, int64_t ld_table, int64_
                             int token_bytes, int64_t n, float scale, void* out, int64_t ld_out, hipStream_t s) {
   if (n <= 0) return hipSuccess;
   const int strips = (int)((d + kStrip - 1) / kStrip);
-  const int64_t units = n * strips, blocks = (units + 3) / 4;
-  if (blocks > INT32_MAX) return hipErrorInvalidValue;
+  const int64_t units = n * strips;
+  dim3 grid;
+  const hipError_t e = row_grid((units + 3) / 4, &grid);
+  if (e != hipSuccess) return e;
   const bool al = (uintptr_t)table % 16 == 0 && (uintptr_t)out % 16 == 0 && (ld_table * elt) % 16 == 0 &&
                   (ld_out * elt) % 16 == 0 && (d * elt) % 16 == 0;
   auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, s, (const uint8_t*)table, ld_table, vocab, (int)d,
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, (const uint8_t*)table, ld_table, vocab, (int)d,
                        tokens, token_bytes, units, strips, scale, (uint8_t*)out, ld_out);
     return hipGetLastError();
   };
@@ -415,10 +417,9 @@ __global__ __launch_bounds__(256) void embgrad_groups_kernel(const uint8_t* __re
                                                              const int* __restrict__ pos, int n_groups, uint32_t vocab,
                                                              float* __restrict__ part, int64_t ld_part, int strips) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t unit = (int64_t)blockIdx.x * 4 + wave;
-  const int j = (int)(unit / strips), base = (int)(unit - (int64_t)j * strips) * 256;
-  if (j >= n_groups) return;
-  const int a = j * kRun;
+  const int64_t unit = row_block() * 4 + wave, group = unit / strips;
+  if (group >= n_groups) return;
+  const int j = (int)group, base = (int)(unit - group * strips) * 256, a = j * kRun;
   const int at = pos[a + (lane & (kRun - 1))];
   const uint32_t v = key[a];
   if (v >= vocab || key[a + kRun - 1] != v) return;
@@ -441,7 +442,7 @@ __global__ __launch_bounds__(256) void embgrad_rows_kernel(const uint8_t* __rest
                                                            int64_t ld_out, int accumulate, int strips) {
   constexpr int F = 64 / E;  // rows in flight
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t unit = (int64_t)blockIdx.x * 4 + wave, first = unit / strips;
+  const int64_t unit = row_block() * 4 + wave, first = unit / strips;
   const int base = (int)(unit - first * strips) * (64 * E);
   if (first >= n) return;
   const int a = (int)first;
@@ -573,13 +574,15 @@ hipError_t launch_embedding_grad(int elt, const void* grad_out, int64_t ld_grad,
   auto go = [&](auto groups_kernel, auto wide_kernel, auto narrow_kernel) {
     const int row_cols = wide ? 16 : 4;
     const int64_t gs = (d + 255) / 256, rs = (d + 64 * row_cols - 1) / (64 * row_cols);
-    const int64_t gb = (n_groups * gs + 3) / 4, rb = (n * rs + 3) / 4;
-    if (gb > INT32_MAX || rb > INT32_MAX) return hipErrorInvalidValue;
+    dim3 gb, rb;
+    hipError_t e = row_grid((n * rs + 3) / 4, &rb);
+    if (e == hipSuccess && n_groups > 0) e = row_grid((n_groups * gs + 3) / 4, &gb);
+    if (e != hipSuccess) return e;
     if (n_groups > 0)
-      hipLaunchKernelGGL(groups_kernel, dim3((unsigned)gb), dim3(256), 0, s, (const uint8_t*)grad_out, ld_grad, (int)d,
+      hipLaunchKernelGGL(groups_kernel, gb, dim3(256), 0, s, (const uint8_t*)grad_out, ld_grad, (int)d,
                          key[cur], pos[cur], (int)n_groups, (uint32_t)vocab, part, ldp, (int)gs);
-    hipLaunchKernelGGL(wide ? wide_kernel : narrow_kernel, dim3((unsigned)rb), dim3(256), 0, s, (const uint8_t*)grad_out, ld_grad, (int)d,
-                       key[cur], pos[cur], (int)n, part, ldp, scale, (uint32_t)vocab, grad_table, ld_table,
+    hipLaunchKernelGGL(wide ? wide_kernel : narrow_kernel, rb, dim3(256), 0, s, (const uint8_t*)grad_out, ld_grad,
+                       (int)d, key[cur], pos[cur], (int)n, part, ldp, scale, (uint32_t)vocab, grad_table, ld_table,
                        (int)accumulate, (int)rs);
     return hipGetLastError();
   };

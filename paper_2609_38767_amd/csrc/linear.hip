@@ -225,9 +225,9 @@ __device__ inline void tile_of(int b, int nm, int nn, int* mt, int* nt) {
 
 }  // namespace
 
-// WM x WN waves; BM x BN blocks of 32 x 32 each.  Grid (tiles, splits of k):
-// split y runs stages [y * sps, min((y + 1) * sps, all)); with several splits
-// (OP kPartial) part holds them as [split][M][ld_part].
+// WM x WN waves; BM x BN blocks of 32 x 32 each.  Grid (tiles, splits of k,
+// more tiles): split y runs stages [y * sps, min((y + 1) * sps, all)); with
+// several splits (OP kPartial) part holds them as [split][M][ld_part].
 template <int OP, bool AC, bool BC, int ELT, int KW, int WM, int WN, int BM, int BN>
 __global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void gemm_kernel(GemmArgs a, int nm, int nn, int sps,
                                                                           float* __restrict__ part, int64_t ld_part) {
@@ -241,8 +241,10 @@ __global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void gemm_kernel(GemmAr
   __shared__ __align__(1024) uint8_t x0[kBuf], x1[kBuf], x2[kBuffers == 4 ? kBuf : 16], x3[kBuffers == 4 ? kBuf : 16];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WN, wn = wave % WN;
+  const int64_t tile = (int64_t)blockIdx.z * gridDim.x + blockIdx.x;
+  if (tile >= (int64_t)nm * nn) return;
   int mt, nt;
-  tile_of(blockIdx.x, nm, nn, &mt, &nt);
+  tile_of((int)tile, nm, nn, &mt, &nt);
   const int m0 = mt * TM, n0 = nt * TN;
   SA sa;
   SB sb;
@@ -455,7 +457,7 @@ struct Repack {
 template <int ELT>
 __global__ __launch_bounds__(256) void repack_kernel(Repack a, Repack b) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t at = (int64_t)blockIdx.x * 4 + wave;  // a wave per row
+  const int64_t at = row_block() * 4 + wave;  // a wave per row
   if (at >= a.rows + b.rows) return;
   const Repack& p = at < a.rows ? a : b;
   const int64_t r = at < a.rows ? at : at - a.rows;
@@ -661,7 +663,9 @@ Repack repack_of(const void** src, int64_t* ld, int64_t w, int64_t rows, int elt
 
 template <int OP, bool AC, bool BC, int ELT, int KW, int WM, int WN, int BM, int BN>
 hipError_t launch_tiles(const GemmArgs& a, const GemmShape& g, float* part, int64_t ldp, hipStream_t s) {
-  const dim3 grid((unsigned)(g.nm * g.nn), g.splits);
+  dim3 grid(1, g.splits);
+  const hipError_t e = row_grid(g.nm * g.nn, &grid, true);
+  if (e != hipSuccess) return e;
   if (g.splits > 1)
     hipLaunchKernelGGL((gemm_kernel<kPartial, AC, BC, ELT, KW, WM, WN, BM, BN>), grid, dim3(256), 0, s, a, (int)g.nm,
                        (int)g.nn, g.sps, part, ldp);
@@ -739,8 +743,10 @@ hipError_t launch_linear(dattri_linear_op op, int elt, bool aligned, GemmArgs a,
     if (L.pack_b) rb = repack_of(&a.B, &a.ldb, L.b_w, L.b_rows, elt, ws + L.off_b);
     const int64_t n = ra.rows + rb.rows;
     if (n > 0) {
-      hipLaunchKernelGGL(elt == 2 ? repack_kernel<2> : repack_kernel<4>, dim3((unsigned)((n + 3) / 4)), dim3(256), 0, s,
-                         ra, rb);
+      dim3 grid;
+      e = row_grid((n + 3) / 4, &grid);
+      if (e != hipSuccess) return e;
+      hipLaunchKernelGGL(elt == 2 ? repack_kernel<2> : repack_kernel<4>, grid, dim3(256), 0, s, ra, rb);
       e = hipGetLastError();
       if (e != hipSuccess) return e;
     }

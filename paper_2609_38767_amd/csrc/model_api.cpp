@@ -354,7 +354,7 @@ dattri_status dattri_linear_weight_grad(const void* G, int64_t ld_g, const void*
 namespace {
 
 // Walks the tensors in launches of at most kClipTensors of them and at most
-// 2^30 chunks; `visit(list, groups)` gets each (with src, dst, dtypes when given).
+// kClipMost chunks; `visit(list, groups)` gets each (with src, dst, dtypes when given).
 template <class F>
 dattri_status clip_launches(const void* const* grads, const int64_t* sizes, const dattri_dtype* dtypes,
                             void* const* outs, const dattri_dtype* out_dtypes, int64_t n_tensors, F visit) {
@@ -370,7 +370,7 @@ dattri_status clip_launches(const void* const* grads, const int64_t* sizes, cons
   for (int64_t i = 0; i < n_tensors; ++i) {
     const int64_t chunks = (sizes[i] + kClipChunk - 1) / kClipChunk;
     if (chunks == 0) continue;
-    if (l.n == kClipTensors || (l.n > 0 && l.first[l.n] + chunks > (1 << 30))) TRY(flush());
+    if (l.n == kClipTensors || (l.n > 0 && l.first[l.n] + chunks > kClipMost)) TRY(flush());
     ClipTensor& t = l.t[l.n];
     t.src = grads ? grads[i] : nullptr;
     t.dst = outs ? outs[i] : nullptr;
@@ -389,7 +389,7 @@ dattri_status clip_sizes(const int64_t* sizes, int64_t n_tensors, int64_t* parti
   if (n_tensors > 0 && !sizes) return fail(DATTRI_E_INVALID_ARG, "sizes is NULL");
   for (int64_t i = 0; i < n_tensors; ++i) {
     if (sizes[i] < 0) return fail(DATTRI_E_INVALID_ARG, "size of tensor %lld is negative", (long long)i);
-    if (sizes[i] > (int64_t)kClipChunk << 30)
+    if (sizes[i] > (int64_t)kClipChunk * kClipMost)
       return fail(DATTRI_E_UNSUPPORTED, "tensor %lld has too many elements", (long long)i);
   }
   int64_t n = 0;
