@@ -11,8 +11,8 @@ Rows are the last axis: ``x [..., d]`` with unit stride along d and one stride
 between rows (a contiguous tensor, or a view of padded rows).  An output may not
 share memory with what else the call reads or writes, except where a function
 says that it may be one of its inputs.  ``stream`` is a
-torch stream, a raw handle or None (the current one); outputs and workspaces
-are allocated on the stream that the call runs on.
+torch stream or a raw handle of the tensors' GPU, or None (its current one);
+outputs and workspaces are allocated on the stream that the call runs on.
 """
 from array import array
 from operator import attrgetter
@@ -42,6 +42,8 @@ def _elsewhere(t, stream):
     if isinstance(stream, int):
         with dev:  # handle 0 is the default stream, which has an object of its own
             stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+    elif stream.device != t.device:
+        raise ValueError(f"stream is on {stream.device}, the tensors on {t.device}")
     return torch.cuda.stream(stream)
 
 

@@ -141,3 +141,15 @@ for kw in (dict(out=P + 1020), dict(out=2 * P), dict(w=P), dict(w=3 * P), dict(t
 def test_outputs_apart_from_everything_else():
     """Every output of the linear layers against every other buffer; the aliases that the header allows go on."""
     child("\n".join(LINEAR.splitlines()))
+
+
+def test_stream_of_another_gpu_is_refused():
+    """A call runs on the stream it was given or raises: it does not fall back to the current one."""
+    from types import SimpleNamespace
+
+    import torch
+
+    from paper_2609_38767_amd import layers
+    at = [SimpleNamespace(device=torch.device("cuda", k)) for k in range(2)]
+    with pytest.raises(ValueError, match="stream is on cuda:1, the tensors on cuda:0"):
+        layers._elsewhere(at[0], at[1])
