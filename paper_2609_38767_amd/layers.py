@@ -5,7 +5,12 @@
 step of an attributed model: the inputs given to ``linear`` are the blocks A and
 the rows that ``linear_input_grad`` returns are the blocks B that a
 ``ProjectionSession`` captures.  All computation happens in libdattri's HIP
-kernels; nothing here is differentiated by autograd.
+kernels.
+
+Nothing here is differentiated by autograd: results do not require grad whatever
+the inputs do, and the backward products are calls of their own.  Writing into a
+tensor counts as a change of it, so that autograd refuses to use what it has
+saved of it.
 
 Rows are the last axis: ``x [..., d]`` with unit stride along d and one stride
 between rows (a contiguous tensor, or a view of padded rows).  An output may not
@@ -123,6 +128,13 @@ def _on_16(t, ld):
     return t.data_ptr() % 16 == 0 and ld * e % 16 == 0
 
 
+def _changed(out):
+    """The kernels write behind torch's back: tells autograd that what the
+    caller handed in (a tensor, a list of them or None) has changed."""
+    if out is not None:
+        torch.autograd.graph.increment_version(out)
+
+
 def _workspace(n, device):
     return torch.empty(n, dtype=torch.uint8, device=device) if n else None
 
@@ -138,10 +150,12 @@ def embedding(table, tokens, scale=1.0, out=None, stream=None):
     code = _code(table, "table")
     tokens = _tokens(tokens)
     vocab, d, ld = _matrix(table, "table", table.dtype)
+    given = out
     if out is None:
         out = torch.empty((*tokens.shape, d), dtype=table.dtype, device=table.device)
     n, _, ld_out = _rows(out, "out", table.dtype, (*tokens.shape, d))
     dattri_embedding(table, ld, vocab, d, code, tokens, tokens.element_size(), tokens.numel(), scale, out, ld_out)
+    _changed(given)
     return out
 
 
@@ -158,6 +172,7 @@ def embedding_grad(grad_out, tokens, vocab, scale=1.0, out=None, accumulate=Fals
     if grad_out.shape[:-1] != tokens.shape:
         raise ValueError(f"grad_out is {tuple(grad_out.shape)} for tokens of {tuple(tokens.shape)}")
     _, d, ld = _rows(grad_out, "grad_out")
+    given = out
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs out")
@@ -167,6 +182,7 @@ def embedding_grad(grad_out, tokens, vocab, scale=1.0, out=None, accumulate=Fals
     ws_bytes = dattri_embedding_grad_workspace_bytes(n, vocab, d)
     dattri_embedding_grad(grad_out, ld, code, tokens, tokens.element_size(), n, scale, vocab, d, out, ld_out,
                           accumulate, _workspace(ws_bytes, out.device), ws_bytes)
+    _changed(given)
     return out
 
 
@@ -185,6 +201,7 @@ def linear(x, weight, bias=None, act="none", residual=None, keep_preact=False, o
     if bias is not None:
         _vector(bias, "bias", d_out, dt)
     ld_r = _rows(residual, "residual", dt, shape)[2] if residual is not None else 0
+    given = out
     if out is None:
         out = torch.empty(shape, dtype=dt, device=x.device)
     ld_y = _rows(out, "out", dt, shape)[2]
@@ -193,6 +210,7 @@ def linear(x, weight, bias=None, act="none", residual=None, keep_preact=False, o
                                              _on_16(x, ld_x) and _on_16(weight, ld_w))
     dattri_linear(x, ld_x, weight, ld_w, bias, _act(act), residual, ld_r, out, ld_y, z, 0, n, d_in, d_out, code,
                   _workspace(ws_bytes, x.device), ws_bytes)
+    _changed(given)
     return (out, z) if keep_preact else out
 
 
@@ -218,6 +236,7 @@ def linear_input_grad(g, weight, residual=None, act="none", preact=None, both=Fa
         raise ValueError(f"act={act!r} needs preact")
     ld_r = _rows(residual, "residual", dt, shape)[2] if residual is not None else 0
     ld_z = _rows(preact, "preact", dt, shape)[2] if preact is not None else 0
+    given = out
     if out is None:
         out = torch.empty(shape, dtype=dt, device=g.device)
     ld_p = _rows(out, "out", dt, shape)[2]
@@ -226,6 +245,7 @@ def linear_input_grad(g, weight, residual=None, act="none", preact=None, both=Fa
                                              _on_16(g, ld_g) and _on_16(weight, ld_w))
     dattri_linear_input_grad(g, ld_g, weight, ld_w, residual, ld_r, a, preact, ld_z, d, 0, out, ld_p, n, d_in, d_out,
                              code, _workspace(ws_bytes, g.device), ws_bytes)
+    _changed(given)
     return (d, out) if both else out
 
 
@@ -245,6 +265,7 @@ def linear_weight_grad(g, x, bias=False, out=None, out_bias=None, accumulate=Fal
     _, d_in, ld_x = _rows(x, "x", g.dtype)
     if accumulate and (out is None or (bias and out_bias is None)):
         raise ValueError("accumulate needs out (and out_bias)")
+    given = [t for t in (out, out_bias if bias else None) if t is not None]
     if out is None:
         out = torch.empty((d_out, d_in), dtype=torch.float32, device=g.device)
     ld_dw = _matrix(out, "out", torch.float32, shape=(d_out, d_in))[2]
@@ -256,6 +277,7 @@ def linear_weight_grad(g, x, bias=False, out=None, out_bias=None, accumulate=Fal
                                              _on_16(g, ld_g) and _on_16(x, ld_x))
     dattri_linear_weight_grad(g, ld_g, x, ld_x, out, ld_dw, out_bias if bias else None, accumulate, n, d_in, d_out,
                               code, _workspace(ws_bytes, g.device), ws_bytes)
+    _changed(given)
     return (out, out_bias) if bias else out
 
 
@@ -289,7 +311,8 @@ def _clip(grads, max_norm, out, stream):
     if out is grads:
         dst, otypes = src, types
     elif out is not None:
-        dst, osizes, otypes = _host_list(list(out), "out", device)
+        out = list(out)
+        dst, osizes, otypes = _host_list(out, "out", device)
         if osizes != sizes:
             raise ValueError("out must have the gradients' sizes")
     norm_coef = torch.empty(2, dtype=torch.float32, device=grads[0].device)
@@ -297,6 +320,7 @@ def _clip(grads, max_norm, out, stream):
     ws_bytes = dattri_clip_workspace_bytes(sizes, n)
     dattri_clip_gradients(src, sizes, types, dst, otypes, n, max_norm, norm_coef,
                           _workspace(ws_bytes, norm_coef.device), ws_bytes)
+    _changed(out)
     return norm_coef[0], norm_coef[1]
 
 

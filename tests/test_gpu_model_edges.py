@@ -48,3 +48,45 @@ def test_outputs_over_inputs_are_refused(dtype):
     assert torch.equal(m.linear(x, w, residual=mid, out=buf[:, 128:]), want)
     assert torch.equal(m.linear(x, w, residual=mid, out=mid), want) and torch.equal(x, was[:, :64])
     assert m.gradient_norm([buf, buf]).item() > 0  # nothing is written
+
+
+def test_autograd_sees_the_writes():
+    """What autograd has saved and a call writes into is refused by the backward pass, not used as it is then."""
+    m, g = layers(), gen(9)
+    x, w, t = rand(g, 6, 8), rand(g, 8, 8), torch.arange(6, device="cuda")
+    vec = rand(g, 8)
+
+    def saved(shape):
+        s = torch.ones(shape, device="cuda")
+        p = torch.ones(shape, device="cuda", requires_grad=True)
+        return s, (p * s).sum()  # autograd keeps s for p's gradient
+
+    for shapes, call in (([(6, 8)], lambda a: m.embedding(w, t, out=a)),
+                         ([(8, 8)], lambda a: m.embedding_grad(x, t, 8, out=a)),
+                         ([(6, 8)], lambda a: m.linear(x, w, out=a)),
+                         ([(6, 8)], lambda a: m.linear(x, w, residual=a, out=a)),
+                         ([(6, 8)], lambda a: m.linear_input_grad(x, w, out=a)),
+                         ([(8, 8)], lambda a: m.linear_weight_grad(x, x, out=a)),
+                         ([(8, 8), (8,)], lambda a, b: m.linear_weight_grad(x, x, bias=True, out=a, out_bias=b)),
+                         ([(5,), (3, 7)], lambda a, b: m.clip_gradients([a, b], 0.5)),
+                         ([(8,)], lambda a: m.clip_gradients([vec], 0.5, out=[a]))):
+        both = [saved(s) for s in shapes]
+        call(*(s for s, _ in both))
+        for _, loss in both:
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                loss.backward()
+    s, loss = saved((4,))
+    m.gradient_norm([s])  # reads only
+    loss.backward()
+
+
+def test_results_do_not_require_grad():
+    """Inputs that require grad are taken as they are."""
+    m, g = layers(), gen(10)
+    x, w = rand(g, 6, 8).requires_grad_(), rand(g, 8, 8).requires_grad_()
+    assert torch.equal(m.linear(x, w), m.linear(x.detach(), w.detach()))
+    assert not m.linear(x, w).requires_grad and not m.linear_weight_grad(x, x).requires_grad
+    with torch.inference_mode():  # tensors without a version counter
+        out = torch.empty(6, 8, device="cuda")
+        m.linear(x, w, out=out)
+        m.clip_gradients([out], 0.5)
