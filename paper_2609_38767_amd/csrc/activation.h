@@ -5,10 +5,11 @@
 // u = sqrt(2/pi) (z + 0.044715 z^3), since (1 + tanh u) / 2 = s(2u);
 // silu(z) = z s(z).  ELT 2 (bf16 results) takes the hardware's exp2 and
 // reciprocal, off by a few 2^-23 (exp2 below 2^-126 is zero), and for Phi(-z) =
-// exp(-z^2 / 2) t P(t), t = 1 / (1 + q z), z >= 0, the P of degree 5 (and q) whose
-// largest relative error over 0 <= z <= 13.5 is least: 3.8e-6, in float32 with
-// its exp 8.9e-6 = 2^-16.8 at most, so the tail keeps what bf16 can hold (a P of
-// least absolute error was off by 0.4% at -6 and 3% at -12).  8192 x 14336
+// exp(-z^2 / 2) t P(t), t = 1 / (1 + q z), z >= 0, the P of degree 6 (and q) whose
+// largest relative error over 0 <= z <= 13.5 is least: 6.2e-7, in float32 with
+// its exp 8.1e-6 = 2^-16.9 at most and nowhere 7 2^-24 of 1, so the tail keeps
+// what bf16 can hold (a P of least absolute error was off by 0.4% at -6 and 3%
+// at -12).  8192 x 14336
 // outputs: erfcf took 207 us beside the product.  ELT 4 takes the library
 // functions and a division.
 // s is formed from exp(-|x|), which cannot overflow; a factor that has reached
@@ -46,12 +47,13 @@ template <int ELT>
 __device__ inline float normal_cdf(float z, float* e) {
   *e = exp_of<ELT>(-0.5f * z * z);
   if constexpr (ELT == 4) return 0.5f * erfcf(-z * kSqrtHalf);
-  const float t = __builtin_amdgcn_rcpf(fmaf(0.3075f, fabsf(z), 1.f));
-  float p = fmaf(t, -0.07584723f, 0.19207588f);
-  p = fmaf(t, p, 0.0049362374f);
-  p = fmaf(t, p, 0.13743412f);
-  p = fmaf(t, p, 0.11845802f);
-  p = fmaf(t, p, 0.12294149f);
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.265f, fabsf(z), 1.f));
+  float p = fmaf(t, -0.067787044f, 0.19527316f);
+  p = fmaf(t, p, -0.06636296f);
+  p = fmaf(t, p, 0.14249335f);
+  p = fmaf(t, p, 0.08294658f);
+  p = fmaf(t, p, 0.107836775f);
+  p = fmaf(t, p, 0.10559983f);
   const float tail = t * p * *e;  // Phi(-|z|)
   return z < 0.f ? tail : 1.f - tail;
 }
