@@ -31,11 +31,11 @@
 // rows, so that the epilogue is one short loop over whole rows: its loads and
 // stores of Z, R and the outputs are contiguous per wave.
 //
-// What bounds it: 8192 x 4096 -> 14336 bf16, medians of five: forward 780 us
-// (1230 TFLOP/s; the vendor library 665), input gradient 735 (1310; 734), weight
-// gradient 776 (1240; 979).  The matrix cores are 70, 73 and 67% busy, at a
+// What bounds it: 8192 x 4096 -> 14336 bf16, medians of five: forward 774 us
+// (1240 TFLOP/s; the vendor library 654), input gradient 735 (1310; 726), weight
+// gradient 764 (1260; 971).  The matrix cores are 70, 73 and 67% busy, at a
 // clock that the load holds at 1.7 GHz.  The weight gradient's 896 tiles are 3.5 rounds
-// of 256 CUs.  Float32, 4096 cubed: 144-150 TFLOP/s (the library 148-150).
+// of 256 CUs.  Float32, 4096 cubed: 145-151 TFLOP/s (the library 147-150).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>

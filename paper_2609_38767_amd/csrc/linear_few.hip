@@ -9,7 +9,7 @@
 // are read element by element, 64 neighbours at a time.
 //
 // What bounds it: HBM.  4096 -> 14336 bf16 (117 MB of weights, not cached): one
-// row 22.1 us (5.3 TB/s), four rows 26.6; five rows, by the tile kernel, 30.9.
+// row 22.3 us (5.3 TB/s), four rows 26.6; five rows, by the tile kernel, 31.2.
 #include "device_common.h"
 #include "epilogue.h"
 #include "model_ops.h"

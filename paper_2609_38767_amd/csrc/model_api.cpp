@@ -15,7 +15,7 @@ using namespace dattri;
 namespace {
 
 constexpr int64_t kClipStream = (int64_t)256 << 20;  // bytes (gradients and other buffers written) that no cache holds
-constexpr int64_t kMaxWidth = (int64_t)1 << 23;  // columns of a row: 256 of them stay below 4 GiB in any type
+constexpr int64_t kMaxWidth = (int64_t)1 << 23;  // columns of a row (check_rows holds 256 rows below 4 GiB)
 
 dattri_status elt_of(dattri_dtype dtype, int* elt) {
   if (dtype != DATTRI_F32 && dtype != DATTRI_BF16)

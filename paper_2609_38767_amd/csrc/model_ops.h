@@ -89,7 +89,7 @@ struct ClipList {
   int first[kClipTensors + 1];  // first chunk of each tensor, then the number of chunks
 };
 static_assert(sizeof(ClipList) <= 3840, "kernel argument size");
-// stream: loads and stores past the caches
+// stream: loads past the caches
 hipError_t launch_clip_squares(const ClipList& l, int groups, double* partials, bool stream, hipStream_t s);
 hipError_t launch_clip_norm(const double* partials, int n_partials, float max_norm, float* norm_coef, hipStream_t s);
 hipError_t launch_clip_scale(const ClipList& l, const float* norm_coef, bool stream, hipStream_t s);

@@ -17,7 +17,9 @@ between rows (a contiguous tensor, or a view of padded rows).  An output may not
 share memory with what else the call reads or writes, except where a function
 says that it may be one of its inputs.  ``stream`` is a
 torch stream or a raw handle of the tensors' GPU, or None (its current one);
-outputs and workspaces are allocated on the stream that the call runs on.
+outputs and workspaces are allocated on the stream that the call runs on.  As
+with torch's own streams it has to wait for what made the inputs, and they have
+to live until it has read them.
 """
 from array import array
 from operator import attrgetter
