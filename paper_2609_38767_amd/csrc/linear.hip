@@ -599,7 +599,7 @@ Repack repack_of(const void** src, int64_t* ld, int64_t w, int64_t rows, int elt
 template <int OP, bool AC, bool BC, int ELT, int KW, int WM, int WN, int BM, int BN>
 hipError_t launch_tiles(const GemmArgs& a, const GemmShape& g, float* part, int64_t ldp, hipStream_t s) {
   dim3 grid(1, g.splits);
-  const hipError_t e = row_grid(g.nm * g.nn, &grid, true);
+  const hipError_t e = row_grid(g.nm * g.nn, &grid, 256, true);
   if (e != hipSuccess) return e;
   if (g.splits > 1)
     hipLaunchKernelGGL((gemm_kernel<kPartial, AC, BC, ELT, KW, WM, WN, BM, BN>), grid, dim3(256), 0, s, a, (int)g.nm,

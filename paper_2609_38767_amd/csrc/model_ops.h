@@ -7,22 +7,9 @@
 #include <stdint.h>
 
 #include "dattri.h"
+#include "row_grid.h"
 
 namespace dattri {
-
-// A grid of n workgroups of 256 in a row, whatever n: the threads along one
-// dimension have to fit 32 bits (a launch of more runs their number modulo 2^32
-// and reports nothing), so long rows go on along y, or z.  Kernels find their
-// place by row_block and return past n.
-constexpr int64_t kRowBlocks = (int64_t)1 << 23;
-inline hipError_t row_grid(int64_t n, dim3* grid, bool along_z = false) {
-  if (n < 1 || n > kRowBlocks * 65535) return hipErrorInvalidValue;
-  const int64_t x = n < kRowBlocks ? n : kRowBlocks;
-  grid->x = (unsigned)x;
-  (along_z ? grid->z : grid->y) = (unsigned)((n + x - 1) / x);
-  return hipSuccess;
-}
-__device__ inline int64_t row_block() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
 
 // ------------------------------------------------------------- embedding
 hipError_t launch_embedding(int elt, const void* table, int64_t ld_table, int64_t vocab, int64_t d, const void* tokens,

@@ -17,6 +17,7 @@
 // its partial tile, and the splits are summed in split order.
 #include "device_common.h"
 #include "internal.h"
+#include "row_grid.h"
 
 namespace dattri {
 using namespace dev;
@@ -325,7 +326,7 @@ __global__ __launch_bounds__(256) void row_inv_norms_kernel(const uint8_t* __res
                                                             float* __restrict__ inv) {
   constexpr int EPL = 16 / ELT;
   const int lane = threadIdx.x & 63;
-  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t r = row_block() * 4 + (threadIdx.x >> 6);
   if (r >= rows) return;  // the whole wave leaves; no barrier below
   const uint8_t* row = X + r * ld * ELT;
   float s = 0.f;
@@ -424,9 +425,10 @@ static hipError_t launch_norms(const uint8_t* X, int64_t ld, int64_t rows, int64
   } else if (rows <= 2048 && bytes > 4096) {
     hipLaunchKernelGGL((row_inv_norms_wide_kernel<ELT, 4>), dim3((unsigned)rows), dim3(256), 0, s, X, ld, F, d, inv);
   } else {
-    const int64_t b = (rows + 3) / 4;
-    if (b > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(row_inv_norms_kernel<ELT>, dim3((unsigned)b), dim3(256), 0, s, X, ld, rows, F, d, inv);
+    dim3 grid;
+    const hipError_t e = row_grid((rows + 3) / 4, &grid);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(row_inv_norms_kernel<ELT>, grid, dim3(256), 0, s, X, ld, rows, F, d, inv);
   }
   return hipGetLastError();
 }

@@ -26,6 +26,7 @@
 
 #include "device_common.h"
 #include "internal.h"
+#include "row_grid.h"
 
 namespace dattri {
 using namespace dev;
@@ -69,7 +70,7 @@ __device__ inline void sort_candidates(uint32_t* ck, int32_t* ci, int P) {
   }
 }
 
-__global__ __launch_bounds__(kTopkThreads) void topk_kernel(const float* __restrict__ S,
+__global__ __launch_bounds__(kTopkThreads) void topk_kernel(const float* __restrict__ S, int64_t n_q,
                                                             int64_t n_train, int k,
                                                             int32_t* __restrict__ idx_out,
                                                             float* __restrict__ val_out) {
@@ -82,7 +83,8 @@ __global__ __launch_bounds__(kTopkThreads) void topk_kernel(const float* __restr
   __shared__ uint32_t s_bin, s_cand, s_rem, s_gt;
 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t q = blockIdx.x;
+  const int64_t q = row_block();
+  if (q >= n_q) return;
   const float* row = S + q * n_train;
   const int n = (int)n_train;
   const bool vec = ((uintptr_t)row & 15) == 0;  // uniform over the workgroup
@@ -316,8 +318,10 @@ hipError_t launch_topk(const float* S, int64_t n_q, int64_t n_train, int32_t k, 
                        float* val, hipStream_t s) {
   if (n_q <= 0 || k <= 0) return hipSuccess;
   if (k > kTopkMax || k > n_train || n_q > INT32_MAX) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(topk_kernel, dim3((unsigned)n_q), dim3(kTopkThreads), 0, s, S, n_train, k, idx,
-                     val);
+  dim3 grid;
+  const hipError_t e = row_grid(n_q, &grid, kTopkThreads);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(topk_kernel, grid, dim3(kTopkThreads), 0, s, S, n_q, n_train, k, idx, val);
   return hipGetLastError();
 }
 
