@@ -41,6 +41,10 @@ __all__ = [
     "DATTRI_ACT_NONE", "DATTRI_ACT_RELU", "DATTRI_ACT_GELU", "DATTRI_ACT_GELU_TANH", "DATTRI_ACT_SILU",
     "DATTRI_LINEAR_FORWARD", "DATTRI_LINEAR_INPUT_GRAD", "DATTRI_LINEAR_WEIGHT_GRAD",
     "dattri_linear_workspace_bytes", "dattri_linear", "dattri_linear_input_grad", "dattri_linear_weight_grad",
+    "dattri_rms_norm", "dattri_rms_norm_grad_workspace_bytes", "dattri_rms_norm_grad",
+    "dattri_quantize_rows", "dattri_quantize_weight", "dattri_linear_scaled_workspace_bytes", "dattri_linear_scaled",
+    "dattri_expert_linear_workspace_bytes", "dattri_expert_linear", "dattri_expert_linear_input_grad",
+    "dattri_expert_linear_weight_grad",
     "dattri_clip_workspace_bytes", "dattri_clip_gradients",
     "dattri_probe_read", "dattri_probe_mfma",
 ]
@@ -156,6 +160,23 @@ _SIGS = {
                                         _i64, _i64, _i32, _vp, _sz, _vp]),
     "dattri_linear_weight_grad": (_i32, [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _i32, _i64, _i64, _i64, _i32, _vp, _sz,
                                          _vp]),
+    "dattri_rms_norm": (_i32, [_vp, _i64, _vp, _i64, _vp, _flt, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i64, _i64,
+                               _i32, _vp]),
+    "dattri_rms_norm_grad_workspace_bytes": (_i32, [_i64, _i64, _i32, _i32, _P(_sz)]),
+    "dattri_rms_norm_grad": (_i32, [_vp, _i64, _vp, _i64, _vp, _flt, _vp, _i64, _vp, _i64, _vp, _i32, _i64, _i64, _i32,
+                                    _vp, _sz, _vp]),
+    "dattri_quantize_rows": (_i32, [_vp, _i64, _i64, _i64, _i32, _vp, _i64, _vp, _i64, _vp]),
+    "dattri_quantize_weight": (_i32, [_vp, _i64, _i64, _i64, _i32, _vp, _i64, _vp, _i64, _vp]),
+    "dattri_linear_scaled_workspace_bytes": (_i32, [_i64, _i64, _i64, _i32, _i32, _P(_sz)]),
+    "dattri_linear_scaled": (_i32, [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i32, _vp, _i64, _vp, _i64, _vp,
+                                  _i64, _i64, _i64, _i64, _i32, _vp, _sz, _vp]),
+    "dattri_expert_linear_workspace_bytes": (_i32, [_i32, _i64, _i64, _i64, _i64, _i32, _i32, _P(_sz)]),
+    "dattri_expert_linear": (_i32, [_vp, _i64, _vp, _i64, _vp, _vp, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _i64,
+                                    _i64, _i64, _i64, _i32, _vp, _sz, _vp]),
+    "dattri_expert_linear_input_grad": (_i32, [_vp, _i64, _vp, _i64, _vp, _i32, _vp, _i64, _i32, _vp, _i64, _vp, _i64,
+                                               _vp, _i64, _i64, _i64, _i64, _i64, _i32, _vp, _sz, _vp]),
+    "dattri_expert_linear_weight_grad": (_i32, [_vp, _i64, _vp, _i64, _vp, _i32, _vp, _i64, _vp, _i32, _i64, _i64,
+                                                _i64, _i64, _i32, _vp, _sz, _vp]),
     "dattri_clip_workspace_bytes": (_i32, [_vp, _i64, _P(_sz)]),
     "dattri_clip_gradients": (_i32, [_vp, _vp, _vp, _vp, _vp, _i64, _flt, _vp, _vp, _sz, _vp]),
     "dattri_probe_read": (_i32, [_vp, _sz, _vp, _i32, _vp]),
@@ -623,6 +644,79 @@ def dattri_linear_weight_grad(G, ld_g, X, ld_x, dW, ld_dw, dbias, accumulate, ro
     _check(load().dattri_linear_weight_grad(_ptr(G), ld_g, _ptr(X), ld_x, _ptr(dW), ld_dw, _ptr(dbias),
                                             int(bool(accumulate)), rows, d_in, d_out, dtype, _ptr(workspace), ws_bytes,
                                             _stream(stream)), "dattri_linear_weight_grad")
+
+
+def dattri_rms_norm(X, ld_x, R, ld_r, W, eps, Y, ld_y, H, ld_h, Q, ld_q, S, ld_s, rows, d, dtype, stream=None):
+    _check(load().dattri_rms_norm(_ptr(X), ld_x, _ptr(R), ld_r, _ptr(W), eps, _ptr(Y), ld_y, _ptr(H), ld_h, _ptr(Q),
+                                  ld_q, _ptr(S), ld_s, rows, d, dtype, _stream(stream)), "dattri_rms_norm")
+
+
+def dattri_rms_norm_grad_workspace_bytes(rows, d, dtype, weight=True):
+    v = _sz()
+    _check(load().dattri_rms_norm_grad_workspace_bytes(rows, d, dtype, int(bool(weight)), ctypes.byref(v)),
+           "dattri_rms_norm_grad_workspace_bytes")
+    return v.value
+
+
+def dattri_rms_norm_grad(G, ld_g, H, ld_h, W, eps, P, ld_p, D, ld_d, dW, accumulate, rows, d, dtype, workspace,
+                         ws_bytes, stream=None):
+    _check(load().dattri_rms_norm_grad(_ptr(G), ld_g, _ptr(H), ld_h, _ptr(W), eps, _ptr(P), ld_p, _ptr(D), ld_d,
+                                       _ptr(dW), int(bool(accumulate)), rows, d, dtype, _ptr(workspace), ws_bytes,
+                                       _stream(stream)), "dattri_rms_norm_grad")
+
+
+def dattri_quantize_rows(X, ld_x, rows, d, dtype, Q, ld_q, S, ld_s, stream=None):
+    _check(load().dattri_quantize_rows(_ptr(X), ld_x, rows, d, dtype, _ptr(Q), ld_q, _ptr(S), ld_s, _stream(stream)),
+           "dattri_quantize_rows")
+
+
+def dattri_quantize_weight(W, ld_w, d_out, d_in, dtype, Q, ld_q, S, ld_s, stream=None):
+    _check(load().dattri_quantize_weight(_ptr(W), ld_w, d_out, d_in, dtype, _ptr(Q), ld_q, _ptr(S), ld_s,
+                                         _stream(stream)), "dattri_quantize_weight")
+
+
+def dattri_linear_scaled_workspace_bytes(rows, d_in, d_out, dtype, aligned=False):
+    v = _sz()
+    _check(load().dattri_linear_scaled_workspace_bytes(rows, d_in, d_out, dtype, int(bool(aligned)), ctypes.byref(v)),
+           "dattri_linear_scaled_workspace_bytes")
+    return v.value
+
+
+def dattri_linear_scaled(X, ld_x, SX, ld_sx, W, ld_w, SW, ld_sw, bias, act, R, ld_r, Y, ld_y, Z, ld_z, rows, d_in, d_out,
+                       dtype, workspace, ws_bytes, stream=None):
+    _check(load().dattri_linear_scaled(_ptr(X), ld_x, _ptr(SX), ld_sx, _ptr(W), ld_w, _ptr(SW), ld_sw, _ptr(bias), act,
+                                     _ptr(R), ld_r, _ptr(Y), ld_y, _ptr(Z), ld_z, rows, d_in, d_out, dtype,
+                                     _ptr(workspace), ws_bytes, _stream(stream)), "dattri_linear_scaled")
+
+
+def dattri_expert_linear_workspace_bytes(op, rows, experts, d_in, d_out, dtype, aligned=False):
+    v = _sz()
+    _check(load().dattri_expert_linear_workspace_bytes(op, rows, experts, d_in, d_out, dtype, int(bool(aligned)),
+                                                       ctypes.byref(v)), "dattri_expert_linear_workspace_bytes")
+    return v.value
+
+
+def dattri_expert_linear(X, ld_x, W, ld_w, bias, offsets, offset_bytes, act, R, ld_r, Y, ld_y, Z, ld_z, rows, experts,
+                         d_in, d_out, dtype, workspace, ws_bytes, stream=None):
+    _check(load().dattri_expert_linear(_ptr(X), ld_x, _ptr(W), ld_w, _ptr(bias), _ptr(offsets), offset_bytes, act,
+                                       _ptr(R), ld_r, _ptr(Y), ld_y, _ptr(Z), ld_z, rows, experts, d_in, d_out, dtype,
+                                       _ptr(workspace), ws_bytes, _stream(stream)), "dattri_expert_linear")
+
+
+def dattri_expert_linear_input_grad(G, ld_g, W, ld_w, offsets, offset_bytes, R, ld_r, act, Z, ld_z, D, ld_d, P, ld_p,
+                                    rows, experts, d_in, d_out, dtype, workspace, ws_bytes, stream=None):
+    _check(load().dattri_expert_linear_input_grad(_ptr(G), ld_g, _ptr(W), ld_w, _ptr(offsets), offset_bytes, _ptr(R),
+                                                  ld_r, act, _ptr(Z), ld_z, _ptr(D), ld_d, _ptr(P), ld_p, rows, experts,
+                                                  d_in, d_out, dtype, _ptr(workspace), ws_bytes, _stream(stream)),
+           "dattri_expert_linear_input_grad")
+
+
+def dattri_expert_linear_weight_grad(G, ld_g, X, ld_x, offsets, offset_bytes, dW, ld_dw, dbias, accumulate, rows,
+                                     experts, d_in, d_out, dtype, workspace, ws_bytes, stream=None):
+    _check(load().dattri_expert_linear_weight_grad(_ptr(G), ld_g, _ptr(X), ld_x, _ptr(offsets), offset_bytes, _ptr(dW),
+                                                   ld_dw, _ptr(dbias), int(bool(accumulate)), rows, experts, d_in,
+                                                   d_out, dtype, _ptr(workspace), ws_bytes, _stream(stream)),
+           "dattri_expert_linear_weight_grad")
 
 
 def dattri_clip_workspace_bytes(sizes, n_tensors):

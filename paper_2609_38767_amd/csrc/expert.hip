@@ -1,0 +1,298 @@
+// Linear layers of experts and their backward products: rows sorted by expert,
+// any number of rows for each, the boundaries on the GPU.
+//   forward      Z[t] = X[t] W_e^T + b_e     input gradient   D[t] = G[t] W_e + R[t]
+//   weight gradient   dW_e = sum_t G[t]^T X[t]     t in [offsets[e], offsets[e + 1])
+//
+// The tiles are those of the linear layers (linear_tile.h).  Nothing of the
+// boundaries is known on the host, so a product over rows is launched with as
+// many tiles as any boundaries can need; every wave adds up the segments' tiles
+// and finds its own.  Rows in front of the first boundary and behind the last
+// one are segments too, whose products have no k: they come out as those of an
+// expert with zero weights and bias.  Boundaries are clamped to the rows and to
+// each other, so wrong ones give wrong rows, never an access out of range.
+#include <algorithm>
+#include <cmath>
+
+#include "api_common.h"
+#include "device_common.h"
+#include "epilogue.h"
+#include "internal.h"
+#include "linear_shape.h"
+#include "linear_tile.h"
+#include "model_ops.h"
+
+namespace dattri {
+using namespace dev;
+using namespace tile;
+
+namespace {
+
+__device__ inline int boundary(const ExpertArgs& x, int i) {
+  const int64_t v = x.offset_bytes == 8 ? ((const int64_t*)x.offsets)[i] : ((const int32_t*)x.offsets)[i];
+  return (int)min(max(v, (int64_t)0), (int64_t)x.rows);
+}
+
+// Segment s of experts + 2: the rows in front, the experts' and the rows behind.
+struct Segment {
+  int begin, end;
+};
+__device__ inline Segment segment(const ExpertArgs& x, int s) {
+  const int begin = s == 0 ? 0 : boundary(x, s - 1);
+  return Segment{begin, max(begin, s > x.experts ? x.rows : boundary(x, s))};
+}
+
+// Tile row `at` of all segments' tile rows of TM rows each.
+struct Place {
+  int segment, m0, end;
+};
+// Sums stop at `most`, the largest number of tile rows that ordered boundaries
+// give: others may not overflow them, and what is found below it is a tile of
+// its segment.
+template <int TM>
+struct Segments {
+  const ExpertArgs& x;
+  int lane, most, total;
+  Segment first;  // of the first 64 segments, this lane's
+  __device__ int tiles(const Segment& g) const { return (g.end - g.begin + TM - 1) / TM; }
+  __device__ Segment load(int s) const { return s < x.experts + 2 ? segment(x, s) : Segment{0, 0}; }
+  __device__ Segments(const ExpertArgs& x_, int most_, int lane_) : x(x_), lane(lane_), most(most_) {
+    first = load(lane);
+    int n = tiles(first);
+    for (int s = 64; s < x.experts + 2; s += 64) n = min(n + tiles(load(s + lane)), most);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) n = min(n + __shfl_xor(n, o), most);
+    total = __builtin_amdgcn_readfirstlane(n);
+  }
+  __device__ Place find(int at) const {  // at < total
+    int before = 0;
+    for (int s = 0;; s += 64) {
+      const Segment g = s ? load(s + lane) : first;
+      int upto = min(before + tiles(g), most);  // of the segments up to this lane's
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int v = __shfl_up(upto - before, o);
+        if (lane >= o) upto = min(upto + v, most);
+      }
+      const uint64_t here = __ballot(upto > at);
+      if (here) {
+        const int l = __builtin_ctzll(here), in_front = l ? __builtin_amdgcn_readlane(upto, l - 1) : before;
+        return Place{s + l, __builtin_amdgcn_readlane(g.begin, l) + (at - in_front) * TM,
+                     __builtin_amdgcn_readlane(g.end, l)};
+      }
+      before = __builtin_amdgcn_readlane(upto, 63);
+      if (s + 64 >= x.experts + 2) return Place{0, 0, 0};
+    }
+  }
+};
+
+}  // namespace
+
+// Products over rows: grid as many tiles as there can be (tiles, 1, more tiles).
+template <int OP, bool BC, int ELT, int KW, int WM, int WN, int BM, int BN>
+__global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void expert_rows_kernel(GemmArgs a, ExpertArgs x, int nm,
+                                                                                 int nn) {
+  constexpr int TM = WM * BM * 32, BK = KW / ELT;
+  const Segments<TM> all(x, nm, threadIdx.x & 63);
+  const int64_t tile = (int64_t)blockIdx.z * gridDim.x + blockIdx.x;
+  if (tile >= (int64_t)all.total * nn) return;
+  int mt, nt;
+  tile_of((int)tile, all.total, nn, &mt, &nt);
+  const Place p = all.find(mt);
+  const int e = p.segment - 1;
+  a.M = p.end;
+  if (e < 0 || e >= x.experts) {
+    a.K = 0;
+    a.bias = nullptr;
+  } else {
+    a.B = (const uint8_t*)a.B + (int64_t)e * x.stride * ELT;
+    if (a.bias) a.bias = (const uint8_t*)a.bias + (int64_t)e * a.N * ELT;
+  }
+  tile_product<OP, true, BC, ELT, KW, WM, WN, BM, BN>(a, p.m0, nt * WN * BN * 32, 0,
+                                                      (int)(((int64_t)a.K + BK - 1) / BK), a.K, nullptr, 0);
+}
+
+// Weight gradients: experts times nm times nn tiles.
+template <int ELT, int KW, int WM, int WN, int BM, int BN>
+__global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void expert_weight_kernel(GemmArgs a, ExpertArgs x, int nm,
+                                                                                   int nn) {
+  constexpr int BK = KW / ELT;
+  const int64_t tile = (int64_t)blockIdx.z * gridDim.x + blockIdx.x;
+  if (tile >= (int64_t)x.experts * nm * nn) return;
+  const int e = (int)(tile / (nm * nn));
+  int mt, nt;
+  tile_of((int)(tile - (int64_t)e * nm * nn), nm, nn, &mt, &nt);
+  const Segment g = segment(x, e + 1);
+  if (a.accumulate && g.begin == g.end) return;
+  a.K = g.end - g.begin;
+  a.A = (const uint8_t*)a.A + (int64_t)g.begin * a.lda * ELT;
+  a.B = (const uint8_t*)a.B + (int64_t)g.begin * a.ldb * ELT;
+  a.out = (float*)a.out + (int64_t)e * x.stride;
+  tile_product<DATTRI_LINEAR_WEIGHT_GRAD, false, false, ELT, KW, WM, WN, BM, BN>(
+      a, mt * WM * BM * 32, nt * WN * BN * 32, 0, (int)(((int64_t)a.K + BK - 1) / BK), a.K, nullptr, 0);
+}
+
+// Column sums of an expert's rows: grid (64 columns, parts, experts); part y of
+// parts takes its share of the expert's rows.  Sums of one part go to out, else
+// part holds [parts][experts][cols].
+template <int ELT>
+__global__ __launch_bounds__(256) void expert_columns_kernel(const void* __restrict__ G, int64_t ld, ExpertArgs x,
+                                                             int cols, float* __restrict__ part,
+                                                             float* __restrict__ out, int accumulate) {
+  __shared__ float red[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane, e = blockIdx.z;
+  const Segment g = segment(x, e + 1);
+  const int64_t per = ((int64_t)g.end - g.begin + gridDim.y - 1) / gridDim.y, r0 = g.begin + blockIdx.y * per,
+                r1 = min((int64_t)g.end, r0 + per);
+  float s = 0.f;
+  if (c < cols)
+#pragma unroll 8
+    for (int64_t r = r0 + wave; r < r1; r += 4) s += load_elt<ELT>(G, r * ld + c);
+  red[wave][lane] = s;
+  __syncthreads();
+  if (wave == 0 && c < cols) {
+    s = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
+    const int64_t at = (int64_t)e * cols + c;
+    if (gridDim.y > 1)
+      part[(int64_t)blockIdx.y * x.experts * cols + at] = s;
+    else
+      out[at] = accumulate ? out[at] + s : s;
+  }
+}
+
+__global__ __launch_bounds__(256) void expert_columns_join_kernel(const float* __restrict__ part, int parts, int64_t n,
+                                                                  float* __restrict__ out, int accumulate) {
+  const int64_t i = row_block() * 256 + threadIdx.x;
+  if (i >= n) return;
+  float s = 0.f;
+#pragma unroll 4
+  for (int y = 0; y < parts; ++y) s += part[y * n + i];
+  out[i] = accumulate ? out[i] + s : s;
+}
+
+namespace {
+
+int64_t column_parts(int64_t rows, int64_t experts, int64_t cols) {
+  return std::max<int64_t>(1, std::min<int64_t>(2048 / ((cols + 63) / 64 * experts), rows / experts / 64));
+}
+
+struct ExpertLayout {
+  int64_t a_rows, a_w, b_rows, b_w;  // as stored
+  bool pack_a, pack_b;
+  size_t off_a, off_b, off_cols, total;
+};
+ExpertLayout expert_layout(dattri_linear_op op, int64_t rows, int64_t experts, int64_t d_in, int64_t d_out, int elt,
+                           bool aligned) {
+  ExpertLayout L = {};
+  const bool wgrad = op == DATTRI_LINEAR_WEIGHT_GRAD;
+  L.a_rows = rows;
+  L.a_w = op == DATTRI_LINEAR_FORWARD ? d_in : d_out;
+  L.b_rows = wgrad ? rows : experts * d_out;
+  L.b_w = d_in;
+  L.pack_a = !aligned || (L.a_w * elt) % 16;
+  L.pack_b = !aligned || (L.b_w * elt) % 16;
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off = align_up(off + bytes);
+    return at;
+  };
+  auto packed = [&](int64_t r, int64_t w) { return (size_t)r * (size_t)((w * elt + 15) / 16 * 16); };
+  L.off_a = take(L.pack_a ? packed(L.a_rows, L.a_w) : 0);
+  L.off_b = take(L.pack_b ? packed(L.b_rows, L.b_w) : 0);
+  L.off_cols = off;
+  if (wgrad) {
+    const int64_t parts = column_parts(rows, experts, d_out);
+    take(parts > 1 ? (size_t)parts * experts * d_out * 4 : 0);
+  }
+  L.total = off;
+  return L;
+}
+
+template <int OP, int ELT, int KW, int WM, int WN, int BM, int BN>
+hipError_t launch_tiles(const GemmArgs& a, const ExpertArgs& x, hipStream_t s) {
+  constexpr int TM = WM * BM * 32, TN = WN * BN * 32;
+  const int64_t nn = ((int64_t)a.N + TN - 1) / TN;
+  dim3 grid;
+  if constexpr (OP == DATTRI_LINEAR_WEIGHT_GRAD) {
+    const int64_t nm = ((int64_t)a.M + TM - 1) / TM;
+    if (nm * nn > INT32_MAX) return hipErrorInvalidValue;
+    const hipError_t e = row_grid(x.experts * nm * nn, &grid, 256, true);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((expert_weight_kernel<ELT, KW, WM, WN, BM, BN>), grid, dim3(256), 0, s, a, x, (int)nm, (int)nn);
+  } else {
+    // every segment with rows has at most one tile more than its rows fill
+    const int64_t nm = x.rows / TM + std::min<int64_t>(x.experts + 2, x.rows);
+    if (nm * nn > INT32_MAX) return hipErrorInvalidValue;
+    const hipError_t e = row_grid(nm * nn, &grid, 256, true);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((expert_rows_kernel<OP, OP == DATTRI_LINEAR_FORWARD, ELT, KW, WM, WN, BM, BN>), grid, dim3(256),
+                       0, s, a, x, (int)nm, (int)nn);
+  }
+  return hipGetLastError();
+}
+
+template <int OP, int ELT>
+hipError_t launch_product(const GemmArgs& a, const ExpertArgs& x, hipStream_t s) {
+  return launch_tiles<OP, ELT, 64, 2, 2, 2, 2>(a, x, s);
+}
+
+}  // namespace
+
+size_t expert_workspace_need(dattri_linear_op op, int64_t rows, int64_t experts, int64_t d_in, int64_t d_out, int elt,
+                             bool aligned) {
+  return expert_layout(op, rows, experts, d_in, d_out, elt, aligned).total;
+}
+
+hipError_t launch_expert(dattri_linear_op op, int elt, bool aligned, GemmArgs a, ExpertArgs x, float* dbias,
+                         uint8_t* ws, hipStream_t s) {
+  const bool wgrad = op == DATTRI_LINEAR_WEIGHT_GRAD;
+  const int64_t d_out = op == DATTRI_LINEAR_FORWARD ? a.N : wgrad ? a.M : a.K,
+                d_in = op == DATTRI_LINEAR_FORWARD ? a.K : a.N;
+  const int oelt = wgrad ? 4 : elt;
+  auto on4 = [](const void* p, int64_t ld, int e) { return !p || ((uintptr_t)p % (4 * e) == 0 && ld % 4 == 0); };
+  a.vec = on4(a.bias, a.N, elt) && on4(a.R, a.ldr, elt) && on4(a.Z, a.ldz, elt) && on4(a.out, a.ldo, oelt) &&
+          on4(a.out2, a.ldo2, elt) && (!wgrad || x.stride % 4 == 0);
+  const ExpertLayout L = expert_layout(op, x.rows, x.experts, d_in, d_out, elt, aligned);
+  hipError_t e;
+  if (dbias) {
+    const int64_t parts = column_parts(x.rows, x.experts, d_out), n = (int64_t)x.experts * d_out;
+    float* part = (float*)(ws + L.off_cols);
+    hipLaunchKernelGGL(elt == 2 ? expert_columns_kernel<2> : expert_columns_kernel<4>,
+                       dim3((unsigned)((d_out + 63) / 64), (unsigned)parts, (unsigned)x.experts), dim3(256), 0, s, a.A,
+                       a.lda, x, (int)d_out, part, dbias, (int)a.accumulate);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (parts > 1) {
+      dim3 grid;
+      if ((e = row_grid((n + 255) / 256, &grid)) != hipSuccess) return e;
+      hipLaunchKernelGGL(expert_columns_join_kernel, grid, dim3(256), 0, s, part, (int)parts, n, dbias,
+                         (int)a.accumulate);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    if (!a.out) return hipSuccess;
+  }
+  if (L.pack_a || L.pack_b) {
+    Repack ra = {}, rb = {};
+    if (L.pack_a) ra = repack_of(&a.A, &a.lda, L.a_w, L.a_rows, elt, ws + L.off_a);
+    if (L.pack_b) {
+      rb = repack_of(&a.B, &a.ldb, L.b_w, L.b_rows, elt, ws + L.off_b);
+      if (!wgrad) x.stride = a.ldb * d_out;
+    }
+    const int64_t n = ra.rows + rb.rows;
+    if (n > 0) {
+      dim3 grid;
+      if ((e = row_grid((n + 3) / 4, &grid)) != hipSuccess) return e;
+      hipLaunchKernelGGL(elt == 2 ? repack_kernel<2> : repack_kernel<4>, grid, dim3(256), 0, s, ra, rb);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+  }
+  if (op == DATTRI_LINEAR_FORWARD)
+    return elt == 2 ? launch_product<DATTRI_LINEAR_FORWARD, 2>(a, x, s)
+                    : launch_product<DATTRI_LINEAR_FORWARD, 4>(a, x, s);
+  if (op == DATTRI_LINEAR_INPUT_GRAD)
+    return elt == 2 ? launch_product<DATTRI_LINEAR_INPUT_GRAD, 2>(a, x, s)
+                    : launch_product<DATTRI_LINEAR_INPUT_GRAD, 4>(a, x, s);
+  return elt == 2 ? launch_product<DATTRI_LINEAR_WEIGHT_GRAD, 2>(a, x, s)
+                  : launch_product<DATTRI_LINEAR_WEIGHT_GRAD, 4>(a, x, s);
+}
+
+}  // namespace dattri

@@ -428,7 +428,9 @@ __global__ __launch_bounds__(256) void repack_kernel(Repack a, Repack b) {
   uint8_t* dst = p.dst + r * p.ld_out * ELT;
 #pragma unroll 8
   for (int c = lane; c < p.ld_out; c += 64) {
-    if constexpr (ELT == 2)
+    if constexpr (ELT == 1)
+      dst[c] = c < p.w ? src[c] : (uint8_t)0;
+    else if constexpr (ELT == 2)
       ((uint16_t*)dst)[c] = c < p.w ? ((const uint16_t*)src)[c] : (uint16_t)0;
     else
       ((uint32_t*)dst)[c] = c < p.w ? ((const uint32_t*)src)[c] : 0u;

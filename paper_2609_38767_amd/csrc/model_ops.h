@@ -60,6 +60,66 @@ hipError_t launch_linear(dattri_linear_op op, int elt, bool aligned, GemmArgs a,
 bool linear_few(dattri_linear_op op, int64_t rows, int64_t d_out);
 hipError_t launch_linear_few(int elt, const GemmArgs& a, bool aligned, hipStream_t s);
 
+// --------------------------------------------------------------- experts
+// A product of rows sorted by expert: rows [offsets[e], offsets[e + 1]) meet
+// expert e's weight.  GemmArgs hold expert 0's weight, bias and weight gradient
+// and the whole buffers' rows.
+struct ExpertArgs {
+  const void* offsets;  // [experts + 1] integers of offset_bytes
+  int offset_bytes, experts;
+  int rows;
+  int64_t stride;  // elements between two experts' weights, or weight gradients
+};
+size_t expert_workspace_need(dattri_linear_op op, int64_t rows, int64_t experts, int64_t d_in, int64_t d_out, int elt,
+                             bool aligned);
+// aligned: both operands readable in 16-byte pieces; a.out may be null beside dbias (weight grad).
+hipError_t launch_expert(dattri_linear_op op, int elt, bool aligned, GemmArgs a, ExpertArgs x, float* dbias,
+                         uint8_t* ws, hipStream_t s);
+
+// ----------------------------------------------------------------- 8 bits
+// Scales of an 8-bit product: x [rows][ldx], w [blocks of 128 outputs][ldw], one
+// for every 128 of k.
+struct Scales8 {
+  const float *x, *w;
+  int64_t ldx, ldw;
+};
+size_t linear8_workspace_need(int64_t rows, int64_t d_in, int64_t d_out, bool aligned);
+// As the forward product: A = X, B = W, one byte per element; elt is that of bias, R, Y and Z.
+hipError_t launch_linear8(int elt, bool aligned, GemmArgs a, const Scales8& sc, uint8_t* ws, hipStream_t s);
+hipError_t launch_quantize_rows(int elt, const void* X, int64_t ldx, int64_t rows, int64_t d, uint8_t* Q, int64_t ldq,
+                                float* S, int64_t lds, hipStream_t s);
+hipError_t launch_quantize_weight(int elt, const void* W, int64_t ldw, int64_t rows, int64_t d, uint8_t* Q, int64_t ldq,
+                                  float* S, int64_t lds, hipStream_t s);
+
+// ------------------------------------------------------------------ norm
+struct NormArgs {
+  const void *X, *R, *W;  // R may be null
+  int64_t ldx, ldr, rows;
+  int d;
+  float eps;
+  void *Y, *H;  // may be null
+  int64_t ldy, ldh;
+  uint8_t* Q;  // may be null, with S
+  float* S;
+  int64_t ldq, lds;
+};
+hipError_t launch_rms_norm(int elt, const NormArgs& a, hipStream_t s);
+struct NormGradArgs {
+  const void *G, *H, *W, *P;  // P may be null
+  int64_t ldg, ldh, ldp, rows;
+  int d;
+  float eps;
+  void* D;
+  int64_t ldd;
+  float* U;  // [rows], set by the launch
+};
+struct NormGradLayout {
+  size_t off_part, total;
+};
+NormGradLayout norm_grad_layout(int64_t rows, int64_t d, bool weight);
+// dw: null or the weight's gradient
+hipError_t launch_norm_grad(int elt, NormGradArgs a, float* dw, bool accumulate, uint8_t* ws, hipStream_t s);
+
 // ------------------------------------------------------------------ clip
 constexpr int kClipTensors = 128;    // tensors per launch (their list is a kernel argument)
 constexpr int kClipChunk = 16384;    // elements per unit of work

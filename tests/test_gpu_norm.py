@@ -1,0 +1,194 @@
+"""Root-mean-square norm, its gradient and 8-bit rows and weights on the GPU
+against the float64 oracle, elementwise within derived bounds.
+
+A sum of squares is at most 128 additions deep in any of the kernels, its terms
+have one sign, so mean and eps are within 130 U, u = (.)^(-1/2) within 65 U and
+four roundings more; y = h u w has the rounding of h and two more: 80 U |y| in
+all, then the output's rounding."""
+import numpy as np
+import pytest
+import torch
+
+from model_util import DT, OUT, U, check, gen, host, rand
+from oracle import block as ob
+
+pytestmark = pytest.mark.gpu
+DTYPES = ["f32", "bf16"]
+DEEP = 80 * U
+# rows, d: single elements, one off the groups of 128 and the waves, widths of every form, odd ones
+SIZES = [(1, 1), (3, 2), (2, 8), (5, 63), (4, 64), (7, 65), (3, 127), (9, 128), (2, 129), (33, 256), (5, 769), (1, 1000),
+         (2, 1024), (17, 2049), (1, 4096), (130, 4096), (3, 4104), (2, 8192), (5, 9001), (1, 16384), (3, 16392),
+         (2, 33000), (1, 65536), (2, 65552), (1, 70001), (2051, 72)]
+
+
+def layers():
+    from paper_2609_38767_amd import layers as m
+    return m
+
+
+def check8(q, s, y, what=""):
+    """8-bit values and scales against exact y, itself known to the kernel within DEEP."""
+    y = y.reshape(-1, y.shape[-1])
+    s, q = host(s).reshape(len(y), -1), host(q).reshape(y.shape)
+    top = np.maximum.reduceat(np.abs(y), np.arange(0, y.shape[1], ob.BLOCK), axis=1)
+    want = np.maximum(top / ob.MOST, ob.LEAST)
+    assert (np.abs(s - want) <= (DEEP + 2 * U) * want).all(), what
+    each = ob.spread(s, *y.shape, 1)
+    # half a step: 2^-4 of a value, 2^-10 of the scale below 2^-6; the quotient's own error before it
+    assert (np.abs(q * each - y) <= np.maximum(2.0 ** -4 * np.abs(y), 2.0 ** -10 * each) + 2 * DEEP * np.abs(y)).all(), what
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size", SIZES, ids=lambda s: "x".join(map(str, s)))
+def test_forward(size, dtype):
+    n, d = size
+    k, g = SIZES.index(size), gen(SIZES.index(size))
+    x, w = rand(g, n, d, dtype=dtype, std=3.0), rand(g, d, dtype=dtype)
+    r = rand(g, n, d, dtype=dtype) if k % 2 else None
+    y, h, _ = ob.rms_norm(host(x), host(w), None if r is None else host(r), 1e-5)
+    by, bh = (DEEP + OUT[dtype] * (1 + DEEP)) * np.abs(y), (U + OUT[dtype] * (1 + U)) * np.abs(h)
+    got = layers().rms_norm(x, w, residual=r, eps=1e-5)
+    if r is not None:
+        check(got[1], h, bh, "h")
+        got = got[0]
+    check(got, y, by, "y")
+    eight = layers().rms_norm_8bit(x, w, residual=r, eps=1e-5, keep=True)
+    check8(*eight[0], y)
+    assert torch.equal(eight[1], got)  # the same bits
+    if r is not None:
+        check(eight[2], h, bh, "h")
+        (q, s), _ = layers().rms_norm_8bit(x, w, residual=r, eps=1e-5)
+    else:
+        q, s = layers().rms_norm_8bit(x, w, eps=1e-5)
+    assert torch.equal(q.view(torch.uint8), eight[0][0].view(torch.uint8)) and torch.equal(s, eight[0][1])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size", SIZES, ids=lambda s: "x".join(map(str, s)))
+def test_gradients(size, dtype):
+    n, d = size
+    k, gn = SIZES.index(size), gen(100 + SIZES.index(size))
+    g, h, w = rand(gn, n, d, dtype=dtype), rand(gn, n, d, dtype=dtype, std=2.0), rand(gn, d, dtype=dtype)
+    p = rand(gn, n, d, dtype=dtype) if k % 2 else None
+    m = layers()
+    got, dw = m.rms_norm_grad(g, h, w, eps=1e-5, residual=p)
+    want, ww = ob.rms_norm_grad(host(g), host(h), host(w), None if p is None else host(p), 1e-5)
+    u = 1 / np.sqrt((host(h) ** 2).mean(1, keepdims=True) + 1e-5)
+    a = np.abs(host(g) * host(w))
+    # sums of 130 U, u and its square, the products around them
+    e = 400 * U * u * (a + np.abs(host(h)) * u ** 2 * (a * np.abs(host(h))).mean(1, keepdims=True))
+    e = e + (0 if p is None else 4 * U * (np.abs(host(p)) + np.abs(want)))
+    check(got, want, e + OUT[dtype] * (np.abs(want) + e), "d")
+    bw = (2 * (n + 8) * U + 90 * U) * np.abs(host(g) * host(h) * u).sum(0)
+    check(dw, ww, bw, "dw")
+    assert torch.equal(m.rms_norm_grad(g, h, w, eps=1e-5, residual=p, weight_grad=False), got)
+    w0 = rand(gn, d)
+    into = w0.clone()
+    assert m.rms_norm_grad(g, h, w, eps=1e-5, residual=p, out_weight=into, accumulate=True)[1] is into
+    check(into, ww + host(w0), bw + U * (np.abs(ww + host(w0)) + bw), "dw accumulated")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,d,pad,offset", [(9, 40, 8, 8), (70, 136, 3, 1), (5, 129, 5, 3), (130, 1024, 1, 0),
+                                            (3, 4096, 0, 1), (4, 20000, 24, 8), (2, 70001, 3, 1)])
+def test_strided_and_unaligned_rows(n, d, pad, offset, dtype):
+    """Padded and misaligned rows in NaN; what lies between the outputs' rows stays."""
+    m, gn = layers(), gen(d)
+    x, r = rand(gn, n, d, dtype=dtype, pad=pad, offset=offset), rand(gn, n, d, dtype=dtype, pad=pad, offset=offset)
+    w = rand(gn, d, dtype=dtype, offset=offset)
+    y, h = (torch.full((n, d + pad), 7.0, dtype=DT[dtype], device="cuda") for _ in range(2))
+    m.rms_norm(x, w, residual=r, out=y[:, :d], out_sum=h[:, :d])
+    plain = m.rms_norm(x.contiguous(), w.clone(), residual=r.contiguous())
+    want, wh, _ = ob.rms_norm(host(x), host(w), host(r))
+    for got, v in ((y[:, :d], want), (h[:, :d], wh), (plain[0], want), (plain[1], wh)):
+        check(got, v, (DEEP + OUT[dtype] * (1 + DEEP)) * np.abs(v))
+    assert (y[:, d:] == 7).all() and (h[:, d:] == 7).all()
+    check8(*m.rms_norm_8bit(x, w), ob.rms_norm(host(x), host(w))[0])
+    dh, dw = m.rms_norm_grad(r, x, w, residual=r, out=y[:, :d])
+    wd, ww = ob.rms_norm_grad(host(r), host(x), host(w), host(r))
+    u = 1 / np.sqrt((host(x) ** 2).mean(1, keepdims=True) + 1e-6)
+    a = np.abs(host(r) * host(w))
+    e = 400 * U * u * (a + np.abs(host(x)) * u ** 2 * (a * np.abs(host(x))).mean(1, keepdims=True))
+    e = e + 4 * U * (np.abs(host(r)) + np.abs(wd))
+    check(dh, wd, e + OUT[dtype] * (np.abs(wd) + e))
+    check(dw, ww, (2 * (n + 8) * U + 90 * U) * np.abs(host(r) * host(x) * u).sum(0))
+    assert (y[:, d:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [40, 769, 4096, 20000, 70001])
+def test_in_place_and_leading_axes(d, dtype):
+    m, gn = layers(), gen(23)
+    x, r, w = rand(gn, 3, 5, d, dtype=dtype), rand(gn, 3, 5, d, dtype=dtype), rand(gn, d, dtype=dtype)
+    y, h = m.rms_norm(x, w, residual=r)
+    assert y.shape == h.shape == x.shape
+    a, b = x.clone(), r.clone()  # the norm over x, the stream over the residual
+    got = m.rms_norm(a, w, residual=b, out=a, out_sum=b)
+    assert got[0] is a and got[1] is b and torch.equal(a, y) and torch.equal(b, h)
+    a, b = x.clone(), r.clone()  # the other way round
+    m.rms_norm(a, w, residual=b, out=b, out_sum=a)
+    assert torch.equal(b, y) and torch.equal(a, h)
+    a = x.clone()
+    assert torch.equal(m.rms_norm(a, w, out=a), m.rms_norm(x, w))
+    (q, s), h8 = m.rms_norm_8bit(x, w, residual=r)
+    assert q.shape == x.shape and s.shape == (3, 5, -(-d // 128)) and torch.equal(h8, h)
+    p = r.clone()
+    want = m.rms_norm_grad(x, h, w, residual=r, weight_grad=False)
+    assert torch.equal(m.rms_norm_grad(x, h, w, residual=p, out=p)[0], want) and torch.equal(p, want)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_no_rows_and_special_values(dtype):
+    m, gn = layers(), gen(5)
+    w = rand(gn, 300, dtype=dtype)
+    none = torch.empty(0, 300, dtype=DT[dtype], device="cuda")
+    assert m.rms_norm(none, w).shape == (0, 300) and m.rms_norm_8bit(none, w)[1].shape == (0, 3)
+    d, dw = m.rms_norm_grad(none, none, w)
+    assert d.shape == (0, 300) and dw.shape == (300,) and not dw.any()
+    x = rand(gn, 6, 300, dtype=dtype)
+    x[0] = 0
+    x[1, 7] = float("nan")
+    x[2, 299] = float("inf")
+    x[3] *= 2.0 ** -60
+    y = m.rms_norm(x, w)
+    assert not y[0].any() and y[1].isnan().all()
+    assert y[2, 299].isnan() and not y[2, :299].any()
+    want = ob.rms_norm(host(x[3:]), host(w))[0]
+    check(y[3:], want, (DEEP + OUT[dtype] * 2) * np.abs(want) + (2.0 ** -133 if dtype == "bf16" else 2.0 ** -149))
+    q, s = m.rms_norm_8bit(x, w)
+    assert not q[0].float().any() and (s[0] == 2.0 ** -126).all() and q[1].float().isnan().all()
+    assert m.rms_norm(x[:1], w, eps=0.0).isnan().all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,d,pad", [(1, 1, 0), (4, 127, 0), (3, 128, 0), (65, 129, 3), (130, 1024, 0), (257, 300, 5),
+                                     (2, 16392, 8), (128, 128, 0), (300, 264, 0)])
+def test_quantize(n, d, pad, dtype):
+    """The very values of the definition: the float32 quotient, rounded to the nearest e4m3 value, ties to even."""
+    m, gn = layers(), gen(n + d)
+    x = rand(gn, n, d, dtype=dtype, pad=pad)
+    x[0] *= 2.0 ** -90
+    x[-1, -1] = 0
+    x[-1, 0] = -7.0  # a scale of a power of two: quotients halfway between two values
+    if n > 2:
+        x[1] = 0
+    q, s = m.quantize_rows(x)
+    wq, ws = ob.quantize(host(x))
+    assert np.array_equal(host(s), ws) and np.array_equal(host(q), wq)
+    q, s = m.quantize_weight(x)
+    wq, ws = ob.quantize(host(x), 128)
+    assert np.array_equal(host(s), ws) and np.array_equal(host(q), wq)
+    qt, st = m.transpose_8bit((q, s))
+    assert np.array_equal(host(qt), wq.T) and np.array_equal(host(st), ws.T)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_quantize_special_values(dtype):
+    m = layers()
+    x = torch.ones(3, 256, dtype=DT[dtype], device="cuda")
+    x[0, 5] = float("nan")
+    x[1, 130] = float("-inf")
+    q, s = m.quantize_rows(x)
+    assert q[0, 5].float().isnan() and (q[0, :5].float() == 448).all() and s[0, 0] == 1 / torch.tensor(448.0)
+    assert s[1, 1] == float("inf") and q[1, 130].float().isnan() and not q[1, 131:].float().any()
+    assert (q[1, :128].float() == 448).all() and (q[2].float() == 448).all()

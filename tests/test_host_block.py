@@ -1,0 +1,141 @@
+"""Refusals and sizes of the norm's, the 8-bit products' and the experts' entry
+points (no GPU): every bad call returns the documented status before any GPU
+work."""
+import pytest
+
+import paper_2609_38767_amd as dt
+
+P = 1 << 20  # addresses that no call here reaches, 1 MB apart
+A = [P * (k + 1) for k in range(12)]
+
+
+def status(fn, *args):
+    with pytest.raises(dt.DattriError) as e:
+        fn(*args)
+    return e.value.status_name
+
+
+def test_rms_norm_errors():
+    def call(X=A[0], lx=0, R=None, lr=0, W=A[1], eps=1e-6, Y=A[2], ly=0, H=None, lh=0, Q=None, lq=0, S=None, ls=0, n=4,
+             d=300, dtype=0):
+        return status(dt.dattri_rms_norm, X, lx, R, lr, W, eps, Y, ly, H, lh, Q, lq, S, ls, n, d, dtype, 0)
+    for kw in (dict(X=None), dict(W=None), dict(Y=None), dict(n=-1), dict(d=0), dict(lx=299), dict(ly=-1), dict(eps=-1.0),
+               dict(eps=float("nan")), dict(eps=float("inf")), dict(X=A[0] + 2), dict(W=A[1] + 1), dict(Q=A[3]),
+               dict(S=A[3]), dict(H=A[3]), dict(Q=A[3], S=A[4] + 2), dict(Q=A[3], S=A[4], ls=2), dict(Q=A[3], S=A[4], lq=9),
+               dict(R=A[3], H=A[4], lh=5)):
+        assert call(**kw) == "E_INVALID_ARG", kw
+    # outputs in inputs or in each other; in place only as a whole
+    for kw in (dict(Y=A[0] + 400), dict(Y=A[1]), dict(R=A[3], H=A[2]), dict(R=A[3], H=A[3] + 1200), dict(Q=A[0], S=A[4]),
+               dict(Q=A[2], S=A[4]), dict(Q=A[3], S=A[3] + 8), dict(Q=A[3], S=A[0]), dict(Y=A[0], lx=304, ly=308)):
+        assert call(**kw) == "E_INVALID_ARG", kw
+    assert call(dtype=2) == "E_DTYPE"
+    for kw in (dict(n=1 << 31), dict(d=(1 << 23) + 1), dict(lx=1 << 23)):
+        assert call(**kw) == "E_UNSUPPORTED", kw
+    dt.dattri_rms_norm(None, 0, None, 0, A[0], 1e-6, None, 0, None, 0, None, 0, None, 0, 0, 8, 0, 0)  # no rows
+
+
+def test_rms_norm_grad_errors():
+    ws = dt.dattri_rms_norm_grad_workspace_bytes(400, 300, 1)
+    assert ws > 0 and dt.dattri_rms_norm_grad_workspace_bytes(400, 300, 1, False) == 0
+
+    def call(G=A[0], lg=0, H=A[1], lh=0, W=A[2], eps=1e-6, Pp=None, lp=0, D=A[3], ld=0, dW=A[4], n=400, d=300, dtype=1,
+             w=A[6], wb=ws):
+        return status(dt.dattri_rms_norm_grad, G, lg, H, lh, W, eps, Pp, lp, D, ld, dW, 0, n, d, dtype, w, wb, 0)
+    for kw in (dict(G=None), dict(H=None), dict(W=None), dict(D=None), dict(n=-1), dict(d=0), dict(lg=3), dict(lp=-1),
+               dict(eps=-0.5), dict(dW=A[4] + 2), dict(D=A[0]), dict(D=A[1]), dict(Pp=A[5], D=A[5] + 2), dict(dW=A[3]),
+               dict(dW=A[0] + 8), dict(w=A[3]), dict(w=A[0] + 256)):
+        assert call(**kw) == "E_INVALID_ARG", kw
+    for kw in (dict(w=None), dict(wb=ws - 1), dict(w=A[6] + 16)):
+        assert call(**kw) == "E_WORKSPACE", kw
+    assert call(dtype=7) == "E_DTYPE" and call(n=1 << 31) == "E_UNSUPPORTED"
+    assert status(dt.dattri_rms_norm_grad_workspace_bytes, -1, 4, 0) == "E_INVALID_ARG"
+    assert dt.load().dattri_rms_norm_grad_workspace_bytes(1, 1, 0, 1, None) == -1
+
+
+def test_quantize_errors():
+    def rows(X=A[0], lx=0, n=4, d=300, dtype=0, Q=A[1], lq=0, S=A[2], ls=0):
+        return status(dt.dattri_quantize_rows, X, lx, n, d, dtype, Q, lq, S, ls, 0)
+
+    def weight(W=A[0], lw=0, o=200, i=300, dtype=0, Q=A[1], lq=0, S=A[2], ls=0):
+        return status(dt.dattri_quantize_weight, W, lw, o, i, dtype, Q, lq, S, ls, 0)
+    for kw in (dict(X=None), dict(Q=None), dict(S=None), dict(n=-1), dict(d=0), dict(lx=1), dict(lq=299), dict(ls=2),
+               dict(S=A[2] + 1), dict(Q=A[0]), dict(S=A[0]), dict(S=A[1])):
+        assert rows(**kw) == "E_INVALID_ARG", kw
+    for kw in (dict(W=None), dict(Q=None), dict(S=None), dict(o=0), dict(i=0), dict(lw=1), dict(ls=2), dict(Q=A[0] + 5),
+               dict(S=A[1] + 4)):
+        assert weight(**kw) == "E_INVALID_ARG", kw
+    assert rows(dtype=3) == weight(dtype=-1) == "E_DTYPE"
+    assert rows(n=1 << 31) == weight(o=1 << 24) == "E_UNSUPPORTED"
+
+
+def test_linear_8bit_errors():
+    n, i, o = 40, 200, 300
+    ws = dt.dattri_linear_scaled_workspace_bytes(n, i, o, 0, False)
+
+    def call(X=A[0], lx=0, SX=A[1], lsx=0, W=A[2], lw=0, SW=A[3], lsw=0, b=None, act=0, R=None, lr=0, Y=A[4], ly=0, Z=None,
+             lz=0, n=n, i=i, o=o, dtype=0, w=A[6], wb=ws):
+        return status(dt.dattri_linear_scaled, X, lx, SX, lsx, W, lw, SW, lsw, b, act, R, lr, Y, ly, Z, lz, n, i, o, dtype, w,
+                      wb, 0)
+    for kw in (dict(X=None), dict(SX=None), dict(W=None), dict(SW=None), dict(Y=None), dict(lx=199), dict(lsx=1),
+               dict(lw=5), dict(lsw=1), dict(SX=A[1] + 2), dict(b=A[5] + 1), dict(act=5), dict(act=-1), dict(n=-1),
+               dict(i=0), dict(o=0), dict(ly=299), dict(Y=A[0]), dict(Y=A[1]), dict(Y=A[2] + 40), dict(Y=A[3]),
+               dict(Z=A[4]), dict(R=A[5], Z=A[5]), dict(R=A[5], Y=A[5] + 4), dict(w=A[4])):
+        assert call(**kw) == "E_INVALID_ARG", kw
+    assert call(dtype=2) == "E_DTYPE"
+    for kw in (dict(n=1 << 31), dict(i=1 << 24), dict(o=1 << 24), dict(lx=1 << 24)):
+        assert call(**kw) == "E_UNSUPPORTED", kw
+    assert dt.dattri_linear_scaled_workspace_bytes(n, i, o, 0, True) <= ws
+    for kw in (dict(w=None), dict(wb=ws - 1), dict(w=A[6] + 16)):  # 200 columns are not whole 16 bytes
+        assert call(**kw) == "E_WORKSPACE", kw
+    assert status(dt.dattri_linear_scaled_workspace_bytes, 1, 1, 1, 5) == "E_DTYPE"
+
+
+def test_expert_errors():
+    n, i, o, e = 40, 24, 40, 3
+    ws = max(dt.dattri_expert_linear_workspace_bytes(op, n, e, i, o, 0, False) for op in range(3)) + 256
+
+    def fwd(X=A[0], lx=0, W=A[1], lw=0, b=None, off=A[2], ob=4, act=0, R=None, lr=0, Y=A[3], ly=0, Z=None, lz=0, n=n, e=e,
+            i=i, o=o, dtype=0, w=A[6], wb=ws):
+        return status(dt.dattri_expert_linear, X, lx, W, lw, b, off, ob, act, R, lr, Y, ly, Z, lz, n, e, i, o, dtype, w, wb,
+                      0)
+
+    def inp(G=A[0], W=A[1], off=A[2], ob=8, R=None, act=0, Z=None, D=None, Pp=A[3], lp=0, e=e, dtype=0, w=A[6], wb=ws):
+        return status(dt.dattri_expert_linear_input_grad, G, 0, W, 0, off, ob, R, 0, act, Z, 0, D, 0, Pp, lp, n, e, i, o,
+                      dtype, w, wb, 0)
+
+    def wgt(G=A[0], X=A[1], off=A[2], ob=4, dW=A[3], ldw=0, db=None, e=e, dtype=0, w=A[6], wb=ws):
+        return status(dt.dattri_expert_linear_weight_grad, G, 0, X, 0, off, ob, dW, ldw, db, 0, n, e, i, o, dtype, w, wb, 0)
+    for kw in (dict(X=None), dict(W=None), dict(off=None), dict(ob=2), dict(off=A[2] + 2), dict(Y=None), dict(lx=23),
+               dict(lw=1), dict(ly=3), dict(n=-1), dict(e=0), dict(e=-4), dict(i=0), dict(o=0), dict(act=5),
+               dict(b=A[5] + 2), dict(Y=A[0]), dict(Y=A[1] + 24 * 4 * 100), dict(Y=A[2]), dict(Z=A[3] + 4),
+               dict(R=A[5], Y=A[5] + 8), dict(b=A[3] + 16), dict(X=A[0] + 4, w=A[1])):
+        assert fwd(**kw) == "E_INVALID_ARG", kw
+    for kw in (dict(G=None), dict(W=None), dict(off=None), dict(ob=5), dict(Pp=None), dict(act=1), dict(D=A[3]),
+               dict(D=A[4], Z=A[4], act=1), dict(lp=23), dict(Pp=A[2]), dict(Pp=A[0])):
+        assert inp(**kw) == "E_INVALID_ARG", kw
+    for kw in (dict(G=None), dict(X=None), dict(off=None), dict(dW=None), dict(ldw=5), dict(db=A[4] + 2), dict(db=A[3]),
+               dict(dW=A[0]), dict(db=A[2])):
+        assert wgt(**kw) == "E_INVALID_ARG", kw
+    assert fwd(dtype=4) == inp(dtype=4) == wgt(dtype=4) == "E_DTYPE"
+    for kw in (dict(n=1 << 31), dict(e=65536), dict(o=1 << 22, e=600), dict(i=1 << 24)):
+        assert fwd(**kw) == "E_UNSUPPORTED", kw
+    assert inp(e=1 << 20) == wgt(e=1 << 20) == "E_UNSUPPORTED"
+    need = dt.dattri_expert_linear_workspace_bytes(0, n, e, i, o, 0, False)
+    assert need >= 4 * (n * i + e * o * i)  # both operands repacked
+    assert fwd(X=A[0] + 4, w=None) == fwd(X=A[0] + 4, wb=need - 1) == fwd(X=A[0] + 4, w=A[6] + 8) == "E_WORKSPACE"
+    assert status(dt.dattri_expert_linear_workspace_bytes, 3, 1, 1, 1, 1, 0) == "E_INVALID_ARG"
+
+
+def test_layers_refuse_on_the_host():
+    """What the tensors themselves show: no GPU tensors, wrong types and shapes."""
+    import torch
+
+    from paper_2609_38767_amd import layers as m
+    x = torch.zeros(3, 8)
+    for call in (lambda: m.rms_norm(x, x[0]), lambda: m.rms_norm_grad(x, x, x[0]), lambda: m.quantize_rows(x),
+                 lambda: m.quantize_weight(x), lambda: m.linear_8bit((x, x), (x, x)),
+                 lambda: m.expert_linear(x, x, x), lambda: m.expert_linear_weight_grad(x, x, x)):
+        with pytest.raises(ValueError, match="on the GPU"):
+            call()
+    q, s = m.transpose_8bit((torch.zeros(3, 8).to(torch.float8_e4m3fn), torch.ones(1, 2)))
+    assert q.shape == (8, 3) and s.shape == (2, 1) and q.is_contiguous()
