@@ -4,9 +4,14 @@
 //   h = x + r,  u = 1 / sqrt(mean_j h_j^2 + eps),  y_j = h_j u w_j
 //   a_j = g_j w_j:  dh_j = u (a_j - h_j u^2 mean_j(a_j h_j)) + p_j,  dw_j = sum_rows g_j h_j u
 //
-// A workgroup per row that reads it twice: for its sums, in float64, and for its
-// outputs.  A wave takes 128 neighbouring columns at a time, 64 apart per lane, so
-// that the largest magnitude of a group of 8-bit values is one reduction.
+// Rows that fit the registers of up to 1024 threads are read once: T threads hold
+// a row, C pieces of 16 bytes each (or of two elements where rows are not on 16
+// bytes), from the sums to the outputs.  Longer rows are read twice, by a
+// workgroup each.  A group of 8-bit values is 128 neighbouring columns of one
+// wave's piece, so its largest magnitude is one reduction over 16, 32 or 64 lanes.
+#include <algorithm>
+#include <type_traits>
+
 #include "api_common.h"
 #include "device_common.h"
 #include "eight.h"
@@ -38,7 +43,177 @@ __device__ inline void store_group8(uint8_t* q, float* s, int lane, int left, fl
   if (lane == 0) *s = sc;
 }
 
+// Sum or maximum over 16 lanes by data-parallel moves: the quad's neighbours, the
+// other quad of eight, the other eight.
+template <class F>
+__device__ inline float over16(float v, F f) {
+  auto moved = [](float x, auto ctrl) {
+    const int i = __builtin_bit_cast(int, x);
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(i, i, decltype(ctrl)::value, 0xF, 0xF, false));
+  };
+  v = f(v, moved(v, std::integral_constant<int, 0xB1>{}));   // quad_perm 1 0 3 2
+  v = f(v, moved(v, std::integral_constant<int, 0x4E>{}));   // quad_perm 2 3 0 1
+  v = f(v, moved(v, std::integral_constant<int, 0x141>{}));  // row_half_mirror
+  return f(v, moved(v, std::integral_constant<int, 0x140>{}));  // row_mirror
+}
+__device__ inline float wave_sum(float v) {
+  v = over16(v, [](float a, float b) { return a + b; });
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
+
+// A thread's pieces of a row of d elements held by T threads.
+template <int ELT, bool VEC, int T>
+struct RowOf {
+  static constexpr int N = VEC ? 16 / ELT : 2;  // elements of a piece
+  typedef std::conditional_t<VEC, i32x4, i32x2> Raw;
+  int t, d;
+  // Column of element e of piece c.  VEC: N neighbours per lane; else 64 apart, lanes neighbours.
+  __device__ int col(int c, int e) const {
+    return VEC ? (c * T + t) * N + e : (c * (T / 64) + (t >> 6)) * kGroup8 + (t & 63) + 64 * e;
+  }
+  __device__ bool has(int c, int e = 0) const { return col(c, e) < d; }
+  __device__ Raw load(const void* row, int c) const {
+    Raw r = {};
+    if constexpr (VEC) {
+      if (has(c)) r = *(const i32x4*)((const uint8_t*)row + (int64_t)col(c, 0) * ELT);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        if (has(c, e)) r[e] = ELT == 2 ? ((const uint16_t*)row)[col(c, e)] : ((const int32_t*)row)[col(c, e)];
+    }
+    return r;
+  }
+  __device__ static void floats(Raw r, float (&v)[N]) {
+    if constexpr (!VEC) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) v[e] = __builtin_bit_cast(float, ELT == 2 ? r[e] << 16 : r[e]);
+    } else if constexpr (ELT == 2) {
+      const uint32_t w[4] = {(uint32_t)r.x, (uint32_t)r.y, (uint32_t)r.z, (uint32_t)r.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[2 * e] = __builtin_bit_cast(float, w[e] << 16);
+        v[2 * e + 1] = __builtin_bit_cast(float, w[e] & 0xFFFF0000u);
+      }
+    } else {
+      const f32x4 f = __builtin_bit_cast(f32x4, r);
+      v[0] = f.x;
+      v[1] = f.y;
+      v[2] = f.z;
+      v[3] = f.w;
+    }
+  }
+  __device__ void store(void* row, int c, const float (&v)[N]) const {
+    if constexpr (!VEC) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        if (has(c, e)) store_elt<ELT>(row, col(c, e), v[e]);
+    } else if (has(c)) {
+      i32x4 w;
+      if constexpr (ELT == 2)
+        w = i32x4{(int)pack_bf16(v[0], v[1]), (int)pack_bf16(v[2], v[3]), (int)pack_bf16(v[4], v[5]),
+                  (int)pack_bf16(v[6], v[7])};
+      else
+        w = __builtin_bit_cast(i32x4, f32x4{v[0], v[1], v[2], v[3]});
+      *(i32x4*)((uint8_t*)row + (int64_t)col(c, 0) * ELT) = w;
+    }
+  }
+  // The piece in 8 bits: values to q, the group's scale to s (both of the row).
+  __device__ void store8(uint8_t* q, float* s, int c, const float (&v)[N]) const {
+    float top = 0.f;
+#pragma unroll
+    for (int e = 0; e < N; ++e) top = max_mag(top, v[e]);
+    top = over16(top, [](float a, float b) { return fmaxf(a, b); });
+    if constexpr (N < 8) top = fmaxf(top, __shfl_xor(top, 16));
+    if constexpr (N < 4) top = fmaxf(top, __shfl_xor(top, 32));
+    const float sc = scale8(top), r = 1.f / sc;
+    if constexpr (!VEC) {
+      const int w = pack8<false>(over_scale(v[0], sc, r), over_scale(v[1], sc, r), 0);
+      if (has(c, 0)) q[col(c, 0)] = (uint8_t)w;
+      if (has(c, 1)) q[col(c, 1)] = (uint8_t)(w >> 8);
+    } else if (has(c)) {
+      int w[N / 4];
+#pragma unroll
+      for (int e = 0; e < N / 4; ++e)
+        w[e] = pack8<true>(over_scale(v[4 * e + 2], sc, r), over_scale(v[4 * e + 3], sc, r),
+                           pack8<false>(over_scale(v[4 * e], sc, r), over_scale(v[4 * e + 1], sc, r), 0));
+      if constexpr (N == 8)
+        *(i32x2*)(q + col(c, 0)) = i32x2{w[0], w[1]};
+      else
+        *(int*)(q + col(c, 0)) = w[0];
+    }
+    if (col(c, 0) % kGroup8 == 0 && has(c)) s[col(c, 0) / kGroup8] = sc;
+  }
+};
+
+// Sums of S values each over the T threads of a row, waves in order; every
+// thread gets them.  `red` holds [2][T / 64][S], `turn` alternates from call to call.
+template <int T, int S>
+__device__ inline void row_sums(float (&v)[S], float* red, int turn) {
+#pragma unroll
+  for (int k = 0; k < S; ++k) v[k] = wave_sum(v[k]);
+  if constexpr (T > 64) {
+    constexpr int W = T / 64;
+    float* at = red + (turn & 1) * W * S;
+    const int t = threadIdx.x % T;
+    if ((t & 63) == 0)
+#pragma unroll
+      for (int k = 0; k < S; ++k) at[(t >> 6) * S + k] = v[k];
+    lds_barrier();
+#pragma unroll
+    for (int k = 0; k < S; ++k) {
+      v[k] = at[k];
+#pragma unroll
+      for (int w = 1; w < W; ++w) v[k] += at[w * S + k];
+    }
+  }
+}
+
 }  // namespace
+
+template <int ELT, bool VEC, int T, int C>
+__global__ __launch_bounds__(T > 256 ? T : 256) void rms_norm_kernel(NormArgs a) {
+  typedef RowOf<ELT, VEC, T> Row;
+  constexpr int N = Row::N, kRows = T > 256 ? 1 : 256 / T;  // rows of a workgroup
+  __shared__ float red[2 * T / 64];
+  const Row p = {(int)threadIdx.x % T, a.d};
+  const int64_t row = row_block() * kRows + (T < 256 ? threadIdx.x / T : 0);
+  if (row >= a.rows) return;  // T < 256: whole waves, which meet no barrier
+  const uint8_t *x = (const uint8_t*)a.X + row * a.ldx * ELT, *r = (const uint8_t*)a.R + row * a.ldr * ELT;
+  typename Row::Raw rx[C], rr[C], rw[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) rx[c] = p.load(x, c);
+  if (a.R)
+#pragma unroll
+    for (int c = 0; c < C; ++c) rr[c] = p.load(r, c);
+#pragma unroll
+  for (int c = 0; c < C; ++c) rw[c] = p.load(a.W, c);
+  float h[C][N], s[1] = {0.f};
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    Row::floats(rx[c], h[c]);
+    if (a.R) {
+      float v[N];
+      Row::floats(rr[c], v);
+#pragma unroll
+      for (int e = 0; e < N; ++e) h[c][e] += v[e];
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) s[0] = fmaf(h[c][e], h[c][e], s[0]);
+  }
+  row_sums<T>(s, red, 0);
+  const float u = 1.f / sqrtf(s[0] / a.d + a.eps);
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    if (a.H) p.store((uint8_t*)a.H + row * a.ldh * ELT, c, h[c]);
+    float w[N];
+    Row::floats(rw[c], w);
+#pragma unroll
+    for (int e = 0; e < N; ++e) h[c][e] = h[c][e] * u * w[e];
+    if (a.Y) p.store((uint8_t*)a.Y + row * a.ldy * ELT, c, h[c]);
+    if (a.Q) p.store8(a.Q + row * a.ldq, a.S + row * a.lds, c, h[c]);
+  }
+}
 
 template <int ELT>
 __global__ __launch_bounds__(256) void rms_norm_long_kernel(NormArgs a) {
@@ -68,6 +243,94 @@ __global__ __launch_bounds__(256) void rms_norm_long_kernel(NormArgs a) {
       if (a.Y) store_elt<ELT>(a.Y, row * a.ldy + j, y[e]);
     }
     if (a.Q) store_group8(a.Q + row * a.ldq + c, a.S + row * a.lds + c / kGroup8, lane, a.d - c, y[0], y[1]);
+  }
+}
+
+// The workgroups walk the rows; each keeps its columns' share of dW and leaves it
+// as one row of part (null: dW is not wanted).
+template <int ELT, bool VEC, int T, int C>
+__global__ __launch_bounds__(T > 256 ? T : 256) void norm_grad_kernel(NormGradArgs a, float* __restrict__ part) {
+  typedef RowOf<ELT, VEC, T> Row;
+  constexpr int N = Row::N, kRows = T > 256 ? 1 : 256 / T;
+  __shared__ float red[4 * T / 64];
+  __shared__ float share[kRows > 1 ? kRows * T * N : 1];
+  const Row p = {(int)threadIdx.x % T, a.d};
+  const int sub = T < 256 ? threadIdx.x / T : 0;
+  typename Row::Raw rw[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) rw[c] = p.load(a.W, c);
+  float dw[C][N] = {};
+  // T > 64: all rows of a workgroup meet the barriers of row_sums, so it runs as long as its first has a row
+  int turn = 0;
+  for (int64_t r0 = (int64_t)blockIdx.x * kRows; r0 < a.rows; r0 += (int64_t)gridDim.x * kRows, ++turn) {
+    const int64_t row = r0 + sub;
+    const bool here = row < a.rows;
+    const uint8_t *g = (const uint8_t*)a.G + row * a.ldg * ELT, *h = (const uint8_t*)a.H + row * a.ldh * ELT,
+                  *q = (const uint8_t*)a.P + row * a.ldp * ELT;
+    typename Row::Raw rg[C] = {}, rh[C] = {}, rp[C] = {};
+    if (here) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) rg[c] = p.load(g, c);
+#pragma unroll
+      for (int c = 0; c < C; ++c) rh[c] = p.load(h, c);
+      if (a.P)
+#pragma unroll
+        for (int c = 0; c < C; ++c) rp[c] = p.load(q, c);
+    }
+    float s[2] = {0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      float vg[N], vh[N], vw[N];
+      Row::floats(rg[c], vg);
+      Row::floats(rh[c], vh);
+      Row::floats(rw[c], vw);
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        s[0] = fmaf(vh[e], vh[e], s[0]);
+        s[1] = fmaf(vg[e] * vw[e], vh[e], s[1]);
+      }
+    }
+    row_sums<T>(s, red, turn);
+    const float u = 1.f / sqrtf(s[0] / a.d + a.eps), k = u * u * (s[1] / a.d);
+    if (!here) continue;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      float vg[N], vh[N], vw[N], vp[N];
+      Row::floats(rg[c], vg);
+      Row::floats(rh[c], vh);
+      Row::floats(rw[c], vw);
+      Row::floats(rp[c], vp);
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        dw[c][e] = fmaf(vg[e], vh[e] * u, dw[c][e]);
+        vg[e] = u * fmaf(-vh[e], k, vg[e] * vw[e]);
+        if (a.P) vg[e] += vp[e];
+      }
+      p.store((uint8_t*)a.D + row * a.ldd * ELT, c, vg);
+    }
+  }
+  if (!part) return;
+  float* out = part + (int64_t)blockIdx.x * a.d;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    if constexpr (kRows > 1) {  // the rows' shares in order
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < N; ++e) share[(sub * N + e) * T + p.t] = dw[c][e];
+      __syncthreads();
+      if (sub == 0)
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          float v = share[e * T + p.t];
+#pragma unroll
+          for (int k = 1; k < kRows; ++k) v += share[(k * N + e) * T + p.t];
+          dw[c][e] = v;
+        }
+    }
+    if (sub == 0)
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (p.has(c, e)) out[p.col(c, e)] = dw[c][e];
   }
 }
 
@@ -115,21 +378,22 @@ __global__ __launch_bounds__(256) void norm_weight_kernel(NormGradArgs a, int64_
   }
 }
 
-// A wave per 64 columns and four interleaved runs of the parts.
-__global__ __launch_bounds__(256) void norm_join_kernel(const float* __restrict__ part, int n_parts, int cols,
-                                                        float* __restrict__ out, int accumulate) {
-  __shared__ float red[4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+// 32 columns per workgroup and 32 interleaved runs of the parts.
+__global__ __launch_bounds__(1024) void norm_join_kernel(const float* __restrict__ part, int n_parts, int cols,
+                                                         float* __restrict__ out, int accumulate) {
+  __shared__ float red[32][33];
+  const int lane = threadIdx.x & 31, run = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
   float s = 0.f;
   if (c < cols)
-#pragma unroll 4
-    for (int y = wave; y < n_parts; y += 4) s += part[(int64_t)y * cols + c];
-  red[wave][lane] = s;
+#pragma unroll 8
+    for (int y = run; y < n_parts; y += 32) s += part[(int64_t)y * cols + c];
+  red[run][lane] = s;
   __syncthreads();
-  if (wave == 0 && c < cols) {
-    s = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
-    out[c] = accumulate ? out[c] + s : s;
-  }
+  const int at = threadIdx.x >> 5, w = blockIdx.x * 32 + at;  // column `at`, summed by 32 lanes
+  s = red[lane][at];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor(s, o);
+  if (lane == 0 && w < cols) out[w] = accumulate ? out[w] + s : s;
 }
 
 // A wave per group of a row.
@@ -174,17 +438,68 @@ __global__ __launch_bounds__(256) void quantize_weight_kernel(const void* __rest
       Q[(r0 + r) * ldq + c] = (uint8_t)pack8<false>(over_scale(load_elt<ELT>(W, (r0 + r) * ldw + c), s, inv), 0.f, 0);
 }
 
-hipError_t launch_rms_norm(int elt, const NormArgs& a, hipStream_t s) {
+namespace {
+
+// Pieces of a row.
+int64_t pieces_of(int elt, bool vec, int64_t d) { return vec ? d / (16 / elt) : (d + kGroup8 - 1) / kGroup8 * 64; }
+
+// f(T, C) with the threads and pieces per thread that hold rows of n pieces, T
+// at least `least`; false if none do.
+template <class F>
+bool with_shape(int64_t n, int least, F f) {
+  auto fits = [&](int t, int c) { return t >= least && n <= (int64_t)t * c; };
+#define SHAPE(T, C) \
+  if (fits(T, C)) return f(std::integral_constant<int, T>{}, std::integral_constant<int, C>{}), true
+  SHAPE(64, 2);
+  SHAPE(64, 4);
+  SHAPE(64, 8);
+  SHAPE(256, 2);
+  SHAPE(256, 4);
+  SHAPE(256, 8);
+  SHAPE(1024, 8);
+#undef SHAPE
+  return false;
+}
+
+bool on(const void* p, int64_t ld, int elt, int bytes) {
+  return !p || ((uintptr_t)p % bytes == 0 && ld * elt % bytes == 0);
+}
+
+template <int ELT, bool VEC>
+hipError_t launch_norm_as(const NormArgs& a, hipStream_t s) {
+  hipError_t e = hipSuccess;
+  const int64_t n = pieces_of(ELT, VEC, a.d);
+  const bool held = with_shape(n, a.rows < 2048 && n > 64 ? 256 : 64, [&](auto T, auto C) {
+    constexpr int t = decltype(T)::value, rows = t > 256 ? 1 : 256 / t;
+    dim3 grid;
+    if ((e = row_grid((a.rows + rows - 1) / rows, &grid, t > 256 ? t : 256)) != hipSuccess) return;
+    hipLaunchKernelGGL((rms_norm_kernel<ELT, VEC, t, decltype(C)::value>), grid, dim3(t > 256 ? t : 256), 0, s, a);
+    e = hipGetLastError();
+  });
+  if (held) return e;
   dim3 grid;
-  const hipError_t e = row_grid(a.rows, &grid);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(elt == 2 ? rms_norm_long_kernel<2> : rms_norm_long_kernel<4>, grid, dim3(256), 0, s, a);
+  if ((e = row_grid(a.rows, &grid)) != hipSuccess) return e;
+  hipLaunchKernelGGL((rms_norm_long_kernel<ELT>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rms_norm(int elt, const NormArgs& a, hipStream_t s) {
+  const bool vec = a.d % (16 / elt) == 0 && on(a.X, a.ldx, elt, 16) && on(a.R, a.ldr, elt, 16) && on(a.W, 0, elt, 16) &&
+                   on(a.Y, a.ldy, elt, 16) && on(a.H, a.ldh, elt, 16) && on(a.Q, a.ldq, 1, 16 / elt);
+  return elt == 2 ? (vec ? launch_norm_as<2, true>(a, s) : launch_norm_as<2, false>(a, s))
+                  : (vec ? launch_norm_as<4, true>(a, s) : launch_norm_as<4, false>(a, s));
 }
 
 namespace {
 
-// Rows per part of the weight gradient, and parts: eight workgroups per CU of 64 rows or more.
+// Workgroups of the gradient where registers hold the rows: four per CU.  Whether
+// they do does not go by the buffers' alignment here, so a layout fits any.
+constexpr int kGradGroups = 1024;
+bool grad_held(int elt, int64_t d) { return pieces_of(elt, false, d) <= 1024 * 8 && d <= 1024 * 8 * (16 / elt); }
+
+// Rows per part of a long row's weight gradient, and parts: eight workgroups per CU of 64 rows or more.
 void weight_shape(int64_t rows, int64_t d, int64_t* per, int64_t* parts) {
   const int64_t p = std::max<int64_t>(1, std::min<int64_t>(2048 / ((d + 63) / 64), rows / 64));
   *per = std::max<int64_t>(1, (rows + p - 1) / p);
@@ -193,9 +508,13 @@ void weight_shape(int64_t rows, int64_t d, int64_t* per, int64_t* parts) {
 
 }  // namespace
 
-NormGradLayout norm_grad_layout(int64_t rows, int64_t d, bool weight) {
+NormGradLayout norm_grad_layout(int elt, int64_t rows, int64_t d, bool weight) {
   NormGradLayout l = {};
   if (!weight) return l;
+  if (grad_held(elt, d)) {
+    l.total = align_up((size_t)std::min<int64_t>(kGradGroups, rows) * d * 4);
+    return l;
+  }
   int64_t per, parts;
   weight_shape(rows, d, &per, &parts);
   l.off_part = align_up((size_t)rows * 4);
@@ -203,7 +522,41 @@ NormGradLayout norm_grad_layout(int64_t rows, int64_t d, bool weight) {
   return l;
 }
 
+namespace {
+
+hipError_t join(const float* part, int64_t parts, int64_t d, float* dw, bool accumulate, hipStream_t s) {
+  hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)((d + 31) / 32)), dim3(1024), 0, s, part, (int)parts, (int)d, dw,
+                     (int)accumulate);
+  return hipGetLastError();
+}
+
+template <int ELT, bool VEC>
+hipError_t launch_grad_as(const NormGradArgs& a, float* dw, bool accumulate, uint8_t* ws, hipStream_t s) {
+  hipError_t e = hipSuccess;
+  int64_t groups = 0;
+  with_shape(pieces_of(ELT, VEC, a.d), 64, [&](auto T, auto C) {
+    constexpr int t = decltype(T)::value, rows = t > 256 ? 1 : 256 / t;
+    groups = std::min<int64_t>(kGradGroups, (a.rows + rows - 1) / rows);
+    if (groups == 0) return;
+    hipLaunchKernelGGL((norm_grad_kernel<ELT, VEC, t, decltype(C)::value>), dim3((unsigned)groups),
+                       dim3(t > 256 ? t : 256), 0, s, a, dw ? (float*)ws : nullptr);
+    e = hipGetLastError();
+  });
+  if (e != hipSuccess || !dw) return e;
+  return join((const float*)ws, groups, a.d, dw, accumulate, s);
+}
+
+}  // namespace
+
 hipError_t launch_norm_grad(int elt, NormGradArgs a, float* dw, bool accumulate, uint8_t* ws, hipStream_t s) {
+  if (grad_held(elt, a.d)) {
+    const bool vec = a.d % (16 / elt) == 0 && on(a.G, a.ldg, elt, 16) && on(a.H, a.ldh, elt, 16) &&
+                     on(a.W, 0, elt, 16) && on(a.P, a.ldp, elt, 16) && on(a.D, a.ldd, elt, 16);
+    return elt == 2 ? (vec ? launch_grad_as<2, true>(a, dw, accumulate, ws, s)
+                           : launch_grad_as<2, false>(a, dw, accumulate, ws, s))
+                    : (vec ? launch_grad_as<4, true>(a, dw, accumulate, ws, s)
+                           : launch_grad_as<4, false>(a, dw, accumulate, ws, s));
+  }
   hipError_t e;
   a.U = dw ? (float*)ws : nullptr;
   if (a.rows > 0) {
@@ -215,13 +568,12 @@ hipError_t launch_norm_grad(int elt, NormGradArgs a, float* dw, bool accumulate,
   if (!dw) return hipSuccess;
   int64_t per, parts;
   weight_shape(a.rows, a.d, &per, &parts);
-  float* part = (float*)(ws + norm_grad_layout(a.rows, a.d, true).off_part);
-  const unsigned strips = (unsigned)((a.d + 63) / 64);
-  hipLaunchKernelGGL(elt == 2 ? norm_weight_kernel<2> : norm_weight_kernel<4>, dim3(strips, (unsigned)parts), dim3(256),
-                     0, s, a, per, parts > 1 ? part : dw, parts > 1 ? 0 : (int)accumulate);
+  float* part = (float*)(ws + norm_grad_layout(elt, a.rows, a.d, true).off_part);
+  hipLaunchKernelGGL(elt == 2 ? norm_weight_kernel<2> : norm_weight_kernel<4>,
+                     dim3((unsigned)((a.d + 63) / 64), (unsigned)parts), dim3(256), 0, s, a, per,
+                     parts > 1 ? part : dw, parts > 1 ? 0 : (int)accumulate);
   if ((e = hipGetLastError()) != hipSuccess || parts == 1) return e;
-  hipLaunchKernelGGL(norm_join_kernel, dim3(strips), dim3(256), 0, s, part, (int)parts, (int)a.d, dw, (int)accumulate);
-  return hipGetLastError();
+  return join(part, parts, a.d, dw, accumulate, s);
 }
 
 hipError_t launch_quantize_rows(int elt, const void* X, int64_t ldx, int64_t rows, int64_t d, uint8_t* Q, int64_t ldq,
