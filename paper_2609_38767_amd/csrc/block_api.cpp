@@ -206,7 +206,7 @@ dattri_status dattri_linear_scaled_workspace_bytes(int64_t rows, int64_t d_in, i
   int elt;
   if (!bytes) return fail(DATTRI_E_INVALID_ARG, "bytes is NULL");
   TRY(check_product(rows, d_in, d_out, dtype, &elt));
-  *bytes = linear8_workspace_need(rows, d_in, d_out, aligned != 0);
+  *bytes = linear8_workspace_need(rows, d_in, d_out, elt, aligned != 0);
   return DATTRI_OK;
 }
 
@@ -226,7 +226,7 @@ dattri_status dattri_linear_scaled(const void* X, int64_t ld_x, const float* SX,
   TRY(check_rows("Z", Z, &ld_z, rows, d_out, elt, false));
   TRY(check_bias("bias", bias, elt));
   const bool aligned = on_16(X, ld_x, W, ld_w, 1);
-  const size_t need = linear8_workspace_need(rows, d_in, d_out, aligned);
+  const size_t need = linear8_workspace_need(rows, d_in, d_out, elt, aligned);
   TRY(check_workspace(workspace, ws_bytes, need));
   {
     const Span x("X", X, rows, d_in, ld_x, 1), sx("SX", SX, rows, groups_of(d_in), ld_sx, 4),

@@ -40,27 +40,6 @@ __global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void gemm_kernel(GemmAr
                                                     part + (int64_t)blockIdx.y * a.M * ld_part, ld_part);
 }
 
-// Sums of a split product's partial tiles in split order, and the epilogue.
-template <int OP, int ELT>
-__global__ __launch_bounds__(256) void gemm_join_kernel(GemmArgs a, const float* __restrict__ part, int64_t ld_part,
-                                                        int splits) {
-  const int nv = (a.N + 3) / 4;
-  const int64_t total = (int64_t)a.M * nv, step = (int64_t)a.M * ld_part;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const int m = (int)(i / nv), n = (int)(i - (int64_t)m * nv) * 4;
-    const float* p = part + m * ld_part + n;
-    f32x4 s = *(const f32x4*)p;
-    int y = 1;
-    for (; y + 3 < splits; y += 4) {
-      const f32x4 v0 = *(const f32x4*)(p + y * step), v1 = *(const f32x4*)(p + (y + 1) * step),
-                  v2 = *(const f32x4*)(p + (y + 2) * step), v3 = *(const f32x4*)(p + (y + 3) * step);
-      s = (((s + v0) + v1) + v2) + v3;
-    }
-    for (; y < splits; ++y) s += *(const f32x4*)(p + y * step);
-    epilogue4<OP, ELT>(a, m, n, s);
-  }
-}
-
 // Column sums over rows [y * per, (y + 1) * per): a wave owns 64 C columns, C
 // neighbours per lane, and every fourth row of the range; the waves' sums are
 // added in wave order.  8192 x 14336 bf16 (235 MB): one column per lane took 80

@@ -18,11 +18,15 @@
 // results would show it (3e-5 of a sum of 16 products): there the values go to
 // bf16, which holds them exactly, and to bf16's instructions, whose products and
 // sums keep all of float32, at half the rate.
+#include <algorithm>
+#include <type_traits>
+
 #include "api_common.h"
 #include "device_common.h"
 #include "eight.h"
 #include "epilogue.h"
 #include "internal.h"
+#include "linear8_shape.h"
 #include "linear_tile.h"
 #include "model_ops.h"
 
@@ -56,6 +60,35 @@ __device__ inline f32x4 block_dot(i32x4 w0, i32x4 w1, i32x4 x0, i32x4 x1) {
   return mfma_bf16_16(widen8(w1.z, w1.w), widen8(x1.z, x1.w), s);
 }
 
+// A 32-row block of a stage: two halves of 64 k, lane l: row l % 32, and of each
+// half chunks l / 32 and 2 + l / 32.
+struct Block8 {
+  i32x8 k[2];
+};
+template <class S>
+__device__ DATTRI_INLINE inline Block8 read_block(const uint8_t* buf, int w0, int lane, int i) {
+  const i32x4 a = S::template read<0>(buf, w0, lane, i), b = S::template read<1>(buf, w0, lane, i),
+              c = S::template read<2>(buf, w0, lane, i), d = S::template read<3>(buf, w0, lane, i);
+  return Block8{{i32x8{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}, i32x8{c.x, c.y, c.z, c.w, d.x, d.y, d.z, d.w}}};
+}
+// Sum over 128 k of a 32 x 32 block, from zero.
+template <int ELT>
+__device__ DATTRI_INLINE inline f32x16 block_sum(const Block8& w, const Block8& x) {
+  f32x16 s = {};
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if constexpr (ELT == 2) {
+      s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w.k[h], x.k[h], s, 0, 0, 0, 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 8; q += 2)
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8(w.k[h][q], w.k[h][q + 1]),
+                                                    widen8(x.k[h][q], x.k[h][q + 1]), s, 0, 0, 0);
+    }
+  }
+  return s;
+}
+
 }  // namespace
 
 template <int ELT>
@@ -84,32 +117,186 @@ __global__ __launch_bounds__(256) void linear8_few_kernel(GemmArgs a, Scales8 sc
   if (m0 + r16 < a.M && n < a.N) epilogue4<DATTRI_LINEAR_FORWARD, ELT>(a, m0 + r16, n, sum);
 }
 
+// Tiles: WM x WN waves with BM x BN blocks of 32 x 32 each, stages of 128 bytes of
+// k (one group of scales) in two buffers, rows and scales by direct loads.  At
+// the last block column of a stage everything of it is in registers: its buffer
+// takes the loads of the stage after the next, which have a whole stage to
+// arrive, and the next stage's first fragments are read between its products.  A
+// block's products start from zero; while the next block's run, the fma of its 16
+// sums with the two scales' product joins them to the accumulators.
+template <int OP, int ELT, int WM, int WN, int BM, int BN>
+__global__ __launch_bounds__(WM* WN * 64) void linear8_kernel(GemmArgs a, Scales8 sc, int nm, int nn, int sps,
+                                                              float* __restrict__ part, int64_t ld_part) {
+  constexpr int TM = WM * BM * 32, TN = WN * BN * 32, kWaves = WM * WN;
+  static_assert(TM / 64 < kWaves && BN * 32 <= 128 && 128 % (BN * 32) == 0 && BM * BN % 2 == 0, "tile shape");
+  typedef tile::Side<1, true, TM, 128, kWaves> SA;
+  typedef tile::Side<1, true, TN, 128, kWaves> SB;
+  constexpr int kRowBytes = SA::kBytes + SB::kBytes, kStage = kRowBytes + TM * 4 + 256;
+  constexpr int kSlab = 32 * TN * 4;
+  constexpr int kBuf = std::max(kStage, WM * kSlab);
+  __shared__ __align__(1024) uint8_t x0[kBuf], x1[kBuf];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / WN, wn = wave % WN, l32 = lane & 31;
+  const int64_t at = (int64_t)blockIdx.z * gridDim.x + blockIdx.x;
+  if (at >= (int64_t)nm * nn) return;
+  int mt, nt;
+  tile::tile_of((int)at, nm, nn, &mt, &nt);
+  const int m0 = mt * TM, n0 = nt * TN;
+  const int all = (int)(((int64_t)a.K + 127) / 128), s0 = blockIdx.y * sps, ns = min(sps, all - s0);
+  const int k_end = (int)min((int64_t)a.K, (int64_t)(s0 + ns) * 128);
+  SA sa;
+  SB sb;
+  sa.init(a.A, a.lda, m0, a.M, k_end, wave, lane);
+  sb.init(a.B, a.ldb, n0, a.N, k_end, wave, lane);
+
+  // Scales of a stage: the first TM / 64 waves load those of 64 rows each, the
+  // others those of the tile's blocks of 128 columns.  Rows past the last repeat it.
+  const bool of_x = wave < TM / 64;
+  const float* const sbase = of_x ? sc.x + (int64_t)m0 * sc.ldx : sc.w + (int64_t)(n0 / kGroup8) * sc.ldw;
+  const int srows = of_x ? min(TM, a.M - m0) : (min(TN, a.N - n0) + kGroup8 - 1) / kGroup8;
+  const uint32_t sld = (uint32_t)((of_x ? sc.ldx : sc.ldw) * 4);
+  const uint32_t soff = (uint32_t)min(of_x ? wave * 64 + lane : lane, srows - 1) * sld;
+  const int sat = kRowBytes + (of_x ? wave * 256 : TM * 4);
+  auto issue = [&](int st, uint8_t* x) DATTRI_INLINE {
+    const rsrc_t ra = sa.range(s0 + st), rb = sb.range(s0 + st);
+    const rsrc_t rs = make_rsrc(sbase + s0 + st, st < ns ? (uint32_t)(srows - 1) * sld + 4 : 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, DATTRI_LDS_PTR(x + sat), 4, soff, 0, 0, 0);
+    tile::unrolled<SA::kLoads>([&](auto J) DATTRI_INLINE { sa.load(ra, s0 + st, x, wave, decltype(J)::value); });
+    tile::unrolled<SB::kLoads>(
+        [&](auto J) DATTRI_INLINE { sb.load(rb, s0 + st, x + SA::kBytes, wave, decltype(J)::value); });
+  };
+
+  f32x16 acc[BN][BM], sum[2];
+#pragma unroll
+  for (int v = 0; v < 16; ++v) {
+    sum[0][v] = sum[1][v] = 0.f;
+#pragma unroll
+    for (int i = 0; i < BN; ++i)
+#pragma unroll
+      for (int j = 0; j < BM; ++j) acc[i][j][v] = 0.f;
+  }
+  Block8 fa[2], fb[BN];
+  float s[2][BM] = {}, before = 0.f;  // scales of even and odd stages; of the block whose sums wait
+  auto read_a = [&](const uint8_t* x, int j) DATTRI_INLINE { return read_block<SA>(x, wm * BM * 32, lane, j); };
+  auto read_b = [&](const uint8_t* x, int i) DATTRI_INLINE {
+    return read_block<SB>(x + SA::kBytes, wn * BN * 32, lane, i);
+  };
+  auto read_scales = [&](const uint8_t* x, float (&to)[BM]) DATTRI_INLINE {
+    const float w = *(const float*)(x + kRowBytes + TM * 4 + (wn * BN * 32 / kGroup8) * 4);
+#pragma unroll
+    for (int j = 0; j < BM; ++j) to[j] = w * *(const float*)(x + kRowBytes + (wm * BM * 32 + j * 32 + l32) * 4);
+  };
+  // Stage st (in cx; P: its parity); the stage after it comes to nx.
+  auto stage = [&](auto P, int st, uint8_t* cx, const uint8_t* nx) DATTRI_INLINE {
+    constexpr int kP = decltype(P)::value;
+    tile::unrolled<BM>([&](auto J) DATTRI_INLINE {
+      constexpr int j = decltype(J)::value, slot = (j + kP * BM) & 1;
+      if constexpr (j + 1 < BM) {
+        fa[1 - slot] = read_a(cx, j + 1);
+      } else {
+        wait_vmcnt_dma<0>();  // the next stage has landed
+        tile::stage_barrier();
+        issue(st + 2, cx);
+        fa[1 - slot] = read_a(nx, 0);
+        read_scales(nx, s[1 - kP]);
+      }
+      tile::unrolled<BN>([&](auto I) DATTRI_INLINE {
+        constexpr int i = decltype(I)::value, b = j * BN + i;
+        sum[b & 1] = block_sum<ELT>(fb[i], fa[slot]);
+        if constexpr (j + 1 == BM) fb[i] = read_b(nx, i);
+        // the block before this one (in front of the first: zeros)
+        constexpr int pj = b ? (b - 1) / BN : BM - 1, pi = b ? (b - 1) % BN : BN - 1;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[pi][pj][v] = fmaf(sum[1 - (b & 1)][v], before, acc[pi][pj][v]);
+        before = s[kP][j];
+      });
+    });
+  };
+  if (ns > 0) {
+    issue(0, x0);
+    issue(1, x1);
+    wait_vmcnt_dma<SA::kLoads + SB::kLoads + 1>();
+    tile::plain_barrier();
+    fa[0] = read_a(x0, 0);
+    read_scales(x0, s[0]);
+#pragma unroll
+    for (int i = 0; i < BN; ++i) fb[i] = read_b(x0, i);
+    for (int st = 0; st < ns; st += 2) {  // an odd number of stages ends in one of zeros
+      stage(std::integral_constant<int, 0>{}, st, x0, x1);
+      stage(std::integral_constant<int, 1>{}, st + 1, x1, x0);
+    }
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[BN - 1][BM - 1][v] = fmaf(sum[1][v], before, acc[BN - 1][BM - 1][v]);
+    tile::wait_all();
+  }
+  tile::finish_tile<OP, ELT, WM, WN, BM, BN>(a, acc, m0, n0, part + (int64_t)blockIdx.y * a.M * ld_part, ld_part,
+                                             [&](int j, int wm) { return (j & 1 ? x1 : x0) + wm * kSlab; });
+}
+
 namespace {
 
 struct Layout8 {
-  bool pack_x, pack_w;
-  size_t off_x, off_w, total;
+  bool pack;
+  size_t off_x, off_w, off_part, total;
+  Shape8 g;
 };
-Layout8 layout8(int64_t rows, int64_t d_in, int64_t d_out, bool aligned) {
+Layout8 layout8(int64_t rows, int64_t d_in, int64_t d_out, int elt, bool aligned) {
   Layout8 l = {};
-  l.pack_x = l.pack_w = !aligned || d_in % 16;
+  l.pack = !aligned || d_in % 16;
   const int64_t w = (d_in + 15) / 16 * 16;
-  l.off_w = align_up(l.pack_x ? (size_t)rows * w : 0);
-  l.total = l.off_w + align_up(l.pack_w ? (size_t)d_out * w : 0);
+  l.off_w = align_up(l.pack ? (size_t)rows * w : 0);
+  l.off_part = l.off_w + align_up(l.pack ? (size_t)d_out * w : 0);
+  l.g = shape8(std::max<int64_t>(rows, 1), d_out, d_in, elt);
+  l.total = l.off_part + align_up(l.g.splits > 1 ? (size_t)l.g.splits * rows * ((d_out + 3) / 4 * 4) * 4 : 0);
   return l;
+}
+
+template <int ELT, int WM, int WN, int BM, int BN>
+hipError_t launch_tiles(const GemmArgs& a, const Scales8& sc, const Shape8& g, float* part, int64_t ldp, hipStream_t s) {
+  constexpr int kThreads = WM * WN * 64;
+  if (g.nm * g.nn > INT32_MAX) return hipErrorInvalidValue;
+  dim3 grid(1, g.splits);
+  hipError_t e = row_grid(g.nm * g.nn, &grid, kThreads, true);
+  if (e != hipSuccess) return e;
+  if (g.splits == 1) {
+    hipLaunchKernelGGL((linear8_kernel<DATTRI_LINEAR_FORWARD, ELT, WM, WN, BM, BN>), grid, dim3(kThreads), 0, s, a, sc,
+                       (int)g.nm, (int)g.nn, g.sps, part, ldp);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((linear8_kernel<tile::kPartial, ELT, WM, WN, BM, BN>), grid, dim3(kThreads), 0, s, a, sc,
+                     (int)g.nm, (int)g.nn, g.sps, part, ldp);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  const int64_t quads = (int64_t)a.M * (ldp / 4);
+  hipLaunchKernelGGL((tile::gemm_join_kernel<DATTRI_LINEAR_FORWARD, ELT>),
+                     dim3((unsigned)std::min<int64_t>((quads + 255) / 256, 16384)), dim3(256), 0, s, a, part, ldp,
+                     g.splits);
+  return hipGetLastError();
+}
+
+template <int ELT>
+hipError_t launch_product(const GemmArgs& a, const Scales8& sc, const Shape8& g, float* part, hipStream_t s) {
+  const int64_t ldp = (a.N + 3) / 4 * 4;
+  if (g.v == kMid) return launch_tiles<ELT, 2, 2, 2, 2>(a, sc, g, part, ldp, s);
+  if (g.v == kSlim) return launch_tiles<ELT, 2, 2, 1, 2>(a, sc, g, part, ldp, s);
+  if constexpr (ELT == 2)
+    if (g.v == kBig) return launch_tiles<ELT, 2, 4, 4, 2>(a, sc, g, part, ldp, s);
+  const unsigned mb = (unsigned)(((int64_t)a.M + 15) / 16), my = std::min(mb, 65535u);
+  hipLaunchKernelGGL(linear8_few_kernel<ELT>, dim3((unsigned)((a.N + 63) / 64), my, (mb + my - 1) / my), dim3(256), 0,
+                     s, a, sc);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-size_t linear8_workspace_need(int64_t rows, int64_t d_in, int64_t d_out, bool aligned) {
-  return layout8(rows, d_in, d_out, aligned).total;
+size_t linear8_workspace_need(int64_t rows, int64_t d_in, int64_t d_out, int elt, bool aligned) {
+  return layout8(rows, d_in, d_out, elt, aligned).total;
 }
 
 hipError_t launch_linear8(int elt, bool aligned, GemmArgs a, const Scales8& sc, uint8_t* ws, hipStream_t s) {
-  const Layout8 l = layout8(a.M, a.K, a.N, aligned);
+  const Layout8 l = layout8(a.M, a.K, a.N, elt, aligned);
   auto on4 = [&](const void* p, int64_t ld) { return !p || ((uintptr_t)p % (4 * elt) == 0 && ld % 4 == 0); };
   a.vec = on4(a.bias, 0) && on4(a.R, a.ldr) && on4(a.Z, a.ldz) && on4(a.out, a.ldo);
-  if (l.pack_x) {
+  if (l.pack) {
     const tile::Repack rx = tile::repack_of(&a.A, &a.lda, a.K, a.M, 1, ws + l.off_x),
                        rw = tile::repack_of(&a.B, &a.ldb, a.K, a.N, 1, ws + l.off_w);
     dim3 grid;
@@ -119,10 +306,8 @@ hipError_t launch_linear8(int elt, bool aligned, GemmArgs a, const Scales8& sc, 
     if ((e = hipGetLastError()) != hipSuccess) return e;
     a.K = (int)a.lda;
   }
-  const unsigned mb = (unsigned)(((int64_t)a.M + 15) / 16), my = std::min(mb, 65535u);
-  hipLaunchKernelGGL(elt == 2 ? linear8_few_kernel<2> : linear8_few_kernel<4>,
-                     dim3((unsigned)((a.N + 63) / 64), my, (mb + my - 1) / my), dim3(256), 0, s, a, sc);
-  return hipGetLastError();
+  float* part = (float*)(ws + l.off_part);
+  return elt == 2 ? launch_product<2>(a, sc, l.g, part, s) : launch_product<4>(a, sc, l.g, part, s);
 }
 
 }  // namespace dattri

@@ -1,0 +1,62 @@
+// How an 8-bit product is cut (host only, no HIP): form, splits of k, groups of
+// 128 k per split.
+#pragma once
+
+#include <stdint.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "linear_shape.h"
+
+namespace dattri {
+
+// kFew: the form without tiles; elt: bytes of a result.
+struct Shape8 {
+  Variant v;
+  int64_t nm, nn;
+  int splits, sps;
+};
+
+inline Shape8 shape8(int64_t M, int64_t N, int64_t K, int elt) {
+  const int64_t stages = std::max<int64_t>(1, (K + 127) / 128);
+  auto cut = [&](Variant v, int64_t splits) {
+    Shape8 g = {};
+    const int tm = v == kBig ? 256 : v == kMid ? 128 : 64, tn = v == kBig ? 256 : 128;
+    g.v = v;
+    g.nm = (M + tm - 1) / tm;
+    g.nn = (N + tn - 1) / tn;
+    splits = std::max<int64_t>(1, std::min(splits, stages / 4));
+    g.sps = (int)((stages + splits - 1) / splits);
+    if (splits > 1) g.sps = (g.sps + 1) / 2 * 2;  // both buffers
+    g.splits = (int)((stages + g.sps - 1) / g.sps);
+    return g;
+  };
+  if (M <= 16) {
+    Shape8 g = cut(kFew, 1);
+    return g;
+  }
+  if (M <= 64) return cut(kSlim, std::min<int64_t>(64, 768 / ((N + 127) / 128)));
+  // The cut with the least modelled time, as for the other products (gemm_shape).
+  const double rate[2] = {8.0e6, elt == 2 ? 5.5e6 : 3.0e6}, fixed[2] = {12., 4.};
+  Shape8 best = {};
+  double best_us = 0.;
+  for (int v = elt == 2 ? kBig : kMid; v <= kMid; ++v)
+    for (int64_t splits = 1; splits <= 32; ++splits) {
+      const Shape8 g = cut((Variant)v, splits);
+      if (g.splits != splits) continue;
+      const double each = (double)g.nm * g.nn, last = splits > 1 ? (double)stages / g.sps - (splits - 1) : 1.;
+      const bool alone = each * splits <= 256.;
+      const double rounds = alone ? 1. : std::max(1. + last, std::ceil(each * (splits - 1 + last) / 256.));
+      const int64_t side = v == kBig ? 256 : 128;
+      double us = rounds * (2. * side * side * g.sps * 128 / (rate[v] * (alone && v == kMid ? 0.8 : 1.)) + fixed[v]);
+      if (g.splits > 1) us += 3. + 8. * g.splits * M * N / 6.0e6;
+      if (best_us == 0. || us < best_us) {
+        best = g;
+        best_us = us;
+      }
+    }
+  return best;
+}
+
+}  // namespace dattri

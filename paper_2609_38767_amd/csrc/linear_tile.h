@@ -106,13 +106,14 @@ __device__ DATTRI_INLINE inline void unrolled(F f) {
 }
 
 // One operand's share of a tile: R rows (of the operand's own index) of which
-// `rows` exist, k contiguous (KC) or strided; KW bytes of k per stage.
-template <int ELT, bool KC, int R, int KW>
+// `rows` exist, k contiguous (KC) or strided; KW bytes of k per stage, loaded by
+// WAVES waves.
+template <int ELT, bool KC, int R, int KW, int WAVES = 4>
 struct Side {
   static constexpr int EPL = 16 / ELT, BK = KW / ELT;    // elements per chunk, k per stage
   static constexpr int kBytes = R * KW;                  // of a stage
   static constexpr int kPieces = kBytes / 1024;          // direct loads of 1 KiB
-  static constexpr int kLoads = kPieces > 4 ? kPieces / 4 : 1;  // per wave; two pieces: each loaded by two waves
+  static constexpr int kLoads = kPieces > WAVES ? kPieces / WAVES : 1;  // per wave; two pieces: each loaded by two waves
   static constexpr int CH = R * ELT / 16;                // chunks per k row (strided)
 
   // A direct load moves 64 chunks: kRows rows of a stage buffer (of the operand
@@ -214,6 +215,85 @@ __device__ inline void tile_of(int b, int nm, int nn, int* mt, int* nt) {
   const int r = L - g * kGroup * nn;
   *mt = m_first + r % gm;
   *nt = r / gm;
+}
+
+// The end of a tile from row m0 and column n0: the waves' sums through LDS to the
+// epilogue (OP kPartial: float32 sums to part, rows ld_part apart).  slab(j, wm):
+// 32 rows of TN float32 for block column j of a row of waves; j and j + 1 may not
+// share any, j and j + 2 may.
+template <int OP, int ELT, int WM, int WN, int BM, int BN, class Slab>
+__device__ DATTRI_INLINE inline void finish_tile(const GemmArgs& a, const f32x16 (&acc)[BN][BM], int m0, int n0,
+                                                 float* __restrict__ part, int64_t ld_part, Slab slab) {
+  constexpr int TM = WM * BM * 32, TN = WN * BN * 32, kThreads = WM * WN * 64;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / WN, wn = wave % WN;
+  // Block column j of every wave as rows of TN float32, 16-byte chunks XORed by
+  // row so that the lanes' writes (32 rows of one chunk) spread over the banks.
+  const int l32 = lane & 31, h = lane >> 5;
+  constexpr int LPR = TN / 4;  // lanes per row in the epilogue
+  constexpr int kRows = 4;     // rows a thread takes at once (a slab holds whole rounds of them)
+  static_assert(WM * 32 % (kThreads / LPR * kRows) == 0, "slab rows");
+  const int c = tid % LPR;
+#pragma unroll
+  for (int j = 0; j < BM; ++j) {
+    uint8_t *const y0 = slab(j, 0), *const y1 = slab(j, 1);  // of the rows of waves
+    if (j == 0) stage_barrier();  // the last stage's reads are done; the buffers of j - 2 are by the barrier below
+#pragma unroll
+    for (int i = 0; i < BN; ++i)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int c = (wn * BN + i) * 8 + 2 * v + h;
+        *(f32x4*)((wm ? y1 : y0) + l32 * (TN * 4) + ((c ^ (l32 & 15)) << 4)) =
+            f32x4{acc[i][j][4 * v], acc[i][j][4 * v + 1], acc[i][j][4 * v + 2], acc[i][j][4 * v + 3]};
+      }
+    stage_barrier();
+    // row r of the slab is row (r / 32) * 32 BM + 32 j + r % 32 of the tile
+    auto tile_row = [&](int row) { return (row >> 5) * (BM * 32) + 32 * j + (row & 31); };
+    auto value = [&](int row) {
+      return *(const f32x4*)((row & 32 ? y1 : y0) + (row & 31) * (TN * 4) + ((c ^ (row & 15)) << 4));
+    };
+    if constexpr (OP == kPartial) {
+      const TileRows<4> out(part, ld_part, m0, n0, min(TM, a.M - m0),
+                            min((int64_t)TN, ld_part - n0));
+      if (n0 + 4 * c < ld_part)
+#pragma unroll 4
+        for (int row = tid / LPR; row < WM * 32; row += kThreads / LPR)
+          buffer_store4<4, 1>(out.r, tile_row(row) * out.ld + 16 * c, value(row), 4);
+    } else {
+      const int rows = min(TM, a.M - m0), width = min(TN, a.N - n0);
+      auto finish = [&](auto take, const auto& e, auto get) {  // `take` rows at once
+        constexpr int U = decltype(take)::value;
+#pragma unroll 1
+        for (int row = tid / LPR; row < WM * 32; row += kThreads / LPR * U) {
+          int at[U];
+          f32x4 v[U];
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            at[u] = tile_row(row + u * (kThreads / LPR));
+            v[u] = get(row + u * (kThreads / LPR));
+          }
+          e.run(at, v);
+        }
+      };
+      if (a.vec && width % 4 == 0) {  // four neighbours per lane
+        if (4 * c < width)
+          finish(std::integral_constant<int, kRows>{}, TileEpilogue<OP, ELT, kRows, 1>(a, m0, n0, rows, width, 4 * c), value);
+      } else {  // rows on any element: every LPR-th column, so that lanes are neighbours
+        auto apart = [&](int row) {
+          f32x4 v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int n = c + e * LPR;
+            v[e] = *(const float*)((row & 32 ? y1 : y0) + (row & 31) * (TN * 4) + (((n >> 2) ^ (row & 15)) << 4) +
+                                   (n & 3) * 4);
+          }
+          return v;
+        };
+        if (c < width)
+          finish(std::integral_constant<int, 2>{}, TileEpilogue<OP, ELT, 2, LPR>(a, m0, n0, rows, width, c), apart);
+      }
+    }
+  }
 }
 
 // The tile from row m0 and column n0, rows and columns below a.M and a.N: stages
@@ -338,74 +418,31 @@ __device__ DATTRI_INLINE inline void tile_product(const GemmArgs& a, int m0, int
     wait_all();
   }
 
-  // Block column j of every wave as rows of TN float32, 16-byte chunks XORed by
-  // row so that the lanes' writes (32 rows of one chunk) spread over the banks.
-  const int l32 = lane & 31, h = lane >> 5;
-  constexpr int LPR = TN / 4;  // lanes per row in the epilogue
-  constexpr int kRows = 4;     // rows a thread takes at once (a slab holds whole rounds of them)
-  static_assert(WM * 32 % (256 / LPR * kRows) == 0, "slab rows");
-  const int c = tid % LPR;
-#pragma unroll
-  for (int j = 0; j < BM; ++j) {
+  finish_tile<OP, ELT, WM, WN, BM, BN>(a, acc, m0, n0, part, ld_part, [&](int j, int wm) {
     // the rows of waves: in one buffer each
-    uint8_t* const y0 = kBuffers == 4 ? (j & 1 ? x2 : x0) : (j & 1 ? x1 : x0);
-    uint8_t* const y1 = kBuffers == 4 ? (j & 1 ? x3 : x1) : y0 + kSlab;
-    if (j == 0) stage_barrier();  // the last stage's reads are done; the buffers of j - 2 are by the barrier below
-#pragma unroll
-    for (int i = 0; i < BN; ++i)
-#pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const int c = (wn * BN + i) * 8 + 2 * v + h;
-        *(f32x4*)((wm ? y1 : y0) + l32 * (TN * 4) + ((c ^ (l32 & 15)) << 4)) =
-            f32x4{acc[i][j][4 * v], acc[i][j][4 * v + 1], acc[i][j][4 * v + 2], acc[i][j][4 * v + 3]};
-      }
-    stage_barrier();
-    // row r of the slab is row (r / 32) * 32 BM + 32 j + r % 32 of the tile
-    auto tile_row = [&](int row) { return (row >> 5) * (BM * 32) + 32 * j + (row & 31); };
-    auto value = [&](int row) {
-      return *(const f32x4*)((row & 32 ? y1 : y0) + (row & 31) * (TN * 4) + ((c ^ (row & 15)) << 4));
-    };
-    if constexpr (OP == kPartial) {
-      const TileRows<4> out(part, ld_part, m0, n0, min(TM, a.M - m0),
-                            min((int64_t)TN, ld_part - n0));
-      if (n0 + 4 * c < ld_part)
-#pragma unroll 4
-        for (int row = tid / LPR; row < WM * 32; row += 256 / LPR)
-          buffer_store4<4, 1>(out.r, tile_row(row) * out.ld + 16 * c, value(row), 4);
-    } else {
-      const int rows = min(TM, a.M - m0), width = min(TN, a.N - n0);
-      auto finish = [&](auto take, const auto& e, auto get) {  // `take` rows at once
-        constexpr int U = decltype(take)::value;
-#pragma unroll 1
-        for (int row = tid / LPR; row < WM * 32; row += 256 / LPR * U) {
-          int at[U];
-          f32x4 v[U];
-#pragma unroll
-          for (int u = 0; u < U; ++u) {
-            at[u] = tile_row(row + u * (256 / LPR));
-            v[u] = get(row + u * (256 / LPR));
-          }
-          e.run(at, v);
-        }
-      };
-      if (a.vec && width % 4 == 0) {  // four neighbours per lane
-        if (4 * c < width)
-          finish(std::integral_constant<int, kRows>{}, TileEpilogue<OP, ELT, kRows, 1>(a, m0, n0, rows, width, 4 * c), value);
-      } else {  // rows on any element: every LPR-th column, so that lanes are neighbours
-        auto apart = [&](int row) {
-          f32x4 v;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int n = c + e * LPR;
-            v[e] = *(const float*)((row & 32 ? y1 : y0) + (row & 31) * (TN * 4) + (((n >> 2) ^ (row & 15)) << 4) +
-                                   (n & 3) * 4);
-          }
-          return v;
-        };
-        if (c < width)
-          finish(std::integral_constant<int, 2>{}, TileEpilogue<OP, ELT, 2, LPR>(a, m0, n0, rows, width, c), apart);
-      }
+    uint8_t* const y = kBuffers == 4 ? (j & 1 ? x2 : x0) : (j & 1 ? x1 : x0);
+    return wm ? (kBuffers == 4 ? (j & 1 ? x3 : x1) : y + kSlab) : y;
+  });
+}
+
+// Sums of a split product's partial tiles in split order, and the epilogue.
+template <int OP, int ELT>
+__global__ __launch_bounds__(256) void gemm_join_kernel(GemmArgs a, const float* __restrict__ part, int64_t ld_part,
+                                                        int splits) {
+  const int nv = (a.N + 3) / 4;
+  const int64_t total = (int64_t)a.M * nv, step = (int64_t)a.M * ld_part;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int m = (int)(i / nv), n = (int)(i - (int64_t)m * nv) * 4;
+    const float* p = part + m * ld_part + n;
+    f32x4 s = *(const f32x4*)p;
+    int y = 1;
+    for (; y + 3 < splits; y += 4) {
+      const f32x4 v0 = *(const f32x4*)(p + y * step), v1 = *(const f32x4*)(p + (y + 1) * step),
+                  v2 = *(const f32x4*)(p + (y + 2) * step), v3 = *(const f32x4*)(p + (y + 3) * step);
+      s = (((s + v0) + v1) + v2) + v3;
     }
+    for (; y < splits; ++y) s += *(const f32x4*)(p + y * step);
+    epilogue4<OP, ELT>(a, m, n, s);
   }
 }
 

@@ -83,7 +83,7 @@ struct Scales8 {
   const float *x, *w;
   int64_t ldx, ldw;
 };
-size_t linear8_workspace_need(int64_t rows, int64_t d_in, int64_t d_out, bool aligned);
+size_t linear8_workspace_need(int64_t rows, int64_t d_in, int64_t d_out, int elt, bool aligned);
 // As the forward product: A = X, B = W, one byte per element; elt is that of bias, R, Y and Z.
 hipError_t launch_linear8(int elt, bool aligned, GemmArgs a, const Scales8& sc, uint8_t* ws, hipStream_t s);
 hipError_t launch_quantize_rows(int elt, const void* X, int64_t ldx, int64_t rows, int64_t d, uint8_t* Q, int64_t ldq,
