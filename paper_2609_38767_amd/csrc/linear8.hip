@@ -65,12 +65,17 @@ __device__ inline f32x4 block_dot(i32x4 w0, i32x4 w1, i32x4 x0, i32x4 x1) {
 struct Block8 {
   i32x8 k[2];
 };
-template <class S>
-__device__ DATTRI_INLINE inline Block8 read_block(const uint8_t* buf, int w0, int lane, int i) {
-  const i32x4 a = S::template read<0>(buf, w0, lane, i), b = S::template read<1>(buf, w0, lane, i),
-              c = S::template read<2>(buf, w0, lane, i), d = S::template read<3>(buf, w0, lane, i);
-  return Block8{{i32x8{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}, i32x8{c.x, c.y, c.z, c.w, d.x, d.y, d.z, d.w}}};
+// at: this lane's four chunks of the wave's first block
+__device__ DATTRI_INLINE inline Block8 read_block(const uint8_t* buf, const uint32_t (&at)[4], int i) {
+  i32x4 c[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) c[q] = *(const i32x4*)(buf + at[q] + i * (32 * 128));
+  return Block8{{i32x8{c[0].x, c[0].y, c[0].z, c[0].w, c[1].x, c[1].y, c[1].z, c[1].w},
+                 i32x8{c[2].x, c[2].y, c[2].z, c[2].w, c[3].x, c[3].y, c[3].z, c[3].w}}};
 }
+// Keeps what is made of v inside the loop: the sums leave few registers for
+// addresses that could be formed again.
+__device__ DATTRI_INLINE inline void renew(uint32_t& v) { asm volatile("" : "+v"(v)); }
 // Sum over 128 k of a 32 x 32 block, from zero.
 template <int ELT>
 __device__ DATTRI_INLINE inline f32x16 block_sum(const Block8& w, const Block8& x) {
@@ -177,18 +182,33 @@ __global__ __launch_bounds__(WM* WN * 64) void linear8_kernel(GemmArgs a, Scales
   }
   Block8 fa[2], fb[BN];
   float s[2][BM] = {}, before = 0.f;  // scales of even and odd stages; of the block whose sums wait
-  auto read_a = [&](const uint8_t* x, int j) DATTRI_INLINE { return read_block<SA>(x, wm * BM * 32, lane, j); };
-  auto read_b = [&](const uint8_t* x, int i) DATTRI_INLINE {
-    return read_block<SB>(x + SA::kBytes, wn * BN * 32, lane, i);
-  };
+  uint32_t at_a[4], at_b[4], at_s = (wm * BM * 32 + l32) * 4;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    at_a[q] = (wm * BM * 32 + l32) * 128 + (((2 * q + (lane >> 5)) ^ SA::swz(l32)) << 4);
+    at_b[q] = SA::kBytes + (wn * BN * 32 + l32) * 128 + (((2 * q + (lane >> 5)) ^ SB::swz(l32)) << 4);
+  }
+  auto read_a = [&](const uint8_t* x, int j) DATTRI_INLINE { return read_block(x, at_a, j); };
+  auto read_b = [&](const uint8_t* x, int i) DATTRI_INLINE { return read_block(x, at_b, i); };
   auto read_scales = [&](const uint8_t* x, float (&to)[BM]) DATTRI_INLINE {
     const float w = *(const float*)(x + kRowBytes + TM * 4 + (wn * BN * 32 / kGroup8) * 4);
 #pragma unroll
-    for (int j = 0; j < BM; ++j) to[j] = w * *(const float*)(x + kRowBytes + (wm * BM * 32 + j * 32 + l32) * 4);
+    for (int j = 0; j < BM; ++j) to[j] = w * *(const float*)(x + kRowBytes + at_s + j * 128);
   };
   // Stage st (in cx; P: its parity); the stage after it comes to nx.
   auto stage = [&](auto P, int st, uint8_t* cx, const uint8_t* nx) DATTRI_INLINE {
     constexpr int kP = decltype(P)::value;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      renew(at_a[q]);
+      renew(at_b[q]);
+    }
+    renew(at_s);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      renew(sa.off[q]);
+      renew(sb.off[q]);
+    }
     tile::unrolled<BM>([&](auto J) DATTRI_INLINE {
       constexpr int j = decltype(J)::value, slot = (j + kP * BM) & 1;
       if constexpr (j + 1 < BM) {
