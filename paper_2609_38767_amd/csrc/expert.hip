@@ -11,11 +11,11 @@
 // expert with zero weights and bias.  Boundaries are clamped to the rows and to
 // each other, so wrong ones give wrong rows, never an access out of range.
 #include <algorithm>
-#include <cmath>
 
 #include "api_common.h"
 #include "device_common.h"
 #include "epilogue.h"
+#include "expert_shape.h"
 #include "internal.h"
 #include "linear_shape.h"
 #include "linear_tile.h"
@@ -233,7 +233,15 @@ hipError_t launch_tiles(const GemmArgs& a, const ExpertArgs& x, hipStream_t s) {
 
 template <int OP, int ELT>
 hipError_t launch_product(const GemmArgs& a, const ExpertArgs& x, hipStream_t s) {
-  return launch_tiles<OP, ELT, 64, 2, 2, 2, 2>(a, x, s);
+  constexpr bool AC = OP != DATTRI_LINEAR_WEIGHT_GRAD, BC = OP == DATTRI_LINEAR_FORWARD;
+  const Variant v = expert_shape(!AC, x.rows, x.experts, a.M, a.N, a.K, ELT);
+  if (v == kBig) return launch_tiles<OP, ELT, stage_bytes(AC, BC, ELT, 256), 2, 2, 4, 4>(a, x, s);
+  if (v == kMid || !AC) return launch_tiles<OP, ELT, stage_bytes(AC, BC, ELT, 128), 2, 2, 2, 2>(a, x, s);
+  if constexpr (AC) {
+    if (v == kSlim) return launch_tiles<OP, ELT, 64, 2, 2, 1, 2>(a, x, s);
+    return launch_tiles<OP, ELT, 64, 1, 4, 1, 1>(a, x, s);
+  }
+  return hipErrorInvalidValue;
 }
 
 }  // namespace

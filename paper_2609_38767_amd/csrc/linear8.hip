@@ -1,7 +1,7 @@
 // Product of 8-bit rows and 8-bit weights with a scale for every 128 of k:
 //   Z[m][n] = sum_b sx[m][b] sw[n / 128][b] sum_{k in b} X[m][k] W[n][k] + bias[n],  Y = act(Z) + R.
 //
-// Few rows: a wave owns 16 weight rows and 16 MB rows of X.  Both come straight
+// Few rows: a wave owns 16 weight rows and up to 16 rows of X.  Both come straight
 // from memory into registers: lane l holds row l % 16 and 16-byte chunks l / 16
 // and 4 + l / 16 of a block of 128 k (the same for both operands, so that every
 // product meets its own), the matrix cores sum the block from zero, and one fma
@@ -96,30 +96,56 @@ __device__ DATTRI_INLINE inline f32x16 block_sum(const Block8& w, const Block8& 
 
 }  // namespace
 
-template <int ELT>
-__global__ __launch_bounds__(256) void linear8_few_kernel(GemmArgs a, Scales8 sc) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15,
+// W waves of a workgroup share 16 weight rows and all rows of X, 16 at most: wave
+// w takes the groups of k w, w + W, ...; the waves' sums are added in their order.
+template <int ELT, int W>
+__global__ __launch_bounds__(W * 64) void linear8_few_kernel(GemmArgs a, Scales8 sc) {
+  constexpr int kAhead = 4;  // groups in flight per wave
+  __shared__ f32x4 red[W][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15,
             c = lane >> 4;
-  const int n0 = (blockIdx.x * 4 + wave) * 16, m0 = (int)(blockIdx.z * gridDim.y + blockIdx.y) * 16;
-  if (n0 >= a.N || m0 >= a.M) return;
+  const int n0 = blockIdx.x * 16, groups = (int)(((int64_t)a.K + kGroup8 - 1) / kGroup8);
   // rows past the last repeat it; their sums are not stored
-  const uint8_t* w = (const uint8_t*)a.B + (int64_t)min(n0 + r16, a.N - 1) * a.ldb;
-  const int m = min(m0 + r16, a.M - 1);
-  const uint8_t* x = (const uint8_t*)a.A + m * a.lda;
-  const float *sx = sc.x + m * sc.ldx, *sw = sc.w + (n0 / kGroup8) * sc.ldw;
-  auto piece = [&](const uint8_t* p, int k) {
-    const i32x4 z = {0, 0, 0, 0};
-    return k < a.K ? *(const i32x4*)(p + k) : z;
-  };
+  const int64_t row = min(m, a.M - 1);
+  const uint8_t *w = (const uint8_t*)a.B + (int64_t)min(n0 + m, a.N - 1) * a.ldb + 16 * c,
+                *x = (const uint8_t*)a.A + row * a.lda + 16 * c;
+  const float *sw = sc.w + (n0 / kGroup8) * sc.ldw, *sx = sc.x + row * sc.ldx;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-  for (int b = 0, k = 16 * c; b * kGroup8 < a.K; ++b, k += kGroup8) {
-    const f32x4 d = block_dot<ELT>(piece(w, k), piece(w, k + 64), piece(x, k), piece(x, k + 64));
-    const float s = sx[b] * sw[b];
+  auto take = [&](int b0, auto count) DATTRI_INLINE {
+    constexpr int U = decltype(count)::value;
+    i32x4 wv[U][2], xv[U][2];
+    float f[U];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sum[e] = fmaf(d[e], s, sum[e]);
-  }
+    for (int u = 0; u < U; ++u) {
+      const int b = b0 + u * W;
+      const int64_t k = (int64_t)b * kGroup8;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        wv[u][h] = xv[u][h] = i32x4{0, 0, 0, 0};
+        if (k + 64 * h + 16 * c < a.K) {
+          wv[u][h] = *(const i32x4*)(w + k + 64 * h);
+          xv[u][h] = *(const i32x4*)(x + k + 64 * h);
+        }
+      }
+      f[u] = sx[b] * sw[b];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const f32x4 d = block_dot<ELT>(wv[u][0], wv[u][1], xv[u][0], xv[u][1]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] = fmaf(d[e], f[u], sum[e]);
+    }
+  };
+  int b = wave;
+  for (; b + (kAhead - 1) * W < groups; b += kAhead * W) take(b, std::integral_constant<int, kAhead>{});
+  for (; b < groups; b += W) take(b, std::integral_constant<int, 1>{});
+  red[wave][lane] = sum;
+  __syncthreads();
   const int n = n0 + 4 * c;
-  if (m0 + r16 < a.M && n < a.N) epilogue4<DATTRI_LINEAR_FORWARD, ELT>(a, m0 + r16, n, sum);
+  if (wave > 0 || m >= a.M || n >= a.N) return;
+#pragma unroll
+  for (int q = 1; q < W; ++q) sum += red[q][lane];
+  epilogue4<DATTRI_LINEAR_FORWARD, ELT>(a, m, n, sum);
 }
 
 // Tiles: WM x WN waves with BM x BN blocks of 32 x 32 each, stages of 128 bytes of
@@ -293,6 +319,19 @@ hipError_t launch_tiles(const GemmArgs& a, const Scales8& sc, const Shape8& g, f
   return hipGetLastError();
 }
 
+// Waves per workgroup: eight (one row of 4096 -> 14336: 14.7 us, with four 16.6),
+// sixteen where there are too few workgroups to fill the CUs with those.
+template <int ELT>
+hipError_t launch_few(const GemmArgs& a, const Scales8& sc, hipStream_t s) {
+  const int64_t strips = ((int64_t)a.N + 15) / 16;
+  const dim3 grid((unsigned)strips);
+  if (strips >= 512 || a.K <= 8 * kGroup8)
+    hipLaunchKernelGGL((linear8_few_kernel<ELT, 8>), grid, dim3(512), 0, s, a, sc);
+  else
+    hipLaunchKernelGGL((linear8_few_kernel<ELT, 16>), grid, dim3(1024), 0, s, a, sc);
+  return hipGetLastError();
+}
+
 template <int ELT>
 hipError_t launch_product(const GemmArgs& a, const Scales8& sc, const Shape8& g, float* part, hipStream_t s) {
   const int64_t ldp = (a.N + 3) / 4 * 4;
@@ -300,10 +339,7 @@ hipError_t launch_product(const GemmArgs& a, const Scales8& sc, const Shape8& g,
   if (g.v == kSlim) return launch_tiles<ELT, 2, 2, 1, 2>(a, sc, g, part, ldp, s);
   if constexpr (ELT == 2)
     if (g.v == kBig) return launch_tiles<ELT, 2, 4, 4, 2>(a, sc, g, part, ldp, s);
-  const unsigned mb = (unsigned)(((int64_t)a.M + 15) / 16), my = std::min(mb, 65535u);
-  hipLaunchKernelGGL(linear8_few_kernel<ELT>, dim3((unsigned)((a.N + 63) / 64), my, (mb + my - 1) / my), dim3(256), 0,
-                     s, a, sc);
-  return hipGetLastError();
+  return launch_few<ELT>(a, sc, s);
 }
 
 }  // namespace

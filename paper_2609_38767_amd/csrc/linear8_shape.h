@@ -32,10 +32,7 @@ inline Shape8 shape8(int64_t M, int64_t N, int64_t K, int elt) {
     g.splits = (int)((stages + g.sps - 1) / g.sps);
     return g;
   };
-  if (M <= 16) {
-    Shape8 g = cut(kFew, 1);
-    return g;
-  }
+  if (M <= 16) return cut(kFew, 1);
   if (M <= 64) return cut(kSlim, std::min<int64_t>(64, 768 / ((N + 127) / 128)));
   // The cut with the least modelled time, as for the other products (gemm_shape).
   const double rate[2] = {8.0e6, elt == 2 ? 5.5e6 : 3.0e6}, fixed[2] = {12., 4.};
