@@ -114,7 +114,7 @@ dattri_status dattri_rms_norm_grad_workspace_bytes(int64_t rows, int64_t d, datt
   TRY(elt_of(dtype, &elt));
   TRY(check_count("rows", rows));
   TRY(check_width("d", d));
-  *bytes = norm_grad_layout(elt, rows, d, weight != 0).total;
+  *bytes = norm_grad_layout(rows, d, weight != 0).total;
   return DATTRI_OK;
 }
 
@@ -135,7 +135,7 @@ dattri_status dattri_rms_norm_grad(const void* G, int64_t ld_g, const void* H, i
   if (!W) return fail(DATTRI_E_INVALID_ARG, "W is NULL");
   TRY(check_bias("W", W, elt));
   TRY(check_bias("dW", dW, 4));
-  const size_t need = norm_grad_layout(elt, rows, d, dW != nullptr).total;
+  const size_t need = norm_grad_layout(rows, d, dW != nullptr).total;
   TRY(check_workspace(workspace, ws_bytes, need));
   {
     const Span g("G", G, rows, d, ld_g, elt), h("H", H, rows, d, ld_h, elt), w("W", W, d * elt),

@@ -149,13 +149,15 @@ __global__ __launch_bounds__(W * 64) void linear8_few_kernel(GemmArgs a, Scales8
 }
 
 // Tiles: WM x WN waves with BM x BN blocks of 32 x 32 each, stages of 128 bytes of
-// k (one group of scales) in two buffers, rows and scales by direct loads.  At
-// the last block column of a stage everything of it is in registers: its buffer
-// takes the loads of the stage after the next, which have a whole stage to
-// arrive, and the next stage's first fragments are read between its products.  A
-// block's products start from zero; while the next block's run, the fma of its 16
-// sums with the two scales' product joins them to the accumulators.
-template <int OP, int ELT, int WM, int WN, int BM, int BN>
+// k (one group of scales) in a ring of BUF buffers, rows and scales by direct
+// loads.  At the last block column of a stage everything of it is in registers:
+// its buffer takes the loads of the stage a ring further on, which have BUF - 1
+// stages to arrive, and the next stage's first fragments are read between its
+// products.  A block's products start from zero; while the next block's run, the
+// fma of its 16 sums with the two scales' product joins them to the accumulators.
+// Four buffers where a stage is short (128 x 128: 0.25 us of products against
+// loads of 1 us or more): 1531 x 1001 -> 2305 took 19.8 us with two.
+template <int OP, int ELT, int WM, int WN, int BM, int BN, int BUF>
 __global__ __launch_bounds__(WM* WN * 64) void linear8_kernel(GemmArgs a, Scales8 sc, int nm, int nn, int sps,
                                                               float* __restrict__ part, int64_t ld_part) {
   constexpr int TM = WM * BM * 32, TN = WN * BN * 32, kWaves = WM * WN;
@@ -164,8 +166,8 @@ __global__ __launch_bounds__(WM* WN * 64) void linear8_kernel(GemmArgs a, Scales
   typedef tile::Side<1, true, TN, 128, kWaves> SB;
   constexpr int kRowBytes = SA::kBytes + SB::kBytes, kStage = kRowBytes + TM * 4 + 256;
   constexpr int kSlab = 32 * TN * 4;
-  constexpr int kBuf = std::max(kStage, WM * kSlab);
-  __shared__ __align__(1024) uint8_t x0[kBuf], x1[kBuf];
+  constexpr int kBuf = std::max(kStage, BUF == 4 ? kSlab : WM * kSlab), kLoads = SA::kLoads + SB::kLoads + 1;
+  __shared__ __align__(1024) uint8_t x0[kBuf], x1[kBuf], x2[BUF == 4 ? kBuf : 16], x3[BUF == 4 ? kBuf : 16];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WN, wn = wave % WN, l32 = lane & 31;
   const int64_t at = (int64_t)blockIdx.z * gridDim.x + blockIdx.x;
@@ -221,7 +223,7 @@ __global__ __launch_bounds__(WM* WN * 64) void linear8_kernel(GemmArgs a, Scales
 #pragma unroll
     for (int j = 0; j < BM; ++j) to[j] = w * *(const float*)(x + kRowBytes + at_s + j * 128);
   };
-  // Stage st (in cx; P: its parity); the stage after it comes to nx.
+  // Stage st (in cx; P: its parity); the stage after it is in nx by its last step.
   auto stage = [&](auto P, int st, uint8_t* cx, const uint8_t* nx) DATTRI_INLINE {
     constexpr int kP = decltype(P)::value;
 #pragma unroll
@@ -240,9 +242,9 @@ __global__ __launch_bounds__(WM* WN * 64) void linear8_kernel(GemmArgs a, Scales
       if constexpr (j + 1 < BM) {
         fa[1 - slot] = read_a(cx, j + 1);
       } else {
-        wait_vmcnt_dma<0>();  // the next stage has landed
+        wait_vmcnt_dma<(BUF - 2) * kLoads>();  // the next stage has landed
         tile::stage_barrier();
-        issue(st + 2, cx);
+        issue(st + BUF, cx);
         fa[1 - slot] = read_a(nx, 0);
         read_scales(nx, s[1 - kP]);
       }
@@ -259,24 +261,39 @@ __global__ __launch_bounds__(WM* WN * 64) void linear8_kernel(GemmArgs a, Scales
     });
   };
   if (ns > 0) {
+    typedef std::integral_constant<int, 0> even_t;
+    typedef std::integral_constant<int, 1> odd_t;
     issue(0, x0);
     issue(1, x1);
-    wait_vmcnt_dma<SA::kLoads + SB::kLoads + 1>();
+    if constexpr (BUF == 4) {
+      issue(2, x2);
+      issue(3, x3);
+    }
+    wait_vmcnt_dma<(BUF - 1) * kLoads>();
     tile::plain_barrier();
     fa[0] = read_a(x0, 0);
     read_scales(x0, s[0]);
 #pragma unroll
     for (int i = 0; i < BN; ++i) fb[i] = read_b(x0, i);
-    for (int st = 0; st < ns; st += 2) {  // an odd number of stages ends in one of zeros
-      stage(std::integral_constant<int, 0>{}, st, x0, x1);
-      stage(std::integral_constant<int, 1>{}, st + 1, x1, x0);
+    for (int st = 0; st < ns; st += BUF) {  // a last round that is not full ends in stages of zeros
+      stage(even_t{}, st, x0, x1);
+      if constexpr (BUF == 4) {
+        stage(odd_t{}, st + 1, x1, x2);
+        stage(even_t{}, st + 2, x2, x3);
+        stage(odd_t{}, st + 3, x3, x0);
+      } else {
+        stage(odd_t{}, st + 1, x1, x0);
+      }
     }
 #pragma unroll
     for (int v = 0; v < 16; ++v) acc[BN - 1][BM - 1][v] = fmaf(sum[1][v], before, acc[BN - 1][BM - 1][v]);
     tile::wait_all();
   }
   tile::finish_tile<OP, ELT, WM, WN, BM, BN>(a, acc, m0, n0, part + (int64_t)blockIdx.y * a.M * ld_part, ld_part,
-                                             [&](int j, int wm) { return (j & 1 ? x1 : x0) + wm * kSlab; });
+                                             [&](int j, int wm) {
+                                               uint8_t* const y = j & 1 ? x1 : x0;
+                                               return BUF == 4 && wm ? (j & 1 ? x3 : x2) : y + wm * kSlab;
+                                             });
 }
 
 namespace {
@@ -297,7 +314,7 @@ Layout8 layout8(int64_t rows, int64_t d_in, int64_t d_out, int elt, bool aligned
   return l;
 }
 
-template <int ELT, int WM, int WN, int BM, int BN>
+template <int ELT, int WM, int WN, int BM, int BN, int BUF>
 hipError_t launch_tiles(const GemmArgs& a, const Scales8& sc, const Shape8& g, float* part, int64_t ldp, hipStream_t s) {
   constexpr int kThreads = WM * WN * 64;
   if (g.nm * g.nn > INT32_MAX) return hipErrorInvalidValue;
@@ -305,11 +322,11 @@ hipError_t launch_tiles(const GemmArgs& a, const Scales8& sc, const Shape8& g, f
   hipError_t e = row_grid(g.nm * g.nn, &grid, kThreads, true);
   if (e != hipSuccess) return e;
   if (g.splits == 1) {
-    hipLaunchKernelGGL((linear8_kernel<DATTRI_LINEAR_FORWARD, ELT, WM, WN, BM, BN>), grid, dim3(kThreads), 0, s, a, sc,
+    hipLaunchKernelGGL((linear8_kernel<DATTRI_LINEAR_FORWARD, ELT, WM, WN, BM, BN, BUF>), grid, dim3(kThreads), 0, s, a, sc,
                        (int)g.nm, (int)g.nn, g.sps, part, ldp);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((linear8_kernel<tile::kPartial, ELT, WM, WN, BM, BN>), grid, dim3(kThreads), 0, s, a, sc,
+  hipLaunchKernelGGL((linear8_kernel<tile::kPartial, ELT, WM, WN, BM, BN, BUF>), grid, dim3(kThreads), 0, s, a, sc,
                      (int)g.nm, (int)g.nn, g.sps, part, ldp);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   const int64_t quads = (int64_t)a.M * (ldp / 4);
@@ -335,10 +352,14 @@ hipError_t launch_few(const GemmArgs& a, const Scales8& sc, hipStream_t s) {
 template <int ELT>
 hipError_t launch_product(const GemmArgs& a, const Scales8& sc, const Shape8& g, float* part, hipStream_t s) {
   const int64_t ldp = (a.N + 3) / 4 * 4;
-  if (g.v == kMid) return launch_tiles<ELT, 2, 2, 2, 2>(a, sc, g, part, ldp, s);
-  if (g.v == kSlim) return launch_tiles<ELT, 2, 2, 1, 2>(a, sc, g, part, ldp, s);
+  // 128 x 128: eight waves and four buffers for bf16 results (1536 x 4096 -> 2304: 26.8 us, with four waves and two
+  // buffers 29.2); float32 results, whose stages are twice as long, the other way (16384 x 4096 -> 4096: 519 and 600)
+  if (g.v == kMid)
+    return ELT == 2 ? launch_tiles<2, 2, 4, 2, 1, 4>(a, sc, g, part, ldp, s)
+                    : launch_tiles<4, 2, 2, 2, 2, 2>(a, sc, g, part, ldp, s);
+  if (g.v == kSlim) return launch_tiles<ELT, 2, 2, 1, 2, 4>(a, sc, g, part, ldp, s);
   if constexpr (ELT == 2)
-    if (g.v == kBig) return launch_tiles<ELT, 2, 4, 4, 2>(a, sc, g, part, ldp, s);
+    if (g.v == kBig) return launch_tiles<ELT, 2, 4, 4, 2, 2>(a, sc, g, part, ldp, s);
   return launch_few<ELT>(a, sc, s);
 }
 

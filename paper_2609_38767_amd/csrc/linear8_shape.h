@@ -18,6 +18,9 @@ struct Shape8 {
   int splits, sps;
 };
 
+// Stage buffers: short stages have four.
+inline int round_of(Variant v, int elt) { return v == kSlim || (v == kMid && elt == 2) ? 4 : 2; }
+
 inline Shape8 shape8(int64_t M, int64_t N, int64_t K, int elt) {
   const int64_t stages = std::max<int64_t>(1, (K + 127) / 128);
   auto cut = [&](Variant v, int64_t splits) {
@@ -28,7 +31,7 @@ inline Shape8 shape8(int64_t M, int64_t N, int64_t K, int elt) {
     g.nn = (N + tn - 1) / tn;
     splits = std::max<int64_t>(1, std::min(splits, stages / 4));
     g.sps = (int)((stages + splits - 1) / splits);
-    if (splits > 1) g.sps = (g.sps + 1) / 2 * 2;  // both buffers
+    if (splits > 1) g.sps = round_of(v, elt) * ((g.sps + round_of(v, elt) - 1) / round_of(v, elt));
     g.splits = (int)((stages + g.sps - 1) / g.sps);
     return g;
   };

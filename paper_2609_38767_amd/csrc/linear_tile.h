@@ -463,11 +463,30 @@ __global__ __launch_bounds__(256) void repack_kernel(Repack a, Repack b) {
   const int64_t r = at < a.rows ? at : at - a.rows;
   const uint8_t* src = p.src + r * p.ld * ELT;
   uint8_t* dst = p.dst + r * p.ld_out * ELT;
+  if constexpr (ELT == 1) {
+    // 16 bytes per lane from the aligned words that hold them, shifted into place; a word is read only if some of its
+    // bytes are the row's
+    const int shift = (int)((uintptr_t)src & 3);
+    const uint32_t* words = (const uint32_t*)(src - shift);
+    const int n_words = (p.w + shift + 3) / 4;
+    for (int c = lane * 4; c * 4 < p.ld_out; c += 256) {
+      uint32_t v[5];
+#pragma unroll
+      for (int e = 0; e < 5; ++e) v[e] = c + e < n_words ? words[c + e] : 0u;
+      i32x4 o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t x = __builtin_amdgcn_alignbyte(v[e + 1], v[e], shift);
+        const int left = p.w - (c + e) * 4;  // bytes of the row in this word
+        o[e] = (int)(left >= 4 ? x : left > 0 ? x & ((1u << 8 * left) - 1u) : 0u);
+      }
+      *(i32x4*)(dst + c * 4) = o;
+    }
+    return;
+  }
 #pragma unroll 8
   for (int c = lane; c < p.ld_out; c += 64) {
-    if constexpr (ELT == 1)
-      dst[c] = c < p.w ? src[c] : (uint8_t)0;
-    else if constexpr (ELT == 2)
+    if constexpr (ELT == 2)
       ((uint16_t*)dst)[c] = c < p.w ? ((const uint16_t*)src)[c] : (uint16_t)0;
     else
       ((uint32_t*)dst)[c] = c < p.w ? ((const uint32_t*)src)[c] : 0u;

@@ -116,7 +116,7 @@ struct NormGradArgs {
 struct NormGradLayout {
   size_t off_part, total;
 };
-NormGradLayout norm_grad_layout(int elt, int64_t rows, int64_t d, bool weight);
+NormGradLayout norm_grad_layout(int64_t rows, int64_t d, bool weight);
 // dw: null or the weight's gradient
 hipError_t launch_norm_grad(int elt, NormGradArgs a, float* dw, bool accumulate, uint8_t* ws, hipStream_t s);
 

@@ -56,33 +56,60 @@ __device__ inline float over16(float v, F f) {
   v = f(v, moved(v, std::integral_constant<int, 0x141>{}));  // row_half_mirror
   return f(v, moved(v, std::integral_constant<int, 0x140>{}));  // row_mirror
 }
-__device__ inline float wave_sum(float v) {
+// Sum over T lanes, 64 at most.
+template <int T>
+__device__ inline float lanes_sum(float v) {
   v = over16(v, [](float a, float b) { return a + b; });
-  v += __shfl_xor(v, 16);
-  return v + __shfl_xor(v, 32);
+  if constexpr (T > 16) v += __shfl_xor(v, 16);
+  if constexpr (T > 32) v += __shfl_xor(v, 32);
+  return v;
 }
 
-// A thread's pieces of a row of d elements held by T threads.
+// A thread's pieces of a row of d elements held by T threads; T below 64: a wave
+// holds 64 / T rows (VEC only).
 template <int ELT, bool VEC, int T>
 struct RowOf {
   static constexpr int N = VEC ? 16 / ELT : 2;  // elements of a piece
+  static constexpr int kRows = T < 256 ? 256 / T : 1, kPerWave = T < 64 ? 64 / T : 1;  // rows of a workgroup, of a wave
+  static constexpr int kThreads = T > 256 ? T : 256;
+  static_assert(T >= (VEC ? kGroup8 / N : 64), "a group of 8-bit values in one row's lanes");
   typedef std::conditional_t<VEC, i32x4, i32x2> Raw;
-  int t, d;
+  int t, sub, d;  // place in the row, row of the wave
+  __device__ explicit RowOf(int d_) : t(threadIdx.x % T), sub(T < 64 ? (threadIdx.x & 63) / T : 0), d(d_) {}
+  // The wave's first row of the workgroup's rows from r0.
+  __device__ static int64_t first(int64_t r0) {
+    return r0 + (T < 256 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 64 / T : 0);
+  }
   // Column of element e of piece c.  VEC: N neighbours per lane; else 64 apart, lanes neighbours.
   __device__ int col(int c, int e) const {
     return VEC ? (c * T + t) * N + e : (c * (T / 64) + (t >> 6)) * kGroup8 + (t & 63) + 64 * e;
   }
-  __device__ bool has(int c, int e = 0) const { return col(c, e) < d; }
-  __device__ Raw load(const void* row, int c) const {
-    Raw r = {};
-    if constexpr (VEC) {
-      if (has(c)) r = *(const i32x4*)((const uint8_t*)row + (int64_t)col(c, 0) * ELT);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-        if (has(c, e)) r[e] = ELT == 2 ? ((const uint16_t*)row)[col(c, e)] : ((const int32_t*)row)[col(c, e)];
-    }
-    return r;
+  // The wave's rows as a buffer that ends with the last one: what lies behind
+  // reads as zero and is not written.  (Rows of their own end at d by themselves;
+  // where several share a buffer the column is looked at.)
+  struct Buffer {
+    rsrc_t r;
+    uint32_t row;
+  };
+  __device__ Buffer buffer(const void* p, int64_t row0, int64_t ld, int64_t rows, int elt = ELT) const {
+    const uint32_t stride = (uint32_t)(ld * elt);
+    const int n = kPerWave > 1 ? (int)min((int64_t)kPerWave, rows - row0) : 1;
+    return Buffer{make_rsrc((const uint8_t*)p + row0 * ld * elt, (uint32_t)(n - 1) * stride + (uint32_t)d * elt),
+                  kPerWave > 1 ? sub * stride : 0};
+  }
+  __device__ uint32_t at(const Buffer& b, int c, int e, int elt = ELT) const {
+    const uint32_t o = b.row + (uint32_t)col(c, e) * elt;
+    return kPerWave > 1 && col(c, e) >= d ? kOOB : o;
+  }
+  // ONCE: past the caches
+  template <bool ONCE = false>
+  __device__ Raw load(const Buffer& b, int c) const {
+    constexpr int kAux = ONCE ? 2 : 0;  // non-temporal
+    if constexpr (VEC)
+      return __builtin_amdgcn_raw_buffer_load_b128(b.r, at(b, c, 0), 0, kAux);
+    else
+      return i32x2{(int)(ELT == 2 ? load2(b.r, at(b, c, 0)) : load4(b.r, at(b, c, 0))),
+                   (int)(ELT == 2 ? load2(b.r, at(b, c, 1)) : load4(b.r, at(b, c, 1)))};
   }
   __device__ static void floats(Raw r, float (&v)[N]) {
     if constexpr (!VEC) {
@@ -103,23 +130,26 @@ struct RowOf {
       v[3] = f.w;
     }
   }
-  __device__ void store(void* row, int c, const float (&v)[N]) const {
+  __device__ void store(const Buffer& b, int c, const float (&v)[N]) const {
     if constexpr (!VEC) {
 #pragma unroll
       for (int e = 0; e < 2; ++e)
-        if (has(c, e)) store_elt<ELT>(row, col(c, e), v[e]);
-    } else if (has(c)) {
+        if constexpr (ELT == 2)
+          __builtin_amdgcn_raw_buffer_store_b16((short)pack_bf16(v[e], 0.f), b.r, at(b, c, e), 0, 0);
+        else
+          __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(int, (float)v[e]), b.r, at(b, c, e), 0, 0);
+    } else {
       i32x4 w;
       if constexpr (ELT == 2)
         w = i32x4{(int)pack_bf16(v[0], v[1]), (int)pack_bf16(v[2], v[3]), (int)pack_bf16(v[4], v[5]),
                   (int)pack_bf16(v[6], v[7])};
       else
         w = __builtin_bit_cast(i32x4, f32x4{v[0], v[1], v[2], v[3]});
-      *(i32x4*)((uint8_t*)row + (int64_t)col(c, 0) * ELT) = w;
+      __builtin_amdgcn_raw_buffer_store_b128(w, b.r, at(b, c, 0), 0, 0);
     }
   }
-  // The piece in 8 bits: values to q, the group's scale to s (both of the row).
-  __device__ void store8(uint8_t* q, float* s, int c, const float (&v)[N]) const {
+  // The piece in 8 bits: values to q, the group's scale to the row's scales s (`here`: the row exists).
+  __device__ void store8(const Buffer& q, float* s, bool here, int c, const float (&v)[N]) const {
     float top = 0.f;
 #pragma unroll
     for (int e = 0; e < N; ++e) top = max_mag(top, v[e]);
@@ -129,20 +159,20 @@ struct RowOf {
     const float sc = scale8(top), r = 1.f / sc;
     if constexpr (!VEC) {
       const int w = pack8<false>(over_scale(v[0], sc, r), over_scale(v[1], sc, r), 0);
-      if (has(c, 0)) q[col(c, 0)] = (uint8_t)w;
-      if (has(c, 1)) q[col(c, 1)] = (uint8_t)(w >> 8);
-    } else if (has(c)) {
+      __builtin_amdgcn_raw_buffer_store_b8((char)w, q.r, at(q, c, 0, 1), 0, 0);
+      __builtin_amdgcn_raw_buffer_store_b8((char)(w >> 8), q.r, at(q, c, 1, 1), 0, 0);
+    } else {
       int w[N / 4];
 #pragma unroll
       for (int e = 0; e < N / 4; ++e)
         w[e] = pack8<true>(over_scale(v[4 * e + 2], sc, r), over_scale(v[4 * e + 3], sc, r),
                            pack8<false>(over_scale(v[4 * e], sc, r), over_scale(v[4 * e + 1], sc, r), 0));
       if constexpr (N == 8)
-        *(i32x2*)(q + col(c, 0)) = i32x2{w[0], w[1]};
+        __builtin_amdgcn_raw_buffer_store_b64(i32x2{w[0], w[1]}, q.r, at(q, c, 0, 1), 0, 0);
       else
-        *(int*)(q + col(c, 0)) = w[0];
+        __builtin_amdgcn_raw_buffer_store_b32(w[0], q.r, at(q, c, 0, 1), 0, 0);
     }
-    if (col(c, 0) % kGroup8 == 0 && has(c)) s[col(c, 0) / kGroup8] = sc;
+    if (here && col(c, 0) % kGroup8 == 0 && col(c, 0) < d) s[col(c, 0) / kGroup8] = sc;
   }
 };
 
@@ -151,7 +181,7 @@ struct RowOf {
 template <int T, int S>
 __device__ inline void row_sums(float (&v)[S], float* red, int turn) {
 #pragma unroll
-  for (int k = 0; k < S; ++k) v[k] = wave_sum(v[k]);
+  for (int k = 0; k < S; ++k) v[k] = lanes_sum<T>(v[k]);
   if constexpr (T > 64) {
     constexpr int W = T / 64;
     float* at = red + (turn & 1) * W * S;
@@ -171,23 +201,25 @@ __device__ inline void row_sums(float (&v)[S], float* red, int turn) {
 
 }  // namespace
 
-template <int ELT, bool VEC, int T, int C>
+template <int ELT, bool VEC, bool ONCE, int T, int C>
 __global__ __launch_bounds__(T > 256 ? T : 256) void rms_norm_kernel(NormArgs a) {
   typedef RowOf<ELT, VEC, T> Row;
-  constexpr int N = Row::N, kRows = T > 256 ? 1 : 256 / T;  // rows of a workgroup
-  __shared__ float red[2 * T / 64];
-  const Row p = {(int)threadIdx.x % T, a.d};
-  const int64_t row = row_block() * kRows + (T < 256 ? threadIdx.x / T : 0);
-  if (row >= a.rows) return;  // T < 256: whole waves, which meet no barrier
-  const uint8_t *x = (const uint8_t*)a.X + row * a.ldx * ELT, *r = (const uint8_t*)a.R + row * a.ldr * ELT;
+  constexpr int N = Row::N;
+  __shared__ float red[T > 64 ? T / 64 : 1];
+  const Row p(a.d);
+  const int64_t row0 = Row::first(row_block() * Row::kRows), row = row0 + p.sub;
+  if (row0 >= a.rows) return;  // T < 256: whole waves, which meet no barrier
+  const bool here = row < a.rows;
+  const auto x = p.buffer(a.X, row0, a.ldx, a.rows), r = p.buffer(a.R, row0, a.ldr, a.rows);
+  const typename Row::Buffer w1 = {p.buffer(a.W, 0, 0, 1).r, 0};
   typename Row::Raw rx[C], rr[C], rw[C];
 #pragma unroll
-  for (int c = 0; c < C; ++c) rx[c] = p.load(x, c);
+  for (int c = 0; c < C; ++c) rx[c] = p.template load<ONCE>(x, c);
   if (a.R)
 #pragma unroll
-    for (int c = 0; c < C; ++c) rr[c] = p.load(r, c);
+    for (int c = 0; c < C; ++c) rr[c] = p.template load<ONCE>(r, c);
 #pragma unroll
-  for (int c = 0; c < C; ++c) rw[c] = p.load(a.W, c);
+  for (int c = 0; c < C; ++c) rw[c] = p.load(w1, c);
   float h[C][N], s[1] = {0.f};
 #pragma unroll
   for (int c = 0; c < C; ++c) {
@@ -205,13 +237,13 @@ __global__ __launch_bounds__(T > 256 ? T : 256) void rms_norm_kernel(NormArgs a)
   const float u = 1.f / sqrtf(s[0] / a.d + a.eps);
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    if (a.H) p.store((uint8_t*)a.H + row * a.ldh * ELT, c, h[c]);
+    if (a.H) p.store(p.buffer(a.H, row0, a.ldh, a.rows), c, h[c]);
     float w[N];
     Row::floats(rw[c], w);
 #pragma unroll
     for (int e = 0; e < N; ++e) h[c][e] = h[c][e] * u * w[e];
-    if (a.Y) p.store((uint8_t*)a.Y + row * a.ldy * ELT, c, h[c]);
-    if (a.Q) p.store8(a.Q + row * a.ldq, a.S + row * a.lds, c, h[c]);
+    if (a.Y) p.store(p.buffer(a.Y, row0, a.ldy, a.rows), c, h[c]);
+    if (a.Q) p.store8(p.buffer(a.Q, row0, a.ldq, a.rows, 1), a.S + row * a.lds, here, c, h[c]);
   }
 }
 
@@ -248,35 +280,48 @@ __global__ __launch_bounds__(256) void rms_norm_long_kernel(NormArgs a) {
 
 // The workgroups walk the rows; each keeps its columns' share of dW and leaves it
 // as one row of part (null: dW is not wanted).
-template <int ELT, bool VEC, int T, int C>
-__global__ __launch_bounds__(T > 256 ? T : 256) void norm_grad_kernel(NormGradArgs a, float* __restrict__ part) {
+template <int ELT, bool VEC, bool ONCE, int T, int C>
+__global__ __launch_bounds__(T > 256 ? T : 256) void norm_grad_kernel(NormGradArgs a,
+                                                                                float* __restrict__ part) {
   typedef RowOf<ELT, VEC, T> Row;
-  constexpr int N = Row::N, kRows = T > 256 ? 1 : 256 / T;
-  __shared__ float red[4 * T / 64];
+  constexpr int N = Row::N, kRows = Row::kRows;
+  constexpr bool kAhead = C <= 2;  // the next row is on its way while this one is worked on
+  __shared__ float red[T > 64 ? 4 * T / 64 : 1];
   __shared__ float share[kRows > 1 ? kRows * T * N : 1];
-  const Row p = {(int)threadIdx.x % T, a.d};
-  const int sub = T < 256 ? threadIdx.x / T : 0;
+  const Row p(a.d);
   typename Row::Raw rw[C];
+  const typename Row::Buffer w1 = {p.buffer(a.W, 0, 0, 1).r, 0};
 #pragma unroll
-  for (int c = 0; c < C; ++c) rw[c] = p.load(a.W, c);
+  for (int c = 0; c < C; ++c) rw[c] = p.load(w1, c);
   float dw[C][N] = {};
-  // T > 64: all rows of a workgroup meet the barriers of row_sums, so it runs as long as its first has a row
-  int turn = 0;
-  for (int64_t r0 = (int64_t)blockIdx.x * kRows; r0 < a.rows; r0 += (int64_t)gridDim.x * kRows, ++turn) {
-    const int64_t row = r0 + sub;
-    const bool here = row < a.rows;
-    const uint8_t *g = (const uint8_t*)a.G + row * a.ldg * ELT, *h = (const uint8_t*)a.H + row * a.ldh * ELT,
-                  *q = (const uint8_t*)a.P + row * a.ldp * ELT;
-    typename Row::Raw rg[C] = {}, rh[C] = {}, rp[C] = {};
-    if (here) {
+  struct Three {
+    typename Row::Raw g[C], h[C], p[C];
+  };
+  auto fetch = [&](int64_t row0) {
+    Three v = {};
+    if (row0 < a.rows) {
+      const auto g = p.buffer(a.G, row0, a.ldg, a.rows), h = p.buffer(a.H, row0, a.ldh, a.rows),
+                 q = p.buffer(a.P, row0, a.ldp, a.rows);
 #pragma unroll
-      for (int c = 0; c < C; ++c) rg[c] = p.load(g, c);
+      for (int c = 0; c < C; ++c) v.g[c] = p.template load<ONCE>(g, c);
 #pragma unroll
-      for (int c = 0; c < C; ++c) rh[c] = p.load(h, c);
+      for (int c = 0; c < C; ++c) v.h[c] = p.template load<ONCE>(h, c);
       if (a.P)
 #pragma unroll
-        for (int c = 0; c < C; ++c) rp[c] = p.load(q, c);
+        for (int c = 0; c < C; ++c) v.p[c] = p.template load<ONCE>(q, c);
     }
+    return v;
+  };
+  const int64_t step = (int64_t)gridDim.x * kRows;
+  int turn = 0;
+  Three next = fetch(Row::first((int64_t)blockIdx.x * kRows));
+  // T > 64: all rows of a workgroup meet the barriers of row_sums, so it runs as long as its first has a row
+  for (int64_t r0 = (int64_t)blockIdx.x * kRows; r0 < a.rows; r0 += step, ++turn) {
+    const int64_t row0 = Row::first(r0);
+    if (!kAhead && turn) next = fetch(row0);
+    Three now = next;
+    auto &rg = now.g, &rh = now.h, &rp = now.p;
+    if (kAhead) next = fetch(row0 + step);
     float s[2] = {0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < C; ++c) {
@@ -292,7 +337,13 @@ __global__ __launch_bounds__(T > 256 ? T : 256) void norm_grad_kernel(NormGradAr
     }
     row_sums<T>(s, red, turn);
     const float u = 1.f / sqrtf(s[0] / a.d + a.eps), k = u * u * (s[1] / a.d);
-    if (!here) continue;
+    if (row0 >= a.rows) continue;  // rows of the wave that are not there are zeros, and are not written
+    const auto out = p.buffer(a.D, row0, a.ldd, a.rows);
+    // 1024 threads: the floats of before are formed again rather than kept, for bf16 takes half the registers
+    // (fewer threads: 16384 rows of 4096 in 73 us kept, 80 formed again)
+    if constexpr (T == 1024)
+#pragma unroll
+      for (int c = 0; c < C; ++c) asm volatile("" : "+v"(rg[c]), "+v"(rh[c]), "+v"(rw[c]));
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       float vg[N], vh[N], vw[N], vp[N];
@@ -306,11 +357,12 @@ __global__ __launch_bounds__(T > 256 ? T : 256) void norm_grad_kernel(NormGradAr
         vg[e] = u * fmaf(-vh[e], k, vg[e] * vw[e]);
         if (a.P) vg[e] += vp[e];
       }
-      p.store((uint8_t*)a.D + row * a.ldd * ELT, c, vg);
+      p.store(out, c, vg);
     }
   }
   if (!part) return;
   float* out = part + (int64_t)blockIdx.x * a.d;
+  const int sub = T < 256 ? threadIdx.x / T : 0;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     if constexpr (kRows > 1) {  // the rows' shares in order
@@ -330,7 +382,7 @@ __global__ __launch_bounds__(T > 256 ? T : 256) void norm_grad_kernel(NormGradAr
     if (sub == 0)
 #pragma unroll
       for (int e = 0; e < N; ++e)
-        if (p.has(c, e)) out[p.col(c, e)] = dw[c][e];
+        if (p.col(c, e) < a.d) out[p.col(c, e)] = dw[c][e];
   }
 }
 
@@ -396,21 +448,27 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const float* __restrict
   if (lane == 0 && w < cols) out[w] = accumulate ? out[w] + s : s;
 }
 
-// A wave per group of a row.
-template <int ELT>
+// A wave takes kQuantize pieces of a row, n_waves waves a row.
+constexpr int kQuantize = 4;
+template <int ELT, bool VEC>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const void* __restrict__ X, int64_t ldx, int64_t rows,
-                                                            int d, uint8_t* __restrict__ Q, int64_t ldq,
+                                                            int d, int n_waves, uint8_t* __restrict__ Q, int64_t ldq,
                                                             float* __restrict__ S, int64_t lds) {
-  const int lane = threadIdx.x & 63;
-  const int64_t groups = (d + kGroup8 - 1) / kGroup8, i = row_block() * 4 + (threadIdx.x >> 6);
-  if (i >= rows * groups) return;
-  const int64_t row = i / groups;
-  const int g = (int)(i - row * groups), c = g * kGroup8;
-  float v[2];
+  typedef RowOf<ELT, VEC, 64> Row;
+  const int64_t i = row_block() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = i / n_waves;
+  if (row >= rows) return;
+  const int c0 = (int)(i - row * n_waves) * kQuantize;
+  const Row p(d);
+  const auto x = p.buffer(X, row, ldx, rows), q = p.buffer(Q, row, ldq, rows, 1);
+  typename Row::Raw r[kQuantize];
 #pragma unroll
-  for (int e = 0; e < 2; ++e)
-    v[e] = c + lane + 64 * e < d ? load_elt<ELT>(X, row * ldx + c + lane + 64 * e) : 0.f;
-  store_group8(Q + row * ldq + c, S + row * lds + g, lane, d - c, v[0], v[1]);
+  for (int c = 0; c < kQuantize; ++c) r[c] = p.load(x, c0 + c);
+#pragma unroll
+  for (int c = 0; c < kQuantize; ++c) {
+    float v[Row::N];
+    Row::floats(r[c], v);
+    p.store8(q, S + row * lds, true, c0 + c, v);
+  }
 }
 
 // A workgroup per block of 128 x 128, read twice (64 KB at most).
@@ -440,22 +498,36 @@ __global__ __launch_bounds__(256) void quantize_weight_kernel(const void* __rest
 
 namespace {
 
+// Bytes read and written from which on rows are loaded past the caches, which
+// cannot hold them for the next reader: 16384 rows of 4096 bf16, norm to 8 bits
+// (471 MB) 71 us, through the caches 79; gradient (537 MB) 83 and 106.
+constexpr int64_t kOnceBytes = (int64_t)256 << 20;
+
 // Pieces of a row.
 int64_t pieces_of(int elt, bool vec, int64_t d) { return vec ? d / (16 / elt) : (d + kGroup8 - 1) / kGroup8 * 64; }
 
-// f(T, C) with the threads and pieces per thread that hold rows of n pieces, T
-// at least `least`; false if none do.
-template <class F>
-bool with_shape(int64_t n, int least, F f) {
-  auto fits = [&](int t, int c) { return t >= least && n <= (int64_t)t * c; };
-#define SHAPE(T, C) \
-  if (fits(T, C)) return f(std::integral_constant<int, T>{}, std::integral_constant<int, C>{}), true
+// f(T, C) with the threads and pieces per thread that hold rows of n pieces;
+// false if none do.  Several short rows in a wave: as few lanes each as hold a
+// group of 8-bit values.  Four waves per row as soon as each has a piece for
+// every lane: 16384 rows of 4096 bf16, norm to 8 bits 71 us, with one wave 74;
+// gradient 83 and 116, whose sums of dW a wave has fewer of.
+//   MOST: pieces of the longest rows that are asked for
+template <int ELT, bool VEC, int MOST, class F>
+bool with_shape(int64_t n, F f) {
+#define SHAPE(T, C)                 \
+  if constexpr ((T) * (C) <= MOST)  \
+    if (n <= (T) * (C)) return f(std::integral_constant<int, T>{}, std::integral_constant<int, C>{}), true
+  if constexpr (VEC) {
+    SHAPE(8 * ELT, 1);
+    SHAPE(8 * ELT, 2);
+  }
+  SHAPE(64, 1);
   SHAPE(64, 2);
-  SHAPE(64, 4);
-  SHAPE(64, 8);
+  if (n < 256) SHAPE(64, 4);
   SHAPE(256, 2);
-  SHAPE(256, 4);
-  SHAPE(256, 8);
+  SHAPE(512, 2);
+  SHAPE(1024, 2);
+  SHAPE(1024, 4);
   SHAPE(1024, 8);
 #undef SHAPE
   return false;
@@ -465,15 +537,16 @@ bool on(const void* p, int64_t ld, int elt, int bytes) {
   return !p || ((uintptr_t)p % bytes == 0 && ld * elt % bytes == 0);
 }
 
-template <int ELT, bool VEC>
+template <int ELT, bool VEC, bool ONCE>
 hipError_t launch_norm_as(const NormArgs& a, hipStream_t s) {
   hipError_t e = hipSuccess;
   const int64_t n = pieces_of(ELT, VEC, a.d);
-  const bool held = with_shape(n, a.rows < 2048 && n > 64 ? 256 : 64, [&](auto T, auto C) {
-    constexpr int t = decltype(T)::value, rows = t > 256 ? 1 : 256 / t;
+  const bool held = with_shape<ELT, VEC, 8192>(n, [&](auto T, auto C) {
+    typedef RowOf<ELT, VEC, decltype(T)::value> Row;
     dim3 grid;
-    if ((e = row_grid((a.rows + rows - 1) / rows, &grid, t > 256 ? t : 256)) != hipSuccess) return;
-    hipLaunchKernelGGL((rms_norm_kernel<ELT, VEC, t, decltype(C)::value>), grid, dim3(t > 256 ? t : 256), 0, s, a);
+    if ((e = row_grid((a.rows + Row::kRows - 1) / Row::kRows, &grid, Row::kThreads)) != hipSuccess) return;
+    hipLaunchKernelGGL((rms_norm_kernel<ELT, VEC, ONCE, decltype(T)::value, decltype(C)::value>), grid,
+                       dim3(Row::kThreads), 0, s, a);
     e = hipGetLastError();
   });
   if (held) return e;
@@ -488,16 +561,21 @@ hipError_t launch_norm_as(const NormArgs& a, hipStream_t s) {
 hipError_t launch_rms_norm(int elt, const NormArgs& a, hipStream_t s) {
   const bool vec = a.d % (16 / elt) == 0 && on(a.X, a.ldx, elt, 16) && on(a.R, a.ldr, elt, 16) && on(a.W, 0, elt, 16) &&
                    on(a.Y, a.ldy, elt, 16) && on(a.H, a.ldh, elt, 16) && on(a.Q, a.ldq, 1, 16 / elt);
-  return elt == 2 ? (vec ? launch_norm_as<2, true>(a, s) : launch_norm_as<2, false>(a, s))
-                  : (vec ? launch_norm_as<4, true>(a, s) : launch_norm_as<4, false>(a, s));
+  const int64_t per = 1 + (a.R != nullptr) + (a.Y != nullptr) + (a.H != nullptr);
+  const bool once = a.rows * a.d * (per * elt + (a.Q != nullptr)) > kOnceBytes;
+  if (!vec) return elt == 2 ? launch_norm_as<2, false, false>(a, s) : launch_norm_as<4, false, false>(a, s);
+  return elt == 2 ? (once ? launch_norm_as<2, true, true>(a, s) : launch_norm_as<2, true, false>(a, s))
+                  : (once ? launch_norm_as<4, true, true>(a, s) : launch_norm_as<4, true, false>(a, s));
 }
 
 namespace {
 
-// Workgroups of the gradient where registers hold the rows: four per CU.  Whether
-// they do does not go by the buffers' alignment here, so a layout fits any.
-constexpr int kGradGroups = 1024;
-bool grad_held(int elt, int64_t d) { return pieces_of(elt, false, d) <= 1024 * 8 && d <= 1024 * 8 * (16 / elt); }
+// Workgroups of the gradient where registers hold the rows: two per CU (16384
+// rows of 4096 bf16: 83 us, with one 87, three 89, four 97).  Whether they do
+// does not go by the buffers' alignment here, so a layout fits any.
+constexpr int kGradGroups = 512;
+constexpr int kGradMost = 16384;  // columns of the longest row that they hold
+bool grad_held(int64_t d) { return d <= kGradMost; }
 
 // Rows per part of a long row's weight gradient, and parts: eight workgroups per CU of 64 rows or more.
 void weight_shape(int64_t rows, int64_t d, int64_t* per, int64_t* parts) {
@@ -508,10 +586,10 @@ void weight_shape(int64_t rows, int64_t d, int64_t* per, int64_t* parts) {
 
 }  // namespace
 
-NormGradLayout norm_grad_layout(int elt, int64_t rows, int64_t d, bool weight) {
+NormGradLayout norm_grad_layout(int64_t rows, int64_t d, bool weight) {
   NormGradLayout l = {};
   if (!weight) return l;
-  if (grad_held(elt, d)) {
+  if (grad_held(d)) {
     l.total = align_up((size_t)std::min<int64_t>(kGradGroups, rows) * d * 4);
     return l;
   }
@@ -530,16 +608,16 @@ hipError_t join(const float* part, int64_t parts, int64_t d, float* dw, bool acc
   return hipGetLastError();
 }
 
-template <int ELT, bool VEC>
+template <int ELT, bool VEC, bool ONCE>
 hipError_t launch_grad_as(const NormGradArgs& a, float* dw, bool accumulate, uint8_t* ws, hipStream_t s) {
   hipError_t e = hipSuccess;
   int64_t groups = 0;
-  with_shape(pieces_of(ELT, VEC, a.d), 64, [&](auto T, auto C) {
-    constexpr int t = decltype(T)::value, rows = t > 256 ? 1 : 256 / t;
-    groups = std::min<int64_t>(kGradGroups, (a.rows + rows - 1) / rows);
+  with_shape<ELT, VEC, VEC ? kGradMost * ELT / 16 : 8192>(pieces_of(ELT, VEC, a.d), [&](auto T, auto C) {
+    typedef RowOf<ELT, VEC, decltype(T)::value> Row;
+    groups = std::min<int64_t>(kGradGroups, (a.rows + Row::kRows - 1) / Row::kRows);
     if (groups == 0) return;
-    hipLaunchKernelGGL((norm_grad_kernel<ELT, VEC, t, decltype(C)::value>), dim3((unsigned)groups),
-                       dim3(t > 256 ? t : 256), 0, s, a, dw ? (float*)ws : nullptr);
+    hipLaunchKernelGGL((norm_grad_kernel<ELT, VEC, ONCE, decltype(T)::value, decltype(C)::value>),
+                       dim3((unsigned)groups), dim3(Row::kThreads), 0, s, a, dw ? (float*)ws : nullptr);
     e = hipGetLastError();
   });
   if (e != hipSuccess || !dw) return e;
@@ -549,13 +627,18 @@ hipError_t launch_grad_as(const NormGradArgs& a, float* dw, bool accumulate, uin
 }  // namespace
 
 hipError_t launch_norm_grad(int elt, NormGradArgs a, float* dw, bool accumulate, uint8_t* ws, hipStream_t s) {
-  if (grad_held(elt, a.d)) {
+  if (grad_held(a.d)) {
     const bool vec = a.d % (16 / elt) == 0 && on(a.G, a.ldg, elt, 16) && on(a.H, a.ldh, elt, 16) &&
                      on(a.W, 0, elt, 16) && on(a.P, a.ldp, elt, 16) && on(a.D, a.ldd, elt, 16);
-    return elt == 2 ? (vec ? launch_grad_as<2, true>(a, dw, accumulate, ws, s)
-                           : launch_grad_as<2, false>(a, dw, accumulate, ws, s))
-                    : (vec ? launch_grad_as<4, true>(a, dw, accumulate, ws, s)
-                           : launch_grad_as<4, false>(a, dw, accumulate, ws, s));
+    const bool once = a.rows * a.d * elt * (3 + (a.P != nullptr)) > kOnceBytes;
+    if (!vec)
+      return elt == 2 ? launch_grad_as<2, false, false>(a, dw, accumulate, ws, s)
+                      : launch_grad_as<4, false, false>(a, dw, accumulate, ws, s);
+    if (elt == 2)
+      return once ? launch_grad_as<2, true, true>(a, dw, accumulate, ws, s)
+                  : launch_grad_as<2, true, false>(a, dw, accumulate, ws, s);
+    return once ? launch_grad_as<4, true, true>(a, dw, accumulate, ws, s)
+                : launch_grad_as<4, true, false>(a, dw, accumulate, ws, s);
   }
   hipError_t e;
   a.U = dw ? (float*)ws : nullptr;
@@ -568,7 +651,7 @@ hipError_t launch_norm_grad(int elt, NormGradArgs a, float* dw, bool accumulate,
   if (!dw) return hipSuccess;
   int64_t per, parts;
   weight_shape(a.rows, a.d, &per, &parts);
-  float* part = (float*)(ws + norm_grad_layout(elt, a.rows, a.d, true).off_part);
+  float* part = (float*)(ws + norm_grad_layout(a.rows, a.d, true).off_part);
   hipLaunchKernelGGL(elt == 2 ? norm_weight_kernel<2> : norm_weight_kernel<4>,
                      dim3((unsigned)((a.d + 63) / 64), (unsigned)parts), dim3(256), 0, s, a, per,
                      parts > 1 ? part : dw, parts > 1 ? 0 : (int)accumulate);
@@ -578,11 +661,14 @@ hipError_t launch_norm_grad(int elt, NormGradArgs a, float* dw, bool accumulate,
 
 hipError_t launch_quantize_rows(int elt, const void* X, int64_t ldx, int64_t rows, int64_t d, uint8_t* Q, int64_t ldq,
                                 float* S, int64_t lds, hipStream_t s) {
+  const bool vec = d % (16 / elt) == 0 && on(X, ldx, elt, 16) && on(Q, ldq, 1, 16 / elt);
+  const int n_waves = (int)((pieces_of(elt, vec, d) + 64 * kQuantize - 1) / (64 * kQuantize));
   dim3 grid;
-  const hipError_t e = row_grid((rows * ((d + kGroup8 - 1) / kGroup8) + 3) / 4, &grid);
+  const hipError_t e = row_grid((rows * n_waves + 3) / 4, &grid);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(elt == 2 ? quantize_rows_kernel<2> : quantize_rows_kernel<4>, grid, dim3(256), 0, s, X, ldx, rows,
-                     (int)d, Q, ldq, S, lds);
+  auto k = elt == 2 ? (vec ? quantize_rows_kernel<2, true> : quantize_rows_kernel<2, false>)
+                    : (vec ? quantize_rows_kernel<4, true> : quantize_rows_kernel<4, false>);
+  hipLaunchKernelGGL(k, grid, dim3(256), 0, s, X, ldx, rows, (int)d, n_waves, Q, ldq, S, lds);
   return hipGetLastError();
 }
 

