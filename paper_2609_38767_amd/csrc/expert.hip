@@ -41,43 +41,58 @@ __device__ inline Segment segment(const ExpertArgs& x, int s) {
   return Segment{begin, max(begin, s > x.experts ? x.rows : boundary(x, s))};
 }
 
-// Tile row `at` of all segments' tile rows of TM rows each.
+// Which tile rows of TM rows each are counted: all of every segment, or those that
+// its rows fill to more than half, or the one that they fill to half at most.
+enum Rows { kAll, kFull, kRest };
+
+// Tile row `at` of all segments' tile rows.
 struct Place {
   int segment, m0, end;
 };
-// Sums stop at `most`, the largest number of tile rows that ordered boundaries
-// give: others may not overflow them, and what is found below it is a tile of
-// its segment.
+// Sums stop at the largest number of tile rows that ordered boundaries give, so
+// others may not overflow them, and what is found below it is a tile row of its
+// segment.
 template <int TM>
 struct Segments {
   const ExpertArgs& x;
-  int lane, most, total;
+  int lane;
   Segment first;  // of the first 64 segments, this lane's
-  __device__ int tiles(const Segment& g) const { return (g.end - g.begin + TM - 1) / TM; }
   __device__ Segment load(int s) const { return s < x.experts + 2 ? segment(x, s) : Segment{0, 0}; }
-  __device__ Segments(const ExpertArgs& x_, int most_, int lane_) : x(x_), lane(lane_), most(most_) {
-    first = load(lane);
-    int n = tiles(first);
-    for (int s = 64; s < x.experts + 2; s += 64) n = min(n + tiles(load(s + lane)), most);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) n = min(n + __shfl_xor(n, o), most);
-    total = __builtin_amdgcn_readfirstlane(n);
+  __device__ Segments(const ExpertArgs& x_, int lane_) : x(x_), lane(lane_) { first = load(lane); }
+  template <Rows R>
+  __device__ static int tiles(const Segment& g) {
+    const int n = g.end - g.begin;
+    return R == kAll ? (n + TM - 1) / TM : R == kFull ? (n + TM / 2 - 1) / TM : n % TM > 0 && n % TM <= TM / 2;
   }
+  template <Rows R>
+  __device__ int most() const {
+    const int full = x.rows / TM, some = min(x.experts + 2, x.rows);
+    return R == kRest ? some : full + some;
+  }
+  template <Rows R>
+  __device__ int total() const {
+    int n = tiles<R>(first);
+    for (int s = 64; s < x.experts + 2; s += 64) n = min(n + tiles<R>(load(s + lane)), most<R>());
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) n = min(n + __shfl_xor(n, o), most<R>());
+    return __builtin_amdgcn_readfirstlane(n);
+  }
+  template <Rows R>
   __device__ Place find(int at) const {  // at < total
     int before = 0;
     for (int s = 0;; s += 64) {
       const Segment g = s ? load(s + lane) : first;
-      int upto = min(before + tiles(g), most);  // of the segments up to this lane's
+      int upto = min(before + tiles<R>(g), most<R>());  // of the segments up to this lane's
 #pragma unroll
       for (int o = 1; o < 64; o <<= 1) {
         const int v = __shfl_up(upto - before, o);
-        if (lane >= o) upto = min(upto + v, most);
+        if (lane >= o) upto = min(upto + v, most<R>());
       }
       const uint64_t here = __ballot(upto > at);
       if (here) {
-        const int l = __builtin_ctzll(here), in_front = l ? __builtin_amdgcn_readlane(upto, l - 1) : before;
-        return Place{s + l, __builtin_amdgcn_readlane(g.begin, l) + (at - in_front) * TM,
-                     __builtin_amdgcn_readlane(g.end, l)};
+        const int l = __builtin_ctzll(here), in_front = l ? __builtin_amdgcn_readlane(upto, l - 1) : before,
+                  begin = __builtin_amdgcn_readlane(g.begin, l), end = __builtin_amdgcn_readlane(g.end, l);
+        return Place{s + l, R == kRest ? begin + (end - begin) / TM * TM : begin + (at - in_front) * TM, end};
       }
       before = __builtin_amdgcn_readlane(upto, 63);
       if (s + 64 >= x.experts + 2) return Place{0, 0, 0};
@@ -88,27 +103,50 @@ struct Segments {
 }  // namespace
 
 // Products over rows: grid as many tiles as there can be (tiles, 1, more tiles).
+// Of 256 x 256 tiles a segment's last is half empty on average: where it would be
+// half empty or more, a tile of 128 x 256 takes its place, behind the others, in
+// half the time.  (Tiles of 128 x 128 for all last rows: 64 experts of 4096 ->
+// 1024, 32768 rows, 455 us, whole tiles 371; alone on a CU they are slow.)
 template <int OP, bool BC, int ELT, int KW, int WM, int WN, int BM, int BN>
-__global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void expert_rows_kernel(GemmArgs a, ExpertArgs x, int nm,
-                                                                                 int nn) {
-  constexpr int TM = WM * BM * 32, BK = KW / ELT;
-  const Segments<TM> all(x, nm, threadIdx.x & 63);
+__global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void expert_rows_kernel(GemmArgs a, ExpertArgs x, int nn) {
+  constexpr int TM = WM * BM * 32, TN = WN * BN * 32, BK = KW / ELT;
+  constexpr bool kHalves = TM == 256;
+  typedef TileBuffers<true, BC, ELT, KW, WM, WN, BM, BN> Buffers;
+  DATTRI_TILE_BUFFERS(Buffers);
+  const Segments<TM> all(x, threadIdx.x & 63);
   const int64_t tile = (int64_t)blockIdx.z * gridDim.x + blockIdx.x;
-  if (tile >= (int64_t)all.total * nn) return;
+  auto run = [&](const Place& p, auto product) DATTRI_INLINE {
+    const int e = p.segment - 1;
+    a.M = p.end;
+    if (e < 0 || e >= x.experts) {
+      a.K = 0;
+      a.bias = nullptr;
+    } else {
+      a.B = (const uint8_t*)a.B + (int64_t)e * x.stride * ELT;
+      if (a.bias) a.bias = (const uint8_t*)a.bias + (int64_t)e * a.N * ELT;
+    }
+    product((int)(((int64_t)a.K + BK - 1) / BK));
+  };
+  const int n = all.template total<kHalves ? kFull : kAll>();
   int mt, nt;
-  tile_of((int)tile, all.total, nn, &mt, &nt);
-  const Place p = all.find(mt);
-  const int e = p.segment - 1;
-  a.M = p.end;
-  if (e < 0 || e >= x.experts) {
-    a.K = 0;
-    a.bias = nullptr;
-  } else {
-    a.B = (const uint8_t*)a.B + (int64_t)e * x.stride * ELT;
-    if (a.bias) a.bias = (const uint8_t*)a.bias + (int64_t)e * a.N * ELT;
+  if (tile < (int64_t)n * nn) {
+    tile_of((int)tile, n, nn, &mt, &nt);
+    const Place p = all.template find<kHalves ? kFull : kAll>(mt);
+    run(p, [&](int stages) DATTRI_INLINE {
+      tile_product<OP, true, BC, ELT, KW, WM, WN, BM, BN>(a, p.m0, nt * TN, 0, stages, a.K, nullptr, 0, x0, x1, x2, x3);
+    });
+    return;
   }
-  tile_product<OP, true, BC, ELT, KW, WM, WN, BM, BN>(a, p.m0, nt * WN * BN * 32, 0,
-                                                      (int)(((int64_t)a.K + BK - 1) / BK), a.K, nullptr, 0);
+  if constexpr (kHalves) {
+    const int64_t half = tile - (int64_t)n * nn;
+    const int rest = all.template total<kRest>();
+    if (half >= (int64_t)rest * nn) return;
+    tile_of((int)half, rest, nn, &mt, &nt);
+    const Place p = all.template find<kRest>(mt);
+    run(p, [&](int stages) DATTRI_INLINE {
+      tile_product<OP, true, BC, ELT, KW, 2, 2, 2, 4>(a, p.m0, nt * TN, 0, stages, a.K, nullptr, 0, x0, x1, x2, x3);
+    });
+  }
 }
 
 // Weight gradients: experts times nm times nn tiles.
@@ -116,6 +154,8 @@ template <int ELT, int KW, int WM, int WN, int BM, int BN>
 __global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void expert_weight_kernel(GemmArgs a, ExpertArgs x, int nm,
                                                                                    int nn) {
   constexpr int BK = KW / ELT;
+  typedef TileBuffers<false, false, ELT, KW, WM, WN, BM, BN> Buffers;
+  DATTRI_TILE_BUFFERS(Buffers);
   const int64_t tile = (int64_t)blockIdx.z * gridDim.x + blockIdx.x;
   if (tile >= (int64_t)x.experts * nm * nn) return;
   const int e = (int)(tile / (nm * nn));
@@ -128,7 +168,8 @@ __global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void expert_weight_kern
   a.B = (const uint8_t*)a.B + (int64_t)g.begin * a.ldb * ELT;
   a.out = (float*)a.out + (int64_t)e * x.stride;
   tile_product<DATTRI_LINEAR_WEIGHT_GRAD, false, false, ELT, KW, WM, WN, BM, BN>(
-      a, mt * WM * BM * 32, nt * WN * BN * 32, 0, (int)(((int64_t)a.K + BK - 1) / BK), a.K, nullptr, 0);
+      a, mt * WM * BM * 32, nt * WN * BN * 32, 0, (int)(((int64_t)a.K + BK - 1) / BK), a.K, nullptr, 0, x0, x1,
+      x2, x3);
 }
 
 // Column sums of an expert's rows: grid (64 columns, parts, experts); part y of
@@ -220,13 +261,13 @@ hipError_t launch_tiles(const GemmArgs& a, const ExpertArgs& x, hipStream_t s) {
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((expert_weight_kernel<ELT, KW, WM, WN, BM, BN>), grid, dim3(256), 0, s, a, x, (int)nm, (int)nn);
   } else {
-    // every segment with rows has at most one tile more than its rows fill
-    const int64_t nm = x.rows / TM + std::min<int64_t>(x.experts + 2, x.rows);
-    if (nm * nn > INT32_MAX) return hipErrorInvalidValue;
-    const hipError_t e = row_grid(nm * nn, &grid, 256, true);
+    // every segment with rows has at most one tile row more than its rows fill
+    const int64_t n = (x.rows / TM + std::min<int64_t>(x.experts + 2, x.rows)) * nn;
+    if (n > INT32_MAX) return hipErrorInvalidValue;
+    const hipError_t e = row_grid(n, &grid, 256, true);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((expert_rows_kernel<OP, OP == DATTRI_LINEAR_FORWARD, ELT, KW, WM, WN, BM, BN>), grid, dim3(256),
-                       0, s, a, x, (int)nm, (int)nn);
+                       0, s, a, x, (int)nn);
   }
   return hipGetLastError();
 }

@@ -30,6 +30,8 @@ template <int OP, bool AC, bool BC, int ELT, int KW, int WM, int WN, int BM, int
 __global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void gemm_kernel(GemmArgs a, int nm, int nn, int sps,
                                                                           float* __restrict__ part, int64_t ld_part) {
   constexpr int BK = KW / ELT;
+  typedef TileBuffers<AC, BC, ELT, KW, WM, WN, BM, BN> Buffers;
+  DATTRI_TILE_BUFFERS(Buffers);
   const int64_t tile = (int64_t)blockIdx.z * gridDim.x + blockIdx.x;
   if (tile >= (int64_t)nm * nn) return;
   int mt, nt;
@@ -37,7 +39,7 @@ __global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void gemm_kernel(GemmAr
   const int all = (int)(((int64_t)a.K + BK - 1) / BK), s0 = blockIdx.y * sps, ns = min(sps, all - s0);
   const int k_end = (int)min((int64_t)a.K, (int64_t)(s0 + ns) * BK);
   tile_product<OP, AC, BC, ELT, KW, WM, WN, BM, BN>(a, mt * WM * BM * 32, nt * WN * BN * 32, s0, ns, k_end,
-                                                    part + (int64_t)blockIdx.y * a.M * ld_part, ld_part);
+                                                    part + (int64_t)blockIdx.y * a.M * ld_part, ld_part, x0, x1, x2, x3);
 }
 
 // Column sums over rows [y * per, (y + 1) * per): a wave owns 64 C columns, C

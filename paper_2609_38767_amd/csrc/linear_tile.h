@@ -296,20 +296,32 @@ __device__ DATTRI_INLINE inline void finish_tile(const GemmArgs& a, const f32x16
   }
 }
 
+// The LDS of a tile: kBuffers arrays of kBytes.
+template <bool AC, bool BC, int ELT, int KW, int WM, int WN, int BM, int BN>
+struct TileBuffers {
+  static constexpr int TM = WM * BM * 32, TN = WN * BN * 32, kBuffers = buffers_of(KW);
+  static constexpr int kStage = Side<ELT, AC, TM, KW>::kBytes + Side<ELT, BC, TN, KW>::kBytes;
+  static constexpr int kSlab = 32 * TN * 4;  // epilogue: one block column of a row of waves, four of them
+  static constexpr int kBytes = std::max(kStage, kSlab * 4 / kBuffers);
+};
+#define DATTRI_TILE_BUFFERS(B)                                                                        \
+  __shared__ __align__(1024) uint8_t x0[B::kBytes], x1[B::kBytes], x2[B::kBuffers == 4 ? B::kBytes : 16], \
+      x3[B::kBuffers == 4 ? B::kBytes : 16]
+
 // The tile from row m0 and column n0, rows and columns below a.M and a.N: stages
 // s0 .. s0 + ns - 1 of k, up to k_end.  WM x WN waves; BM x BN blocks of 32 x 32
-// each.  OP kPartial: float32 sums to part, rows ld_part apart.
+// each.  OP kPartial: float32 sums to part, rows ld_part apart.  x0 .. x3: arrays
+// of TileBuffers, or larger ones (different arrays, so that the compiler can tell
+// a read of one from the loads into another).
 template <int OP, bool AC, bool BC, int ELT, int KW, int WM, int WN, int BM, int BN>
 __device__ DATTRI_INLINE inline void tile_product(const GemmArgs& a, int m0, int n0, int s0, int ns, int k_end,
-                                                  float* __restrict__ part, int64_t ld_part) {
+                                                  float* __restrict__ part, int64_t ld_part, uint8_t* x0, uint8_t* x1,
+                                                  uint8_t* x2, uint8_t* x3) {
   static_assert(WM * WN == 4 && WM <= 2, "four waves");
   constexpr int TM = WM * BM * 32, TN = WN * BN * 32;
   typedef Side<ELT, AC, TM, KW> SA;
   typedef Side<ELT, BC, TN, KW> SB;
-  constexpr int kStage = SA::kBytes + SB::kBytes, kBuffers = buffers_of(KW), kSteps = KW / 32;
-  constexpr int kSlab = 32 * TN * 4;  // epilogue: one block column of a row of waves, four of them
-  constexpr int kBuf = std::max(kStage, kSlab * 4 / kBuffers);
-  __shared__ __align__(1024) uint8_t x0[kBuf], x1[kBuf], x2[kBuffers == 4 ? kBuf : 16], x3[kBuffers == 4 ? kBuf : 16];
+  constexpr int kBuffers = buffers_of(KW), kSteps = KW / 32, kSlab = 32 * TN * 4;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WN, wn = wave % WN;
   SA sa;

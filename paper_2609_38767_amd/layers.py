@@ -444,9 +444,9 @@ def linear_8bit(x, weight, bias=None, act="none", residual=None, keep_preact=Fal
     ld_r = _rows(residual, "residual", dtype, shape)[2] if residual is not None else 0
     given = out
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=x.device)
+        out = x.new_empty(shape, dtype=dtype)
     ld_y = _rows(out, "out", dtype, shape)[2]
-    z = torch.empty(shape, dtype=dtype, device=x.device) if keep_preact else None
+    z = _like(out) if keep_preact else None
     ws_bytes = dattri_linear_scaled_workspace_bytes(n, d_in, d_out, code, _on_16(x, ld_x) and _on_16(weight, ld_w))
     dattri_linear_scaled(x, ld_x, sx, ld_sx, weight, ld_w, sw, ld_sw, bias, _act(act), residual, ld_r, out, ld_y, z, 0, n,
                        d_in, d_out, code, _workspace(ws_bytes, x.device), ws_bytes)
@@ -498,9 +498,9 @@ def expert_linear(x, weight, offsets, bias=None, act="none", residual=None, keep
     ld_r = _rows(residual, "residual", dt, shape)[2] if residual is not None else 0
     given = out
     if out is None:
-        out = torch.empty(shape, dtype=dt, device=x.device)
+        out = x.new_empty(shape)
     ld_y = _rows(out, "out", dt, shape)[2]
-    z = torch.empty(shape, dtype=dt, device=x.device) if keep_preact else None
+    z = _like(out) if keep_preact else None
     ws_bytes = dattri_expert_linear_workspace_bytes(DATTRI_LINEAR_FORWARD, n, e, d_in, d_out, code,
                                                     _on_16(x, ld_x) and _on_16(weight, ld_w))
     dattri_expert_linear(x, ld_x, weight, ld_w, bias, offsets, offsets.element_size(), _act(act), residual, ld_r, out,
@@ -529,9 +529,9 @@ def expert_linear_input_grad(g, weight, offsets, residual=None, act="none", prea
     ld_z = _rows(preact, "preact", dt, shape)[2] if preact is not None else 0
     given = out
     if out is None:
-        out = torch.empty(shape, dtype=dt, device=g.device)
+        out = g.new_empty(shape)
     ld_p = _rows(out, "out", dt, shape)[2]
-    d = torch.empty(shape, dtype=dt, device=g.device) if both else None
+    d = _like(out) if both else None
     ws_bytes = dattri_expert_linear_workspace_bytes(DATTRI_LINEAR_INPUT_GRAD, n, e, d_in, d_out, code,
                                                     _on_16(g, ld_g) and _on_16(weight, ld_w))
     dattri_expert_linear_input_grad(g, ld_g, weight, ld_w, offsets, offsets.element_size(), residual, ld_r, a, preact,
