@@ -172,31 +172,52 @@ __global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void expert_weight_kern
       x2, x3);
 }
 
-// Column sums of an expert's rows: grid (64 columns, parts, experts); part y of
-// parts takes its share of the expert's rows.  Sums of one part go to out, else
-// part holds [parts][experts][cols].
-template <int ELT>
+// Column sums of an expert's rows: grid (64 C columns, parts, experts); part y of
+// parts takes its share of the expert's rows, a wave every fourth of them, C
+// neighbouring columns per lane.  Sums of one part go to out, else part holds
+// [parts][experts][cols].  16384 x 14336 bf16 of eight experts took 125 us with
+// one column per lane.
+template <int ELT, int C>
 __global__ __launch_bounds__(256) void expert_columns_kernel(const void* __restrict__ G, int64_t ld, ExpertArgs x,
                                                              int cols, float* __restrict__ part,
                                                              float* __restrict__ out, int accumulate) {
-  __shared__ float red[4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane, e = blockIdx.z;
+  constexpr int kAhead = 8;
+  __shared__ float red[4][64 * C];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (blockIdx.x * 64 + lane) * C, e = blockIdx.z;
   const Segment g = segment(x, e + 1);
   const int64_t per = ((int64_t)g.end - g.begin + gridDim.y - 1) / gridDim.y, r0 = g.begin + blockIdx.y * per,
                 r1 = min((int64_t)g.end, r0 + per);
-  float s = 0.f;
-  if (c < cols)
-#pragma unroll 8
-    for (int64_t r = r0 + wave; r < r1; r += 4) s += load_elt<ELT>(G, r * ld + c);
-  red[wave][lane] = s;
+  f32x4 s[2] = {};
+  auto get = [&](int64_t r) {
+    if constexpr (C == 4) return load4_elt<ELT>(G, r * ld + c, true, 4);
+    return f32x4{load_elt<ELT>(G, r * ld + c), 0.f, 0.f, 0.f};
+  };
+  if (c < cols) {
+    int64_t r = r0 + wave;
+    for (; r + 4 * (kAhead - 1) < r1; r += 4 * kAhead) {
+      f32x4 v[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) v[u] = get(r + 4 * u);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) s[u & 1] += v[u];
+    }
+    for (; r < r1; r += 4) s[0] += get(r);
+  }
+  s[0] += s[1];
+#pragma unroll
+  for (int k = 0; k < C; ++k) red[wave][k * 64 + lane] = s[0][k];
   __syncthreads();
   if (wave == 0 && c < cols) {
-    s = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
     const int64_t at = (int64_t)e * cols + c;
-    if (gridDim.y > 1)
-      part[(int64_t)blockIdx.y * x.experts * cols + at] = s;
-    else
-      out[at] = accumulate ? out[at] + s : s;
+#pragma unroll
+    for (int k = 0; k < C; ++k) {
+      const int i = k * 64 + lane;
+      const float v = (red[0][i] + red[1][i]) + (red[2][i] + red[3][i]);
+      if (gridDim.y > 1)
+        part[(int64_t)blockIdx.y * x.experts * cols + at + k] = v;
+      else
+        out[at + k] = accumulate ? out[at + k] + v : v;
+    }
   }
 }
 
@@ -213,7 +234,7 @@ __global__ __launch_bounds__(256) void expert_columns_join_kernel(const float* _
 namespace {
 
 int64_t column_parts(int64_t rows, int64_t experts, int64_t cols) {
-  return std::max<int64_t>(1, std::min<int64_t>(2048 / ((cols + 63) / 64 * experts), rows / experts / 64));
+  return std::max<int64_t>(1, std::min<int64_t>(4096 / ((cols + 255) / 256 * experts), rows / experts / 64));
 }
 
 struct ExpertLayout {
@@ -306,9 +327,12 @@ hipError_t launch_expert(dattri_linear_op op, int elt, bool aligned, GemmArgs a,
   if (dbias) {
     const int64_t parts = column_parts(x.rows, x.experts, d_out), n = (int64_t)x.experts * d_out;
     float* part = (float*)(ws + L.off_cols);
-    hipLaunchKernelGGL(elt == 2 ? expert_columns_kernel<2> : expert_columns_kernel<4>,
-                       dim3((unsigned)((d_out + 63) / 64), (unsigned)parts, (unsigned)x.experts), dim3(256), 0, s, a.A,
-                       a.lda, x, (int)d_out, part, dbias, (int)a.accumulate);
+    const bool four = on4(a.A, a.lda, elt) && d_out % 4 == 0;
+    auto k = elt == 2 ? (four ? expert_columns_kernel<2, 4> : expert_columns_kernel<2, 1>)
+                      : (four ? expert_columns_kernel<4, 4> : expert_columns_kernel<4, 1>);
+    const int64_t wide = four ? 256 : 64;
+    hipLaunchKernelGGL(k, dim3((unsigned)((d_out + wide - 1) / wide), (unsigned)parts, (unsigned)x.experts), dim3(256), 0,
+                       s, a.A, a.lda, x, (int)d_out, part, dbias, (int)a.accumulate);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if (parts > 1) {
       dim3 grid;
