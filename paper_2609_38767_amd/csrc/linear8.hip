@@ -65,10 +65,10 @@ __device__ inline f32x4 block_dot(i32x4 w0, i32x4 w1, i32x4 x0, i32x4 x1) {
 struct Block8 {
   i32x8 k[2];
 };
-// Half h of block i; at: this lane's four chunks of the wave's first block.
-__device__ DATTRI_INLINE inline i32x8 read_half(const uint8_t* buf, const uint32_t (&at)[4], int i, int h) {
-  const i32x4 c = *(const i32x4*)(buf + at[2 * h] + i * (32 * 128)),
-              d = *(const i32x4*)(buf + at[2 * h + 1] + i * (32 * 128));
+// Half h of block i; at: this lane's four chunks of X's first block of the wave, by: from there to the operand's.
+__device__ DATTRI_INLINE inline i32x8 read_half(const uint8_t* buf, const uint32_t (&at)[4], int by, int i, int h) {
+  const i32x4 c = *(const i32x4*)(buf + (at[2 * h] + by) + i * (32 * 128)),
+              d = *(const i32x4*)(buf + (at[2 * h + 1] + by) + i * (32 * 128));
   return i32x8{c.x, c.y, c.z, c.w, d.x, d.y, d.z, d.w};
 }
 // Keeps what is made of v inside the loop: the sums leave few registers for
@@ -163,10 +163,10 @@ __global__ __launch_bounds__(WM* WN * 64) void linear8_kernel(GemmArgs a, Scales
   __shared__ __align__(1024) uint8_t x0[kBuf], x1[kBuf], x2[BUF == 4 ? kBuf : 16], x3[BUF == 4 ? kBuf : 16];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WN, wn = wave % WN, l32 = lane & 31;
-  const int64_t at = (int64_t)blockIdx.z * gridDim.x + blockIdx.x;
-  if (at >= (int64_t)nm * nn) return;
+  const int64_t tile = (int64_t)blockIdx.z * gridDim.x + blockIdx.x;
+  if (tile >= (int64_t)nm * nn) return;
   int mt, nt;
-  tile::tile_of((int)at, nm, nn, &mt, &nt);
+  tile::tile_of((int)tile, nm, nn, &mt, &nt);
   const int m0 = mt * TM, n0 = nt * TN;
   const int all = (int)(((int64_t)a.K + 127) / 128), s0 = blockIdx.y * sps, ns = min(sps, all - s0);
   const int k_end = (int)min((int64_t)a.K, (int64_t)(s0 + ns) * 128);
@@ -219,14 +219,12 @@ __global__ __launch_bounds__(WM* WN * 64) void linear8_kernel(GemmArgs a, Scales
   Block8 fa[kSlots], fb[BN];
   // scales: of the blocks whose sums wait, of this block column, of the next one, the stage's and the next stage's weight's
   float before = 0.f, now = 0.f, then = 0.f, of_w = 0.f;
-  uint32_t at_a[4], at_b[4], at_s = (wm * BM * 32 + l32) * 4;
+  uint32_t at[4], at_s = (wm * BM * 32 + l32) * 4;
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    at_a[q] = (wm * BM * 32 + l32) * 128 + (((2 * q + (lane >> 5)) ^ SA::swz(l32)) << 4);
-    at_b[q] = SA::kBytes + (wn * BN * 32 + l32) * 128 + (((2 * q + (lane >> 5)) ^ SB::swz(l32)) << 4);
-  }
-  auto read_a = [&](const uint8_t* x, int j, int h) DATTRI_INLINE { return read_half(x, at_a, j, h); };
-  auto read_b = [&](const uint8_t* x, int i, int h) DATTRI_INLINE { return read_half(x, at_b, i, h); };
+  for (int q = 0; q < 4; ++q) at[q] = (wm * BM * 32 + l32) * 128 + (((2 * q + (lane >> 5)) ^ SA::swz(l32)) << 4);
+  const int to_b = SA::kBytes + (wn * BN - wm * BM) * 32 * 128;  // rows of both operands are swizzled alike
+  auto read_a = [&](const uint8_t* x, int j, int h) DATTRI_INLINE { return read_half(x, at, 0, j, h); };
+  auto read_b = [&](const uint8_t* x, int i, int h) DATTRI_INLINE { return read_half(x, at, to_b, i, h); };
   auto read_s = [&](const uint8_t* x, int j) DATTRI_INLINE {
     return *(const float*)(x + kRowBytes + at_s + j * 128);
   };
@@ -236,10 +234,7 @@ __global__ __launch_bounds__(WM* WN * 64) void linear8_kernel(GemmArgs a, Scales
   // Stage st (in cx; P: its parity); the stage after it is in nx by its last block column.
   auto stage = [&](auto P, int st, uint8_t* cx, const uint8_t* nx) DATTRI_INLINE {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      renew(at_a[q]);
-      renew(at_b[q]);
-    }
+    for (int q = 0; q < 4; ++q) renew(at[q]);
     renew(at_s);
 #pragma unroll
     for (int q = 0; q < 2; ++q) {

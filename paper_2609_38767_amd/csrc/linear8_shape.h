@@ -37,8 +37,10 @@ inline Shape8 shape8(int64_t M, int64_t N, int64_t K, int elt) {
   };
   if (M <= 16) return cut(kFew, 1);
   if (M <= 64) return cut(kSlim, std::min<int64_t>(64, 768 / ((N + 127) / 128)));
-  // The cut with the least modelled time, as for the other products (gemm_shape).
-  const double rate[2] = {8.0e6, elt == 2 ? 5.5e6 : 3.0e6}, fixed[2] = {12., 4.};
+  // The cut with the least modelled time, as for the other products (gemm_shape):
+  // FLOP per us of a CU, us besides, and what a lone workgroup of 128 x 128 reaches
+  // of the rate where two share a CU otherwise (float32 results).
+  const double rate[2] = {8.8e6, elt == 2 ? 6.2e6 : 4.3e6}, fixed[2] = {12., 4.}, lone = elt == 2 ? 1. : 0.85;
   Shape8 best = {};
   double best_us = 0.;
   for (int v = elt == 2 ? kBig : kMid; v <= kMid; ++v)
@@ -49,7 +51,7 @@ inline Shape8 shape8(int64_t M, int64_t N, int64_t K, int elt) {
       const bool alone = each * splits <= 256.;
       const double rounds = alone ? 1. : std::max(1. + last, std::ceil(each * (splits - 1 + last) / 256.));
       const int64_t side = v == kBig ? 256 : 128;
-      double us = rounds * (2. * side * side * g.sps * 128 / (rate[v] * (alone && v == kMid ? 0.8 : 1.)) + fixed[v]);
+      double us = rounds * (2. * side * side * g.sps * 128 / (rate[v] * (alone && v == kMid ? lone : 1.)) + fixed[v]);
       if (g.splits > 1) us += 3. + 8. * g.splits * M * N / 6.0e6;
       if (best_us == 0. || us < best_us) {
         best = g;
