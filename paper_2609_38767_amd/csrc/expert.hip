@@ -297,8 +297,9 @@ template <int OP, int ELT>
 hipError_t launch_product(const GemmArgs& a, const ExpertArgs& x, hipStream_t s) {
   constexpr bool AC = OP != DATTRI_LINEAR_WEIGHT_GRAD, BC = OP == DATTRI_LINEAR_FORWARD;
   const Variant v = expert_shape(!AC, x.rows, x.experts, a.M, a.N, a.K, ELT);
-  if (v == kBig) return launch_tiles<OP, ELT, stage_bytes(AC, BC, ELT, 256), 2, 2, 4, 4>(a, x, s);
-  if (v == kMid || !AC) return launch_tiles<OP, ELT, stage_bytes(AC, BC, ELT, 128), 2, 2, 2, 2>(a, x, s);
+  if constexpr (AC || ELT == 2)
+    if (v == kBig) return launch_tiles<OP, ELT, stage_bytes(AC, BC, ELT, 256), 2, 2, 4, 4>(a, x, s);
+  if (v == kMid) return launch_tiles<OP, ELT, stage_bytes(AC, BC, ELT, 128), 2, 2, 2, 2>(a, x, s);
   if constexpr (AC) {
     if (v == kSlim) return launch_tiles<OP, ELT, 64, 2, 2, 1, 2>(a, x, s);
     return launch_tiles<OP, ELT, 64, 1, 4, 1, 1>(a, x, s);
