@@ -102,13 +102,17 @@ struct Segments {
 
 }  // namespace
 
-// Products over rows: grid as many tiles as there can be (tiles, 1, more tiles).
+// Products over rows: grid as many tiles as there can be (tiles, splits of k, more
+// tiles); split y runs stages [y * sps, (y + 1) * sps), with several splits (OP
+// kPartial) part holds them as [split][rows][ld_part].
 // Of 256 x 256 tiles a segment's last is half empty on average: where it would be
 // half empty or more, a tile of 128 x 256 takes its place, behind the others, in
 // half the time.  (Tiles of 128 x 128 for all last rows: 64 experts of 4096 ->
 // 1024, 32768 rows, 455 us, whole tiles 371; alone on a CU they are slow.)
 template <int OP, bool BC, int ELT, int KW, int WM, int WN, int BM, int BN>
-__global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void expert_rows_kernel(GemmArgs a, ExpertArgs x, int nn) {
+__global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void expert_rows_kernel(GemmArgs a, ExpertArgs x, int nn,
+                                                                                 int sps, float* __restrict__ part,
+                                                                                 int64_t ld_part) {
   constexpr int TM = WM * BM * 32, TN = WN * BN * 32, BK = KW / ELT;
   constexpr bool kHalves = TM == 256;
   typedef TileBuffers<true, BC, ELT, KW, WM, WN, BM, BN> Buffers;
@@ -125,15 +129,17 @@ __global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void expert_rows_kernel
       a.B = (const uint8_t*)a.B + (int64_t)e * x.stride * ELT;
       if (a.bias) a.bias = (const uint8_t*)a.bias + (int64_t)e * a.N * ELT;
     }
-    product((int)(((int64_t)a.K + BK - 1) / BK));
+    const int all = (int)(((int64_t)a.K + BK - 1) / BK), s0 = blockIdx.y * sps, ns = min(sps, all - s0);
+    product(s0, ns, (int)min((int64_t)a.K, (int64_t)(s0 + ns) * BK));
   };
+  part += (int64_t)blockIdx.y * x.rows * ld_part;
   const int n = all.template total<kHalves ? kFull : kAll>();
   int mt, nt;
   if (tile < (int64_t)n * nn) {
     tile_of((int)tile, n, nn, &mt, &nt);
     const Place p = all.template find<kHalves ? kFull : kAll>(mt);
-    run(p, [&](int stages) DATTRI_INLINE {
-      tile_product<OP, true, BC, ELT, KW, WM, WN, BM, BN>(a, p.m0, nt * TN, 0, stages, a.K, nullptr, 0, x0, x1, x2, x3);
+    run(p, [&](int s0, int ns, int k_end) DATTRI_INLINE {
+      tile_product<OP, true, BC, ELT, KW, WM, WN, BM, BN>(a, p.m0, nt * TN, s0, ns, k_end, part, ld_part, x0, x1, x2, x3);
     });
     return;
   }
@@ -143,17 +149,19 @@ __global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void expert_rows_kernel
     if (half >= (int64_t)rest * nn) return;
     tile_of((int)half, rest, nn, &mt, &nt);
     const Place p = all.template find<kRest>(mt);
-    run(p, [&](int stages) DATTRI_INLINE {
-      tile_product<OP, true, BC, ELT, KW, 2, 2, 2, 4>(a, p.m0, nt * TN, 0, stages, a.K, nullptr, 0, x0, x1, x2, x3);
+    run(p, [&](int s0, int ns, int k_end) DATTRI_INLINE {
+      tile_product<OP, true, BC, ELT, KW, 2, 2, 2, 4>(a, p.m0, nt * TN, s0, ns, k_end, part, ld_part, x0, x1, x2, x3);
     });
   }
 }
 
-// Weight gradients: experts times nm times nn tiles.
-template <int ELT, int KW, int WM, int WN, int BM, int BN>
+// Weight gradients: experts times nm times nn tiles, grid as above; the splits of k
+// cut each expert's rows, part holds [split][experts * M][ld_part].
+template <int OP, int ELT, int KW, int WM, int WN, int BM, int BN>
 __global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void expert_weight_kernel(GemmArgs a, ExpertArgs x, int nm,
-                                                                                   int nn) {
-  constexpr int BK = KW / ELT;
+                                                                                   int nn, float* __restrict__ part,
+                                                                                   int64_t ld_part) {
+  constexpr int BK = KW / ELT, kRound = buffers_of(KW);
   typedef TileBuffers<false, false, ELT, KW, WM, WN, BM, BN> Buffers;
   DATTRI_TILE_BUFFERS(Buffers);
   const int64_t tile = (int64_t)blockIdx.z * gridDim.x + blockIdx.x;
@@ -162,14 +170,45 @@ __global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void expert_weight_kern
   int mt, nt;
   tile_of((int)(tile - (int64_t)e * nm * nn), nm, nn, &mt, &nt);
   const Segment g = segment(x, e + 1);
-  if (a.accumulate && g.begin == g.end) return;
+  if (OP != kPartial && a.accumulate && g.begin == g.end) return;
   a.K = g.end - g.begin;
   a.A = (const uint8_t*)a.A + (int64_t)g.begin * a.lda * ELT;
   a.B = (const uint8_t*)a.B + (int64_t)g.begin * a.ldb * ELT;
   a.out = (float*)a.out + (int64_t)e * x.stride;
-  tile_product<DATTRI_LINEAR_WEIGHT_GRAD, false, false, ELT, KW, WM, WN, BM, BN>(
-      a, mt * WM * BM * 32, nt * WN * BN * 32, 0, (int)(((int64_t)a.K + BK - 1) / BK), a.K, nullptr, 0, x0, x1,
-      x2, x3);
+  part += ((int64_t)blockIdx.y * x.experts + e) * a.M * ld_part;
+  const int all = (int)(((int64_t)a.K + BK - 1) / BK), splits = gridDim.y,
+            sps = splits > 1 ? ((all + splits - 1) / splits + kRound - 1) / kRound * kRound : all;
+  const int s0 = (int)min((int64_t)blockIdx.y * sps, (int64_t)all), ns = min(sps, all - s0);
+  tile_product<OP, false, false, ELT, KW, WM, WN, BM, BN>(a, mt * WM * BM * 32, nt * WN * BN * 32, s0, ns,
+                                                          (int)min((int64_t)a.K, (int64_t)(s0 + ns) * BK), part, ld_part,
+                                                          x0, x1, x2, x3);
+}
+
+// Sums of a split product over rows in split order, and the epilogue with the
+// bias of the row's expert: the last one whose rows begin at or before it.
+template <int OP, int ELT>
+__global__ __launch_bounds__(256) void expert_join_kernel(GemmArgs a, ExpertArgs x, const float* __restrict__ part,
+                                                          int64_t ld_part, int splits) {
+  const int nv = (a.N + 3) / 4;
+  const int64_t total = (int64_t)a.M * nv, step = (int64_t)a.M * ld_part;
+  const uint8_t* const bias = (const uint8_t*)a.bias;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int m = (int)(i / nv), n = (int)(i - (int64_t)m * nv) * 4;
+    const float* p = part + m * ld_part + n;
+    f32x4 s = *(const f32x4*)p;
+#pragma unroll 4
+    for (int y = 1; y < splits; ++y) s += *(const f32x4*)(p + y * step);
+    if (bias) {
+      int lo = -1, hi = x.experts;  // boundary(lo) <= m < boundary(hi + 1), experts + 1 boundaries
+      while (lo < hi) {
+        const int mid = lo + (hi - lo + 1) / 2;
+        if (boundary(x, mid) <= m) lo = mid;
+        else hi = mid - 1;
+      }
+      a.bias = lo < 0 || lo >= x.experts ? nullptr : bias + (int64_t)lo * a.N * ELT;
+    }
+    epilogue4<OP, ELT>(a, m, n, s);
+  }
 }
 
 // Column sums of an expert's rows: grid (64 C columns, parts, experts); part y of
@@ -240,7 +279,8 @@ int64_t column_parts(int64_t rows, int64_t experts, int64_t cols) {
 struct ExpertLayout {
   int64_t a_rows, a_w, b_rows, b_w;  // as stored
   bool pack_a, pack_b;
-  size_t off_a, off_b, off_cols, total;
+  size_t off_a, off_b, off_part, off_cols, total;
+  ExpertShape g;
 };
 ExpertLayout expert_layout(dattri_linear_op op, int64_t rows, int64_t experts, int64_t d_in, int64_t d_out, int elt,
                            bool aligned) {
@@ -261,6 +301,10 @@ ExpertLayout expert_layout(dattri_linear_op op, int64_t rows, int64_t experts, i
   auto packed = [&](int64_t r, int64_t w) { return (size_t)r * (size_t)((w * elt + 15) / 16 * 16); };
   L.off_a = take(L.pack_a ? packed(L.a_rows, L.a_w) : 0);
   L.off_b = take(L.pack_b ? packed(L.b_rows, L.b_w) : 0);
+  const int64_t m = wgrad ? d_out : rows, n = op == DATTRI_LINEAR_FORWARD ? d_out : d_in,
+                k = op == DATTRI_LINEAR_FORWARD ? d_in : wgrad ? rows : d_out;
+  L.g = expert_shape(wgrad, rows, experts, m, n, k, elt, op == DATTRI_LINEAR_FORWARD);
+  L.off_part = take(L.g.splits > 1 ? (size_t)L.g.splits * (wgrad ? experts * m : m) * ((n + 3) / 4 * 4) * 4 : 0);
   L.off_cols = off;
   if (wgrad) {
     const int64_t parts = column_parts(rows, experts, d_out);
@@ -270,39 +314,62 @@ ExpertLayout expert_layout(dattri_linear_op op, int64_t rows, int64_t experts, i
   return L;
 }
 
-template <int OP, int ELT, int KW, int WM, int WN, int BM, int BN>
-hipError_t launch_tiles(const GemmArgs& a, const ExpertArgs& x, hipStream_t s) {
+// OP kPartial: partial sums of splits to part, else the whole product.
+template <int OP, int REAL, int ELT, int KW, int WM, int WN, int BM, int BN>
+hipError_t launch_grid(const GemmArgs& a, const ExpertArgs& x, int splits, float* part, int64_t ldp, hipStream_t s) {
   constexpr int TM = WM * BM * 32, TN = WN * BN * 32;
   const int64_t nn = ((int64_t)a.N + TN - 1) / TN;
-  dim3 grid;
-  if constexpr (OP == DATTRI_LINEAR_WEIGHT_GRAD) {
+  dim3 grid(1, (unsigned)splits);
+  if constexpr (REAL == DATTRI_LINEAR_WEIGHT_GRAD) {
     const int64_t nm = ((int64_t)a.M + TM - 1) / TM;
     if (nm * nn > INT32_MAX) return hipErrorInvalidValue;
     const hipError_t e = row_grid(x.experts * nm * nn, &grid, 256, true);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((expert_weight_kernel<ELT, KW, WM, WN, BM, BN>), grid, dim3(256), 0, s, a, x, (int)nm, (int)nn);
+    hipLaunchKernelGGL((expert_weight_kernel<OP, ELT, KW, WM, WN, BM, BN>), grid, dim3(256), 0, s, a, x, (int)nm,
+                       (int)nn, part, ldp);
   } else {
     // every segment with rows has at most one tile row more than its rows fill
     const int64_t n = (x.rows / TM + std::min<int64_t>(x.experts + 2, x.rows)) * nn;
     if (n > INT32_MAX) return hipErrorInvalidValue;
     const hipError_t e = row_grid(n, &grid, 256, true);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((expert_rows_kernel<OP, OP == DATTRI_LINEAR_FORWARD, ELT, KW, WM, WN, BM, BN>), grid, dim3(256),
-                       0, s, a, x, (int)nn);
+    const int64_t stages = ((int64_t)a.K * ELT + KW - 1) / KW, round = buffers_of(KW),
+                  sps = splits > 1 ? ((stages + splits - 1) / splits + round - 1) / round * round : stages;
+    hipLaunchKernelGGL((expert_rows_kernel<OP, REAL == DATTRI_LINEAR_FORWARD, ELT, KW, WM, WN, BM, BN>), grid,
+                       dim3(256), 0, s, a, x, (int)nn, (int)sps, part, ldp);
   }
   return hipGetLastError();
 }
 
+template <int OP, int ELT, int KW, int WM, int WN, int BM, int BN>
+hipError_t launch_tiles(const GemmArgs& a, const ExpertArgs& x, int splits, float* part, hipStream_t s) {
+  const int64_t ldp = ((int64_t)a.N + 3) / 4 * 4;
+  if constexpr (expert_splits(BM * BN == 16 ? kBig : BM * BN == 4 ? kMid : BM * BN == 2 ? kSlim : kFew, ELT)) {
+    if (splits > 1) {
+      const hipError_t e = launch_grid<kPartial, OP, ELT, KW, WM, WN, BM, BN>(a, x, splits, part, ldp, s);
+      if (e != hipSuccess) return e;
+      GemmArgs j = a;  // all rows of the buffers
+      if (OP == DATTRI_LINEAR_WEIGHT_GRAD) j.M = (int)(x.experts * (int64_t)a.M);
+      const dim3 grid((unsigned)std::min<int64_t>(((int64_t)j.M * (ldp / 4) + 255) / 256, 16384));
+      if constexpr (OP == DATTRI_LINEAR_WEIGHT_GRAD)
+        hipLaunchKernelGGL((gemm_join_kernel<OP, ELT>), grid, dim3(256), 0, s, j, part, ldp, splits);
+      else
+        hipLaunchKernelGGL((expert_join_kernel<OP, ELT>), grid, dim3(256), 0, s, j, x, part, ldp, splits);
+      return hipGetLastError();
+    }
+  }
+  return launch_grid<OP, OP, ELT, KW, WM, WN, BM, BN>(a, x, 1, nullptr, 0, s);
+}
+
 template <int OP, int ELT>
-hipError_t launch_product(const GemmArgs& a, const ExpertArgs& x, hipStream_t s) {
+hipError_t launch_product(const GemmArgs& a, const ExpertArgs& x, const ExpertShape& g, float* part, hipStream_t s) {
   constexpr bool AC = OP != DATTRI_LINEAR_WEIGHT_GRAD, BC = OP == DATTRI_LINEAR_FORWARD;
-  const Variant v = expert_shape(!AC, x.rows, x.experts, a.M, a.N, a.K, ELT);
   if constexpr (AC || ELT == 2)
-    if (v == kBig) return launch_tiles<OP, ELT, stage_bytes(AC, BC, ELT, 256), 2, 2, 4, 4>(a, x, s);
-  if (v == kMid) return launch_tiles<OP, ELT, stage_bytes(AC, BC, ELT, 128), 2, 2, 2, 2>(a, x, s);
+    if (g.v == kBig) return launch_tiles<OP, ELT, stage_bytes(AC, BC, ELT, 256), 2, 2, 4, 4>(a, x, 1, part, s);
+  if (g.v == kMid) return launch_tiles<OP, ELT, stage_bytes(AC, BC, ELT, 128), 2, 2, 2, 2>(a, x, g.splits, part, s);
   if constexpr (AC) {
-    if (v == kSlim) return launch_tiles<OP, ELT, 64, 2, 2, 1, 2>(a, x, s);
-    return launch_tiles<OP, ELT, 64, 1, 4, 1, 1>(a, x, s);
+    if (g.v == kSlim) return launch_tiles<OP, ELT, 64, 2, 2, 1, 2>(a, x, g.splits, part, s);
+    return launch_tiles<OP, ELT, 64, 1, 4, 1, 1>(a, x, g.splits, part, s);
   }
   return hipErrorInvalidValue;
 }
@@ -359,14 +426,15 @@ hipError_t launch_expert(dattri_linear_op op, int elt, bool aligned, GemmArgs a,
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
   }
+  float* part = (float*)(ws + L.off_part);
   if (op == DATTRI_LINEAR_FORWARD)
-    return elt == 2 ? launch_product<DATTRI_LINEAR_FORWARD, 2>(a, x, s)
-                    : launch_product<DATTRI_LINEAR_FORWARD, 4>(a, x, s);
+    return elt == 2 ? launch_product<DATTRI_LINEAR_FORWARD, 2>(a, x, L.g, part, s)
+                    : launch_product<DATTRI_LINEAR_FORWARD, 4>(a, x, L.g, part, s);
   if (op == DATTRI_LINEAR_INPUT_GRAD)
-    return elt == 2 ? launch_product<DATTRI_LINEAR_INPUT_GRAD, 2>(a, x, s)
-                    : launch_product<DATTRI_LINEAR_INPUT_GRAD, 4>(a, x, s);
-  return elt == 2 ? launch_product<DATTRI_LINEAR_WEIGHT_GRAD, 2>(a, x, s)
-                  : launch_product<DATTRI_LINEAR_WEIGHT_GRAD, 4>(a, x, s);
+    return elt == 2 ? launch_product<DATTRI_LINEAR_INPUT_GRAD, 2>(a, x, L.g, part, s)
+                    : launch_product<DATTRI_LINEAR_INPUT_GRAD, 4>(a, x, L.g, part, s);
+  return elt == 2 ? launch_product<DATTRI_LINEAR_WEIGHT_GRAD, 2>(a, x, L.g, part, s)
+                  : launch_product<DATTRI_LINEAR_WEIGHT_GRAD, 4>(a, x, L.g, part, s);
 }
 
 }  // namespace dattri

@@ -1,5 +1,6 @@
-// Which tiles the experts' products take (host only, no HIP).  Nothing of the
-// boundaries is known here: the choice goes by the mean rows of an expert.
+// How the experts' products are cut (host only, no HIP): tiles, splits of k.
+// Nothing of the boundaries is known here: the choice goes by the mean rows of an
+// expert.
 #pragma once
 
 #include <stdint.h>
@@ -11,20 +12,32 @@
 
 namespace dattri {
 
-// The tiles with the least modelled time, in us: FLOP at the rate that a CU
-// reaches with them on many rows, what a tile costs besides, the rounds of tiles
-// over the CUs (the largest tiles come one per CU, others share it), and the
-// bytes of operands and weights met at 5 TB/s, of which the smaller part is
-// hidden but for three tenths.
+struct ExpertShape {
+  Variant v;
+  int kw;      // bytes of k per stage
+  int splits;  // of k: an expert's rows (weight gradients), else all of it
+};
+
+// Whether tiles are split along k at all: the largest have work enough, and float32
+// ones of 64 x 128 lie too near to 32 x 128 whole.
+constexpr bool expert_splits(Variant v, int elt) { return v != kBig && !(v == kSlim && elt == 4); }
+
+// The cut with the least modelled time, in us: FLOP at the rate that a CU reaches
+// with its tiles on many rows, what a tile costs besides, the rounds of tiles over
+// the CUs (the largest tiles come one per CU, others share it), the partial tiles
+// of a split written, read and joined, and the bytes of operands and weights met
+// at 5 TB/s, of which the smaller part is hidden but for three tenths.
 //   m, n, k as in GemmArgs; rows take the place of m in products over rows, and
 //   the mean rows of an expert that of k in weight gradients.
 // Measured, bf16, us with 256 x 256 / 128 x 128 / 64 x 128 / 32 x 128 tiles:
 // forward 4096 -> 14336, eight experts: 16 rows 206/143/135/133, 256 rows
 // 215/192/185/203, 1024 rows 242/263/309/485, 16384 rows 1692/2435/3498/6390; 64
 // experts of 4096 -> 1024, 32768 rows 371/449/566/876.  float32, five experts of
-// 769 -> 1030, 1531 rows: 284/75/50/50.
+// 769 -> 1030, 1531 rows: 284/75/50/50; one of 3232 -> 392, 28 rows, without a
+// split: 64 in 32 x 128.
 // float32 weight gradients take 128 x 128 always: larger tiles reach 3% more at most.
-inline Variant expert_shape(bool weight_grad, int64_t rows, int64_t experts, int64_t m, int64_t n, int64_t k, int elt) {
+inline ExpertShape expert_shape(bool weight_grad, int64_t rows, int64_t experts, int64_t m, int64_t n, int64_t k,
+                                int elt, bool bc) {
   const double rate[4] = {elt == 2 ? 5.2e6 : 0.58e6, elt == 2 ? 3.4e6 : 0.565e6, elt == 2 ? 2.4e6 : 0.5e6,
                           elt == 2 ? 1.4e6 : 0.45e6},
                fixed[4] = {12., 3., 2., 1.5};
@@ -32,25 +45,36 @@ inline Variant expert_shape(bool weight_grad, int64_t rows, int64_t experts, int
   const double mean = (double)rows / experts;
   const double bytes = weight_grad ? 4. * experts * m * n + (double)elt * rows * (m + n)
                                    : (double)elt * (met * n * k + rows * (n + k));
-  if (weight_grad && elt == 4) return kMid;
-  Variant best = kMid;
+  ExpertShape best = {};
   double best_us = 0.;
-  for (int v = kBig; v <= (weight_grad ? kMid : kFew); ++v) {
+  for (int v = weight_grad && elt == 4 ? kMid : kBig; v <= (weight_grad ? kMid : kFew); ++v) {
     const int64_t tm = v == kBig ? 256 : v == kMid ? 128 : v == kSlim ? 64 : 32, tn = v == kBig ? 256 : 128;
+    const int kw = stage_bytes(!weight_grad, bc, elt, (int)tm);
     const double nn = (double)((n + tn - 1) / tn);
     // an expert's last tile is half empty on average, and none has less than one
     const double nm = weight_grad ? (double)experts * ((m + tm - 1) / tm)
                                   : std::max((double)met, (double)rows / tm + 0.5 * met);
-    const double tiles = nm * nn / 256., depth = weight_grad ? mean : (double)k;
-    // weight gradients: an expert of many rows makes long tiles, which many short ones even out
-    const double rounds = weight_grad ? std::max(1., tiles + (v == kBig ? 1. : 0.5))
-                          : v <= kMid ? std::max(1., std::ceil(tiles)) : std::max(1., tiles + 0.5);
-    const double work = rounds * (2. * tm * tn * depth / rate[v] + fixed[v]), read = bytes / 5.e6;
-    const double us = std::max(work, read) + 0.3 * std::min(work, read);
-    if (best_us == 0. || us < best_us) {
-      best = (Variant)v;
-      best_us = us;
+    const double depth = weight_grad ? mean : (double)k;
+    for (int splits = 1; splits <= (expert_splits((Variant)v, elt) ? 32 : 1); ++splits) {
+      if (splits > 1 && depth * elt / splits < 512.) break;
+      const double tiles = nm * nn * splits / 256.;
+      // weight gradients: an expert of many rows makes long tiles, which many short ones even out
+      const double rounds = weight_grad ? std::max(1., tiles + (v == kBig ? 1. : 0.5))
+                            : v <= kMid ? std::max(1., std::ceil(tiles)) : std::max(1., tiles + 0.5);
+      const double work = rounds * (2. * tm * tn * depth / splits / rate[v] + fixed[v]), read = bytes / 5.e6;
+      double us = std::max(work, read) + 0.3 * std::min(work, read);
+      if (splits > 1)  // and only where the gain is clear: 64 rows of 14336 <- 4096, eight experts, 137 us whole, 160 in five
+        us = 1.1 * us + 4. + 8. * splits * (weight_grad ? (double)experts * m : (double)rows) * n / 5.e6;
+      if (best_us == 0. || us < best_us) {
+        best = ExpertShape{(Variant)v, kw, splits};
+        best_us = us;
+      }
     }
+  }
+  if (best.splits > 1 && !weight_grad) {  // whole rounds of the buffers
+    const int64_t stages = (k * elt + best.kw - 1) / best.kw, round = buffers_of(best.kw),
+                  sps = ((stages + best.splits - 1) / best.splits + round - 1) / round * round;
+    best.splits = (int)((stages + sps - 1) / sps);
   }
   return best;
 }

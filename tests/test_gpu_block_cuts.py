@@ -62,7 +62,7 @@ def boundaries(n, e, seed):
 
 @pytest.mark.parametrize("cut", CUTSX, ids=lambda c: "-".join(map(str, c)))
 def test_expert_products(cut):
-    op, dtype, n, e, i, o, _ = cut
+    op, dtype, n, e, i, o, _, _ = cut
     k = CUTSX.index(cut)
     g, f = gen(50 + k), boundaries(n, e, k)
     off = torch.tensor(f, dtype=torch.int32, device="cuda")
@@ -70,6 +70,9 @@ def test_expert_products(cut):
     if op == 2:
         gr, x = rand(g, n, o, dtype=dtype), rand(g, n, i, dtype=dtype)
         dw, db = layers().expert_linear_weight_grad(gr, x, off, bias=True)
+        twice = dw.clone()
+        layers().expert_linear_weight_grad(gr, x, off, out=twice, accumulate=True)
+        assert torch.equal(twice, 2 * dw)
         for q, s in at:
             if q is not None:
                 a, c = host(gr[s]), host(x[s])
@@ -78,9 +81,9 @@ def test_expert_products(cut):
         return
     a, w = rand(g, n, i if op == 0 else o, dtype=dtype), rand(g, e, o, i, dtype=dtype, std=0.1)
     wide = o if op == 0 else i
-    r = rand(g, n, wide, dtype=dtype)
+    r, b = rand(g, n, wide, dtype=dtype), rand(g, e, o, dtype=dtype)
     if op == 0:
-        got = layers().expert_linear(a, w, off, residual=r)
+        got = layers().expert_linear(a, w, off, b, residual=r)
     else:
         got = layers().expert_linear_input_grad(a, w, off, residual=r)
     want, bound = np.zeros((n, wide)), np.zeros((n, wide))
@@ -88,6 +91,8 @@ def test_expert_products(cut):
         if q is not None:
             m = host(w[q]).T.copy() if op == 0 else host(w[q])
             want[s], bound[s] = matmul64(host(a[s]), m), bound64(host(a[s]), m)
+            if op == 0:
+                want[s] += host(b[q])
     bound = bound + 2 * U * (np.abs(want) + np.abs(host(r)))
     want = want + host(r)
     check(got, want, bound + OUT[dtype] * (np.abs(want) + bound))

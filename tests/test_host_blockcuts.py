@@ -25,7 +25,8 @@ int main() {
       printf("%d %d %d\n", (int)g.v, g.splits, g.sps);
     } else {  // op, elt, rows, experts, d_in, d_out
       const long op = a[0], m = op == 2 ? a[5] : a[2], n = op == 0 ? a[5] : a[4], k = op == 0 ? a[4] : op == 1 ? a[5] : a[2];
-      printf("%d 1 0\n", (int)dattri::expert_shape(op == 2, a[2], a[3], m, n, k, (int)a[1]));
+      const dattri::ExpertShape g = dattri::expert_shape(op == 2, a[2], a[3], m, n, k, (int)a[1], op == 0);
+      printf("%d %d %d\n", (int)g.v, g.splits, g.kw);
     }
   }
 }
@@ -75,9 +76,19 @@ def test_no_other_cut_is_reached(ask):
         assert v4 != 0 and (v4 == v2 == 3) == (n <= 16) and (n > 16 or s4 == s2 == 1)
 
 
-def test_expert_sizes_take_the_tiles_they_stand_for(ask):
-    got = ask([f"e {op} {elt(t)} {n} {e} {i} {o}" for op, t, n, e, i, o, _ in CUTSX])
-    assert [TILES[v] for v, _, _ in got] == [c[6] for c in CUTSX]
-    ways = {(op, t, tile) for op in (0, 1) for t in ("f32", "bf16") for tile in TILES}
-    ways |= {(2, "f32", "128x128"), (2, "bf16", "128x128"), (2, "bf16", "256x256")}
-    assert {(c[0], c[1], c[6]) for c in CUTSX} == ways
+def test_expert_sizes_take_the_cut_they_stand_for(ask):
+    got = ask([f"e {op} {elt(t)} {n} {e} {i} {o}" for op, t, n, e, i, o, _, _ in CUTSX])
+    assert [(TILES[v], splits > 1) for v, splits, _ in got] == [c[6:] for c in CUTSX]
+    ways = {(op, t, tile, s) for op in (0, 1) for t in ("f32", "bf16") for tile in TILES for s in (False, True)
+            if not (s and (tile == "256x256" or (tile == "64x128" and t == "f32")))}
+    ways |= {(2, t, "128x128", s) for t in ("f32", "bf16") for s in (False, True)} | {(2, "bf16", "256x256", False)}
+    assert {(c[0], c[1], c[6], c[7]) for c in CUTSX} == ways
+
+
+def test_no_other_expert_cut_is_reached(ask):
+    """256 x 256 is never split, nor float32 in 64 x 128; float32 weight gradients take 128 x 128, whatever the size."""
+    sizes = [(n, e, i, o) for n in (1, 50, 3000, 100000) for e in (1, 9, 300) for i in (8, 700, 16384) for o in (40, 5000)]
+    for op in range(3):
+        for b in (2, 4):
+            for (n, e, i, o), (v, splits, _) in zip(sizes, ask([f"e {op} {b} {n} {e} {i} {o}" for n, e, i, o in sizes])):
+                assert 1 <= splits <= 32 and (splits == 1 or v == 1 or v == 3 or (v == 2 and b == 2)) and (op < 2 or v == 1 or (v == 0 and b == 2))
