@@ -305,8 +305,8 @@ def rms_norm(x, weight, residual=None, eps=1e-6, out=None, out_sum=None, stream=
 def rms_norm_8bit(x, weight, residual=None, eps=1e-6, keep=False, out=None, out_sum=None, stream=None):
     """rms_norm with its result in 8 bits: (values [..., d] float8_e4m3fn, scales
     [..., ceil(d / 128)] float32), what ``linear_8bit`` takes for its rows.
-    Returns that pair; with keep=True or a residual a tuple of it, y (keep) and
-    h (residual)."""
+    Returns that pair; with keep=True (or `out`) or a residual a tuple of it, y
+    and h as far as they are there."""
     return _norm(x, weight, residual, eps, out, out_sum, keep or out is not None, True, stream)
 
 
@@ -416,6 +416,8 @@ def transpose_8bit(weight):
     """The transposed 8-bit weight, with which ``linear_8bit`` carries a gradient
     back through the layer.  Laid out once, beside the weight."""
     q, s = weight
+    if q.dtype != torch.float8_e4m3fn or q.dim() != 2 or s.shape != (_groups(q.shape[0]), _groups(q.shape[1])):
+        raise ValueError("weight must be float8_e4m3fn of two axes with a scale for each 128 x 128 block")
     return q.view(torch.uint8).t().contiguous().view(torch.float8_e4m3fn), s.t().contiguous()
 
 

@@ -69,7 +69,7 @@ def test_forward(size, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("size,pad", [((9, 40, 24), 8), ((70, 136, 200), 3), ((1, 257, 129), 5), ((300, 528, 40), 16)])
+@pytest.mark.parametrize("size,pad", [((9, 40, 24), 8), ((9, 48, 24), 16), ((70, 136, 200), 3), ((1, 257, 129), 5), ((300, 528, 40), 16)])
 def test_strided_rows_and_in_place(size, pad, dtype):
     """Rows between NaN bytes, scales in padded rows, outputs in padded rows, the residual overwritten."""
     n, i, o = size

@@ -137,5 +137,8 @@ def test_layers_refuse_on_the_host():
                  lambda: m.expert_linear(x, x, x), lambda: m.expert_linear_weight_grad(x, x, x)):
         with pytest.raises(ValueError, match="on the GPU"):
             call()
-    q, s = m.transpose_8bit((torch.zeros(3, 8).to(torch.float8_e4m3fn), torch.ones(1, 2)))
-    assert q.shape == (8, 3) and s.shape == (2, 1) and q.is_contiguous()
+    q, s = m.transpose_8bit((torch.zeros(3, 200).to(torch.float8_e4m3fn), torch.ones(1, 2)))
+    assert q.shape == (200, 3) and s.shape == (2, 1) and q.is_contiguous()
+    for bad in ((torch.zeros(3, 8), torch.ones(1, 1)), (q, torch.ones(1, 2)), (q[0], torch.ones(1))):
+        with pytest.raises(ValueError, match="128 x 128"):
+            m.transpose_8bit(bad)
