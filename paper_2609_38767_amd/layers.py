@@ -323,15 +323,19 @@ def _norm(x, weight, residual, eps, out, out_sum, keep, eight, stream):
     if out_sum is not None and residual is None:
         raise ValueError("out_sum needs a residual")
     given = [t for t in (out, out_sum) if t is not None]
-    if keep and out is None:
+    ld_y = ld_h = 0  # dense, as what is made here is
+    if out is not None:
+        ld_y = _rows(out, "out", dt, x.shape)[2]
+    elif keep:
         out = _like(x)
-    if residual is not None and out_sum is None:
+    if out_sum is not None:
+        ld_h = _rows(out_sum, "out_sum", dt, x.shape)[2]
+    elif residual is not None:
         out_sum = _like(x)
-    ld_y = _rows(out, "out", dt, x.shape)[2] if out is not None else 0
-    ld_h = _rows(out_sum, "out_sum", dt, x.shape)[2] if out_sum is not None else 0
     q, s = _eight_bit_rows(x) if eight else (None, None)
     dattri_rms_norm(x, ld_x, residual, ld_r, weight, eps, out, ld_y, out_sum, ld_h, q, 0, s, 0, n, d, code)
-    _changed(given)
+    if given:
+        _changed(given)
     got = ([(q, s)] if eight else []) + [t for t in (out, out_sum) if t is not None]
     return got[0] if len(got) == 1 else tuple(got)
 
@@ -355,17 +359,21 @@ def rms_norm_grad(g, h, weight, eps=1e-6, residual=None, weight_grad=True, out=N
     if accumulate and (out_weight is None or not weight_grad):
         raise ValueError("accumulate needs out_weight")
     given = [t for t in (out, out_weight if weight_grad else None) if t is not None]
+    ld_d = 0
     if out is None:
         out = _like(g)
-    ld_d = _rows(out, "out", dt, g.shape)[2]
-    if weight_grad and out_weight is None:
-        out_weight = torch.empty(d, dtype=torch.float32, device=g.device)
+    else:
+        ld_d = _rows(out, "out", dt, g.shape)[2]
     if weight_grad:
-        _vector(out_weight, "out_weight", d, torch.float32)
+        if out_weight is None:
+            out_weight = weight.new_empty((d,), dtype=torch.float32)
+        else:
+            _vector(out_weight, "out_weight", d, torch.float32)
     ws_bytes = dattri_rms_norm_grad_workspace_bytes(n, d, code, weight_grad)
     dattri_rms_norm_grad(g, ld_g, h, ld_h, weight, eps, residual, ld_p, out, ld_d, out_weight if weight_grad else None,
                          accumulate, n, d, code, _workspace(ws_bytes, g.device), ws_bytes)
-    _changed(given)
+    if given:
+        _changed(given)
     return (out, out_weight) if weight_grad else out
 
 
@@ -444,10 +452,11 @@ def linear_8bit(x, weight, bias=None, act="none", residual=None, keep_preact=Fal
     if bias is not None:
         _vector(bias, "bias", d_out, dtype)
     ld_r = _rows(residual, "residual", dtype, shape)[2] if residual is not None else 0
-    given = out
+    given, ld_y = out, 0
     if out is None:
         out = x.new_empty(shape, dtype=dtype)
-    ld_y = _rows(out, "out", dtype, shape)[2]
+    else:
+        ld_y = _rows(out, "out", dtype, shape)[2]
     z = _like(out) if keep_preact else None
     ws_bytes = dattri_linear_scaled_workspace_bytes(n, d_in, d_out, code, _on_16(x, ld_x) and _on_16(weight, ld_w))
     dattri_linear_scaled(x, ld_x, sx, ld_sx, weight, ld_w, sw, ld_sw, bias, _act(act), residual, ld_r, out, ld_y, z, 0, n,
@@ -498,10 +507,11 @@ def expert_linear(x, weight, offsets, bias=None, act="none", residual=None, keep
     if bias is not None:
         _bias_rows(bias, "bias", e, d_out, dt)
     ld_r = _rows(residual, "residual", dt, shape)[2] if residual is not None else 0
-    given = out
+    given, ld_y = out, 0
     if out is None:
         out = x.new_empty(shape)
-    ld_y = _rows(out, "out", dt, shape)[2]
+    else:
+        ld_y = _rows(out, "out", dt, shape)[2]
     z = _like(out) if keep_preact else None
     ws_bytes = dattri_expert_linear_workspace_bytes(DATTRI_LINEAR_FORWARD, n, e, d_in, d_out, code,
                                                     _on_16(x, ld_x) and _on_16(weight, ld_w))
@@ -529,10 +539,11 @@ def expert_linear_input_grad(g, weight, offsets, residual=None, act="none", prea
         raise ValueError(f"act={act!r} needs preact")
     ld_r = _rows(residual, "residual", dt, shape)[2] if residual is not None else 0
     ld_z = _rows(preact, "preact", dt, shape)[2] if preact is not None else 0
-    given = out
+    given, ld_p = out, 0
     if out is None:
         out = g.new_empty(shape)
-    ld_p = _rows(out, "out", dt, shape)[2]
+    else:
+        ld_p = _rows(out, "out", dt, shape)[2]
     d = _like(out) if both else None
     ws_bytes = dattri_expert_linear_workspace_bytes(DATTRI_LINEAR_INPUT_GRAD, n, e, d_in, d_out, code,
                                                     _on_16(g, ld_g) and _on_16(weight, ld_w))
