@@ -367,10 +367,9 @@ hipError_t launch_product(const GemmArgs& a, const ExpertArgs& x, const ExpertSh
   if constexpr (AC || ELT == 2)
     if (g.v == kBig) return launch_tiles<OP, ELT, stage_bytes(AC, BC, ELT, 256), 2, 2, 4, 4>(a, x, 1, part, s);
   if (g.v == kMid) return launch_tiles<OP, ELT, stage_bytes(AC, BC, ELT, 128), 2, 2, 2, 2>(a, x, g.splits, part, s);
-  if constexpr (AC) {
+  if constexpr (AC || ELT == 4)
     if (g.v == kSlim) return launch_tiles<OP, ELT, 64, 2, 2, 1, 2>(a, x, g.splits, part, s);
-    return launch_tiles<OP, ELT, 64, 1, 4, 1, 1>(a, x, g.splits, part, s);
-  }
+  if constexpr (AC) return launch_tiles<OP, ELT, 64, 1, 4, 1, 1>(a, x, g.splits, part, s);
   return hipErrorInvalidValue;
 }
 

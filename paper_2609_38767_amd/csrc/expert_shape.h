@@ -35,7 +35,9 @@ constexpr bool expert_splits(Variant v, int elt) { return v != kBig && !(v == kS
 // experts of 4096 -> 1024, 32768 rows 371/449/566/876.  float32, five experts of
 // 769 -> 1030, 1531 rows: 284/75/50/50; one of 3232 -> 392, 28 rows, without a
 // split: 64 in 32 x 128.
-// float32 weight gradients take 128 x 128 always: larger tiles reach 3% more at most.
+// float32 weight gradients leave out 256 x 256 (3% more at most) and take 64 x 128
+// too: five experts of 769 -> 1030, 1531 rows, 50 us, in 128 x 128 64; bf16 ones
+// would gain little there (24 and 27) and lose elsewhere.
 inline ExpertShape expert_shape(bool weight_grad, int64_t rows, int64_t experts, int64_t m, int64_t n, int64_t k,
                                 int elt, bool bc) {
   const double rate[4] = {elt == 2 ? 5.2e6 : 0.58e6, elt == 2 ? 3.4e6 : 0.565e6, elt == 2 ? 2.4e6 : 0.5e6,
@@ -47,7 +49,7 @@ inline ExpertShape expert_shape(bool weight_grad, int64_t rows, int64_t experts,
                                    : (double)elt * (met * n * k + rows * (n + k));
   ExpertShape best = {};
   double best_us = 0.;
-  for (int v = weight_grad && elt == 4 ? kMid : kBig; v <= (weight_grad ? kMid : kFew); ++v) {
+  for (int v = weight_grad && elt == 4 ? kMid : kBig; v <= (!weight_grad ? kFew : elt == 4 ? kSlim : kMid); ++v) {
     const int64_t tm = v == kBig ? 256 : v == kMid ? 128 : v == kSlim ? 64 : 32, tn = v == kBig ? 256 : 128;
     const int kw = stage_bytes(!weight_grad, bc, elt, (int)tm);
     const double nn = (double)((n + tn - 1) / tn);
@@ -59,7 +61,7 @@ inline ExpertShape expert_shape(bool weight_grad, int64_t rows, int64_t experts,
       if (splits > 1 && depth * elt / splits < 512.) break;
       const double tiles = nm * nn * splits / 256.;
       // weight gradients: an expert of many rows makes long tiles, which many short ones even out
-      const double rounds = weight_grad ? std::max(1., tiles + (v == kBig ? 1. : 0.5))
+      const double rounds = weight_grad ? std::max(1., tiles + (v == kBig || (v == kMid && elt == 4) ? 1. : 0.5))
                             : v <= kMid ? std::max(1., std::ceil(tiles)) : std::max(1., tiles + 0.5);
       const double work = rounds * (2. * tm * tn * depth / splits / rate[v] + fixed[v]), read = bytes / 5.e6;
       double us = std::max(work, read) + 0.3 * std::min(work, read);

@@ -81,14 +81,15 @@ def test_expert_sizes_take_the_cut_they_stand_for(ask):
     assert [(TILES[v], splits > 1) for v, splits, _ in got] == [c[6:] for c in CUTSX]
     ways = {(op, t, tile, s) for op in (0, 1) for t in ("f32", "bf16") for tile in TILES for s in (False, True)
             if not (s and (tile == "256x256" or (tile == "64x128" and t == "f32")))}
-    ways |= {(2, t, "128x128", s) for t in ("f32", "bf16") for s in (False, True)} | {(2, "bf16", "256x256", False)}
+    ways |= {(2, t, "128x128", s) for t in ("f32", "bf16") for s in (False, True)} | {(2, "bf16", "256x256", False), (2, "f32", "64x128", False)}
     assert {(c[0], c[1], c[6], c[7]) for c in CUTSX} == ways
 
 
 def test_no_other_expert_cut_is_reached(ask):
-    """256 x 256 is never split, nor float32 in 64 x 128; float32 weight gradients take 128 x 128, whatever the size."""
+    """256 x 256 is never split, nor float32 in 64 x 128; weight gradients take their own, whatever the size."""
     sizes = [(n, e, i, o) for n in (1, 50, 3000, 100000) for e in (1, 9, 300) for i in (8, 700, 16384) for o in (40, 5000)]
     for op in range(3):
         for b in (2, 4):
             for (n, e, i, o), (v, splits, _) in zip(sizes, ask([f"e {op} {b} {n} {e} {i} {o}" for n, e, i, o in sizes])):
-                assert 1 <= splits <= 32 and (splits == 1 or v == 1 or v == 3 or (v == 2 and b == 2)) and (op < 2 or v == 1 or (v == 0 and b == 2))
+                assert 1 <= splits <= 32 and (splits == 1 or v == 1 or v == 3 or (v == 2 and b == 2))
+                assert op < 2 or v == 1 or v == (0 if b == 2 else 2)
