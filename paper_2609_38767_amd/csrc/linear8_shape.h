@@ -36,22 +36,26 @@ inline Shape8 shape8(int64_t M, int64_t N, int64_t K, int elt) {
     return g;
   };
   if (M <= 16) return cut(kFew, 1);
-  if (M <= 64) return cut(kSlim, std::min<int64_t>(64, 768 / ((N + 127) / 128)));
+  // One workgroup per CU, whose ring keeps 75 KB of loads under way: 64 x 4096 -> 14336 17.3 us in two splits, 17.8
+  // whole, 22.5 in six; 64 x 14336 -> 4096 17.8 in eight, 46.2 whole.
+  if (M <= 64) return cut(kSlim, std::min<int64_t>(64, 256 / ((N + 127) / 128)));
   // The cut with the least modelled time, as for the other products (gemm_shape):
   // FLOP per us of a CU, us besides, and what a lone workgroup of 128 x 128 reaches
-  // of the rate where two share a CU otherwise (float32 results).
-  const double rate[2] = {8.8e6, elt == 2 ? 6.2e6 : 4.3e6}, fixed[2] = {12., 4.}, lone = elt == 2 ? 1. : 0.85;
+  // of the rate where two share a CU otherwise (float32 results).  1000 x 1000 ->
+  // 1000: 64 x 128 12.3 us, 128 x 128 14.1; 1536 x 4096 -> 2304: 35.6 and 24.7.
+  const double rate[3] = {8.8e6, elt == 2 ? 6.2e6 : 4.3e6, elt == 2 ? 4.8e6 : 3.e6}, fixed[3] = {12., 4., 3.5},
+               lone = elt == 2 ? 1. : 0.85;
   Shape8 best = {};
   double best_us = 0.;
-  for (int v = elt == 2 ? kBig : kMid; v <= kMid; ++v)
+  for (int v = elt == 2 ? kBig : kMid; v <= kSlim; ++v)
     for (int64_t splits = 1; splits <= 32; ++splits) {
       const Shape8 g = cut((Variant)v, splits);
       if (g.splits != splits) continue;
       const double each = (double)g.nm * g.nn, last = splits > 1 ? (double)stages / g.sps - (splits - 1) : 1.;
       const bool alone = each * splits <= 256.;
       const double rounds = alone ? 1. : std::max(1. + last, std::ceil(each * (splits - 1 + last) / 256.));
-      const int64_t side = v == kBig ? 256 : 128;
-      double us = rounds * (2. * side * side * g.sps * 128 / (rate[v] * (alone && v == kMid ? lone : 1.)) + fixed[v]);
+      const double area = v == kBig ? 65536. : v == kMid ? 16384. : 8192.;
+      double us = rounds * (2. * area * g.sps * 128 / (rate[v] * (alone && v == kMid ? lone : 1.)) + fixed[v]);
       if (g.splits > 1) us += 3. + 8. * g.splits * M * N / 6.0e6;
       if (best_us == 0. || us < best_us) {
         best = g;
