@@ -890,7 +890,8 @@ dattri_status dattri_linear_weight_grad(const void* G, int64_t ld_g, const void*
  *   Q: NULL or device [rows of d] bytes, S: NULL or device float32 [rows of
  *   ceil(d / 128)], rows ld_s apart; Y or Q has to be given, both may be.
  *   Y and H may each be X or R itself (same stride).
- *   eps: finite, >= 0 (0: rows of zeros give NaN)
+ *   eps: finite, >= 0 (0: rows of zeros give NaN).  Sums of squares are those of
+ *   float32: rows whose squares add up past its range may give zeros.
  * Errors: INVALID_ARG, DTYPE, UNSUPPORTED, HIP. */
 dattri_status dattri_rms_norm(const void* X, int64_t ld_x, const void* R, int64_t ld_r, const void* W,
                               float eps, void* Y, int64_t ld_y, void* H, int64_t ld_h, void* Q,

@@ -211,3 +211,19 @@ def test_large_sets(dtype):
         assert torch.equal(m.rms_norm_grad(r[at], x[at], w, residual=r[at], weight_grad=False), g[at])
     want, _, _ = ob.rms_norm(host(x[-3:]), host(w), host(r[-3:]))
     check(y[-3:], want, (DEEP + OUT[dtype] * (1 + DEEP)) * np.abs(want))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size", [(1, 8), (2, 64), (5, 64), (7, 128), (6, 256), (3, 72)], ids=lambda s: "x".join(map(str, s)))
+def test_gradients_without_eps(size, dtype):
+    """Rows that share a wave with places behind the last row, whose norm would be 0 / 0."""
+    n, d = size
+    gn = gen(300 + n)
+    g, h, w = rand(gn, n, d, dtype=dtype), rand(gn, n, d, dtype=dtype, std=2.0), rand(gn, d, dtype=dtype)
+    got, dw = layers().rms_norm_grad(g, h, w, eps=0.0)
+    want, ww = ob.rms_norm_grad(host(g), host(h), host(w), None, 0.0)
+    u = 1 / np.sqrt((host(h) ** 2).mean(1, keepdims=True))
+    a = np.abs(host(g) * host(w))
+    e = 400 * U * u * (a + np.abs(host(h)) * u ** 2 * (a * np.abs(host(h))).mean(1, keepdims=True))
+    check(got, want, e + OUT[dtype] * (np.abs(want) + e), "gradient")
+    check(dw, ww, 100 * U * (np.abs(host(g) * host(h)) * u).sum(0), "weight gradient")
