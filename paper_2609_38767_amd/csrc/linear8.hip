@@ -25,7 +25,7 @@
 // (259 us) copies for timing without its loads took 221, without the scales' fma
 // 240, without barriers and waits 251: it is the power, not one unit, that ends it.
 // Float32 results 1723 us (1.12 PFLOP/s).  One row of 4096 -> 14336: 14.3 us, 4.1
-// TB/s of weights; 16 rows 23; 64 rows, by tiles, 17.3.
+// TB/s of weights; 16 rows, by tiles, 16.7; 64 rows 17.3.
 #include <algorithm>
 #include <type_traits>
 
@@ -97,11 +97,13 @@ __device__ DATTRI_INLINE inline f32x16 half_sum(const i32x8& w, const i32x8& x, 
 
 }  // namespace
 
-// W waves of a workgroup share 16 weight rows and all rows of X, 16 at most: wave
-// w takes the groups of k w, w + W, ...; the waves' sums are added in their order.
-template <int ELT, int W>
-__global__ __launch_bounds__(W * 64) void linear8_few_kernel(GemmArgs a, Scales8 sc) {
-  constexpr int kAhead = 4;  // groups in flight per wave
+// Eight waves of a workgroup share 16 weight rows and all rows of X, 16 at most:
+// wave w takes the groups of k w, w + 8, ...; the waves' sums are added in their
+// order.  (One row of 4096 -> 14336: 13.4 us, with four waves 14.4, with sixteen
+// 18.4; 4096 -> 4096, whose workgroups are one per CU, 5.0, with sixteen 5.5.)
+template <int ELT>
+__global__ __launch_bounds__(512) void linear8_few_kernel(GemmArgs a, Scales8 sc) {
+  constexpr int W = 8, kAhead = 4;  // groups in flight per wave
   __shared__ f32x4 red[W][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15,
             c = lane >> 4;
@@ -374,16 +376,9 @@ hipError_t launch_tiles(const GemmArgs& a, const Scales8& sc, const Shape8& g, f
   return hipGetLastError();
 }
 
-// Waves per workgroup: eight (one row of 4096 -> 14336: 14.7 us, with four 16.6),
-// sixteen where there are too few workgroups to fill the CUs with those.
 template <int ELT>
 hipError_t launch_few(const GemmArgs& a, const Scales8& sc, hipStream_t s) {
-  const int64_t strips = ((int64_t)a.N + 15) / 16;
-  const dim3 grid((unsigned)strips);
-  if (strips >= 512 || a.K <= 8 * kGroup8)
-    hipLaunchKernelGGL((linear8_few_kernel<ELT, 8>), grid, dim3(512), 0, s, a, sc);
-  else
-    hipLaunchKernelGGL((linear8_few_kernel<ELT, 16>), grid, dim3(1024), 0, s, a, sc);
+  hipLaunchKernelGGL(linear8_few_kernel<ELT>, dim3((unsigned)(((int64_t)a.N + 15) / 16)), dim3(512), 0, s, a, sc);
   return hipGetLastError();
 }
 

@@ -35,7 +35,10 @@ inline Shape8 shape8(int64_t M, int64_t N, int64_t K, int elt) {
     g.splits = (int)((stages + g.sps - 1) / g.sps);
     return g;
   };
-  if (M <= 16) return cut(kFew, 1);
+  // Without tiles every 16 weight rows read all rows of X again.  us without and with tiles, weights out of the caches:
+  // 4096 -> 14336 one row 14.6/16.5, four 16.3/16.6, eight 17.9/16.4, sixteen 22.5/16.7; 14336 -> 4096 eight 18.1/16.9
+  // (float32 18.3/18.0); 8192 -> 4096, 34M weights, eight 11.0/13.3, sixteen 13.3/13.7.
+  if (M < 8 || (M <= 16 && N * K < 40000000)) return cut(kFew, 1);
   // One workgroup per CU, whose ring keeps 75 KB of loads under way: 64 x 4096 -> 14336 17.3 us in two splits, 17.8
   // whole, 22.5 in six; 64 x 14336 -> 4096 17.8 in eight, 46.2 whole.
   if (M <= 64) return cut(kSlim, std::min<int64_t>(64, 256 / ((N + 127) / 128)));
