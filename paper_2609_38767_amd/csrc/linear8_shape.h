@@ -40,8 +40,14 @@ inline Shape8 shape8(int64_t M, int64_t N, int64_t K, int elt) {
   // (float32 18.3/18.0); 8192 -> 4096, 34M weights, eight 11.0/13.3, sixteen 13.3/13.7.
   if (M < 8 || (M <= 16 && N * K < 40000000)) return cut(kFew, 1);
   // One workgroup per CU, whose ring keeps 75 KB of loads under way: 64 x 4096 -> 14336 17.3 us in two splits, 17.8
-  // whole, 22.5 in six; 64 x 14336 -> 4096 17.8 in eight, 46.2 whole.
-  if (M <= 64) return cut(kSlim, std::min<int64_t>(64, 256 / ((N + 127) / 128)));
+  // whole, 22.5 in six; 64 x 14336 -> 4096 17.8 in eight, 46.2 whole.  With half the CUs at work splits of eight groups
+  // of k or more do (weights out of the caches: 64 x 4096 -> 4096 14.0 us in four, 15.1 in eight; 64 x 8192 -> 2048 14.3
+  // in eight, 15.3 in sixteen; but 64 x 4096 -> 1024 12.0 in four, 10.9 in eight), and eight groups stay whole (64 x
+  // 1024 -> 4096 8.5, in two 9.7).
+  if (M <= 64) {
+    const int64_t strips = (N + 127) / 128;
+    return cut(kSlim, stages <= 8 ? 1 : std::min<int64_t>({64, 256 / strips, std::max<int64_t>(128 / strips, stages / 8)}));
+  }
   // The cut with the least modelled time, as for the other products (gemm_shape):
   // FLOP per us of a CU, us besides, and what a lone workgroup of 128 x 128 reaches
   // of the rate where two share a CU otherwise (float32 results).  1000 x 1000 ->
