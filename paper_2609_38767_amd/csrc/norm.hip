@@ -12,8 +12,8 @@
 //
 // What bounds it: memory.  16384 rows of 4096 bf16: sum, norm and 8 bits 72 us
 // (471 MB, 6.5 TB/s), gradients 87 + 5 (537 MB, 6.2); 65536 rows of 128 12.1 us
-// (67 MB); 8192 rows of 4099, most of them off 16 bytes, 62 us (4.3 TB/s), the
-// gradients 74.  One row of 4096 2.1 us: the launch.  Rows that no registers hold
+// (67 MB); 8192 rows of 4099, most of them off 16 bytes, 54 us (5.0 TB/s), the
+// gradients 67.  One row of 4096 2.1 us: the launch.  Rows that no registers hold
 // are read twice: 4096 of 40000 float32 834 us, 3.9 TB/s of what it then moves.
 #include <algorithm>
 #include <type_traits>
@@ -76,15 +76,16 @@ __device__ inline float lanes_sum(float v) {
 template <int ELT, bool VEC, int T>
 struct RowOf {
   static constexpr int N = VEC ? 16 / ELT : 2;  // elements of a piece
-  static constexpr int kRows = T < 256 ? 256 / T : 1, kPerWave = T < 64 ? 64 / T : 1;  // rows of a workgroup, of a wave
-  static constexpr int kThreads = T > 256 ? T : 256;
+  // rows of a workgroup (one as soon as its waves have to meet), of a wave
+  static constexpr int kRows = T <= 64 ? 256 / T : 1, kPerWave = T < 64 ? 64 / T : 1;
+  static constexpr int kThreads = T <= 64 ? 256 : T;
   static_assert(T >= (VEC ? kGroup8 / N : 64), "a group of 8-bit values in one row's lanes");
   typedef std::conditional_t<VEC, i32x4, i32x2> Raw;
   int t, sub, d;  // place in the row, row of the wave
   __device__ explicit RowOf(int d_) : t(threadIdx.x % T), sub(T < 64 ? (threadIdx.x & 63) / T : 0), d(d_) {}
   // The wave's first row of the workgroup's rows from r0.
   __device__ static int64_t first(int64_t r0) {
-    return r0 + (T < 256 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 64 / T : 0);
+    return r0 + (T <= 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 64 / T : 0);
   }
   // Column of element e of piece c.  VEC: N neighbours per lane; else 64 apart, lanes neighbours.
   __device__ int col(int c, int e) const {
@@ -208,13 +209,13 @@ __device__ inline void row_sums(float (&v)[S], float* red, int turn) {
 }  // namespace
 
 template <int ELT, bool VEC, bool ONCE, int T, int C>
-__global__ __launch_bounds__(T > 256 ? T : 256) void rms_norm_kernel(NormArgs a) {
+__global__ __launch_bounds__(T <= 64 ? 256 : T) void rms_norm_kernel(NormArgs a) {
   typedef RowOf<ELT, VEC, T> Row;
   constexpr int N = Row::N;
   __shared__ float red[T > 64 ? T / 64 : 1];
   const Row p(a.d);
   const int64_t row0 = Row::first(row_block() * Row::kRows), row = row0 + p.sub;
-  if (row0 >= a.rows) return;  // T < 256: whole waves, which meet no barrier
+  if (row0 >= a.rows) return;  // T up to 64: whole waves, which meet no barrier
   const bool here = row < a.rows;
   const auto x = p.buffer(a.X, row0, a.ldx, a.rows), r = p.buffer(a.R, row0, a.ldr, a.rows);
   const typename Row::Buffer w1 = {p.buffer(a.W, 0, 0, 1).r, 0};
@@ -287,8 +288,7 @@ __global__ __launch_bounds__(256) void rms_norm_long_kernel(NormArgs a) {
 // The workgroups walk the rows; each keeps its columns' share of dW and leaves it
 // as one row of part (null: dW is not wanted).
 template <int ELT, bool VEC, bool ONCE, int T, int C>
-__global__ __launch_bounds__(T > 256 ? T : 256) void norm_grad_kernel(NormGradArgs a,
-                                                                                float* __restrict__ part) {
+__global__ __launch_bounds__(T <= 64 ? 256 : T) void norm_grad_kernel(NormGradArgs a, float* __restrict__ part) {
   typedef RowOf<ELT, VEC, T> Row;
   constexpr int N = Row::N, kRows = Row::kRows;
   constexpr bool kAhead = C <= 2;  // the next row is on its way while this one is worked on
@@ -369,7 +369,7 @@ __global__ __launch_bounds__(T > 256 ? T : 256) void norm_grad_kernel(NormGradAr
   }
   if (!part) return;
   float* out = part + (int64_t)blockIdx.x * a.d;
-  const int sub = T < 256 ? threadIdx.x / T : 0;
+  const int sub = T <= 64 ? threadIdx.x / T : 0;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     if constexpr (kRows > 1) {  // the rows' shares in order
@@ -518,11 +518,21 @@ int64_t pieces_of(int elt, bool vec, int64_t d) { return vec ? d / (16 / elt) : 
 // group of 8-bit values.  Four waves per row as soon as each has a piece for
 // every lane: 16384 rows of 4096 bf16, norm to 8 bits 71 us, with one wave 74;
 // gradient 83 and 116, whose sums of dW a wave has fewer of.
-//   MOST: pieces of the longest rows that are asked for
-template <int ELT, bool VEC, int MOST, class F>
-bool with_shape(int64_t n, F f) {
-#define SHAPE(T, C)                 \
-  if constexpr ((T) * (C) <= MOST)  \
+// Rows off 16 bytes, whose pieces are two elements: eight pieces per thread, for
+// fewer sums across waves and more loads under way, where there are rows enough.
+// us of the norm, with two pieces per thread in brackets: 40000 rows of 1001 bf16
+// 33 (52), gradient 47 (102); 8192 of 3001 26 (48) and 39 (66); 8192 of 4099
+// float32 53 (72), but its gradient 92 (85).  Few rows: 1024 of 769 float32 to 8
+// bits 5.5 (4.3), gradient 8.0 (8.4); 300 of 1023 5.0 (3.4) and 7.1 (6.6).  Of 1025
+// to 2048 columns a wave takes sixteen pieces for the gradient, whose workgroups
+// (kGradGroups) of 128 threads would leave half the CUs' places empty: 20000 rows
+// of 1501 bf16 43, with 128 threads 70.
+constexpr int kGradMost = 16384;  // columns of the longest row of a gradient that they hold
+template <int ELT, bool VEC, bool GRAD, class F>
+bool with_shape(int64_t n, int64_t rows, F f) {
+  constexpr int kMost = GRAD && VEC ? kGradMost * ELT / 16 : 8192;
+#define SHAPE(T, C)                  \
+  if constexpr ((T) * (C) <= kMost)  \
     if (n <= (T) * (C)) return f(std::integral_constant<int, T>{}, std::integral_constant<int, C>{}), true
   if constexpr (VEC) {
     SHAPE(8 * ELT, 1);
@@ -530,7 +540,14 @@ bool with_shape(int64_t n, F f) {
   }
   SHAPE(64, 1);
   SHAPE(64, 2);
-  if (n < 256) SHAPE(64, 4);
+  if (!VEC || n < 256) SHAPE(64, 4);
+  if constexpr (!VEC)
+    if (rows >= (GRAD ? 400 : 2048)) {
+      SHAPE(64, 8);
+      SHAPE(GRAD ? 64 : 128, GRAD ? 16 : 8);
+      SHAPE(256, 8);
+      if constexpr (!GRAD || ELT == 2) SHAPE(512, 8);
+    }
   SHAPE(256, 2);
   SHAPE(512, 2);
   SHAPE(1024, 2);
@@ -548,7 +565,7 @@ template <int ELT, bool VEC, bool ONCE>
 hipError_t launch_norm_as(const NormArgs& a, hipStream_t s) {
   hipError_t e = hipSuccess;
   const int64_t n = pieces_of(ELT, VEC, a.d);
-  const bool held = with_shape<ELT, VEC, 8192>(n, [&](auto T, auto C) {
+  const bool held = with_shape<ELT, VEC, false>(n, a.rows, [&](auto T, auto C) {
     typedef RowOf<ELT, VEC, decltype(T)::value> Row;
     dim3 grid;
     if ((e = row_grid((a.rows + Row::kRows - 1) / Row::kRows, &grid, Row::kThreads)) != hipSuccess) return;
@@ -581,7 +598,6 @@ namespace {
 // rows of 4096 bf16: 83 us, with one 87, three 89, four 97).  Whether they do
 // does not go by the buffers' alignment here, so a layout fits any.
 constexpr int kGradGroups = 512;
-constexpr int kGradMost = 16384;  // columns of the longest row that they hold
 bool grad_held(int64_t d) { return d <= kGradMost; }
 
 // Rows per part of a long row's weight gradient, and parts: eight workgroups per CU of 64 rows or more.
@@ -619,7 +635,7 @@ template <int ELT, bool VEC, bool ONCE>
 hipError_t launch_grad_as(const NormGradArgs& a, float* dw, bool accumulate, uint8_t* ws, hipStream_t s) {
   hipError_t e = hipSuccess;
   int64_t groups = 0;
-  with_shape<ELT, VEC, VEC ? kGradMost * ELT / 16 : 8192>(pieces_of(ELT, VEC, a.d), [&](auto T, auto C) {
+  with_shape<ELT, VEC, true>(pieces_of(ELT, VEC, a.d), a.rows, [&](auto T, auto C) {
     typedef RowOf<ELT, VEC, decltype(T)::value> Row;
     groups = std::min<int64_t>(kGradGroups, (a.rows + Row::kRows - 1) / Row::kRows);
     if (groups == 0) return;

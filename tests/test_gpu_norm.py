@@ -227,3 +227,30 @@ def test_gradients_without_eps(size, dtype):
     e = 400 * U * u * (a + np.abs(host(h)) * u ** 2 * (a * np.abs(host(h))).mean(1, keepdims=True))
     check(got, want, e + OUT[dtype] * (np.abs(want) + e), "gradient")
     check(dw, ww, 100 * U * (np.abs(host(g) * host(h)) * u).sum(0), "weight gradient")
+
+
+# rows off 16 bytes, many enough for the forms with eight pieces per thread: 64, 128, 256 and 512 threads a row
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,d", [(2051, 513), (2049, 769), (2050, 1501), (2048, 2049), (2053, 3001), (2049, 4099),
+                                 (2050, 8191), (401, 1023), (400, 2047), (409, 6001)])
+def test_many_rows_off_16_bytes(n, d, dtype):
+    m, gn = layers(), gen(n + d)
+    x, r, w = rand(gn, n, d, dtype=dtype, std=3.0), rand(gn, n, d, dtype=dtype), rand(gn, d, dtype=dtype)
+    y, h, _ = ob.rms_norm(host(x), host(w), host(r), 1e-5)
+    by, bh = (DEEP + OUT[dtype] * (1 + DEEP)) * np.abs(y), (U + OUT[dtype] * (1 + U)) * np.abs(h)
+    eight, gy, gh = m.rms_norm_8bit(x, w, residual=r, eps=1e-5, keep=True)
+    check(gy, y, by, "y")
+    check(gh, h, bh, "h")
+    check8(*eight, y)
+    out = x.clone()
+    both = m.rms_norm(out, w, residual=r, eps=1e-5, out=out)
+    assert both[0] is out and torch.equal(out, gy) and torch.equal(both[1], gh)
+    got, dw = m.rms_norm_grad(r, x, w, eps=1e-5, residual=gy)
+    want, ww = ob.rms_norm_grad(host(r), host(x), host(w), host(gy), 1e-5)
+    u = 1 / np.sqrt((host(x) ** 2).mean(1, keepdims=True) + 1e-5)
+    a = np.abs(host(r) * host(w))
+    e = 400 * U * u * (a + np.abs(host(x)) * u ** 2 * (a * np.abs(host(x))).mean(1, keepdims=True))
+    e = e + 4 * U * (np.abs(host(gy)) + np.abs(want))
+    check(got, want, e + OUT[dtype] * (np.abs(want) + e), "d")
+    # a workgroup adds up n / 512 rows in turn, the joins 16 and 5 more; each term has u and two products
+    check(dw, ww, (2 * (n // 512 + 40) * U + 90 * U) * np.abs(host(r) * host(x) * u).sum(0), "dw")
