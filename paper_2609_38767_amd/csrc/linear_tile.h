@@ -468,40 +468,41 @@ struct Repack {
 };
 template <int ELT>
 __global__ __launch_bounds__(256) void repack_kernel(Repack a, Repack b) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t at = row_block() * 4 + wave;  // a wave per row
+  constexpr int U = ELT == 1 ? 2 : 4;  // pieces per lane under way
+  const int lane = threadIdx.x & 63;
+  const int64_t at = row_block() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // a wave per row
   if (at >= a.rows + b.rows) return;
-  const Repack& p = at < a.rows ? a : b;
+  const Repack p = at < a.rows ? a : b;
   const int64_t r = at < a.rows ? at : at - a.rows;
-  const uint8_t* src = p.src + r * p.ld * ELT;
-  uint8_t* dst = p.dst + r * p.ld_out * ELT;
-  if constexpr (ELT == 1) {
-    // 16 bytes per lane from the aligned words that hold them, shifted into place; a word is read only if some of its
-    // bytes are the row's
-    const int shift = (int)((uintptr_t)src & 3);
-    const uint32_t* words = (const uint32_t*)(src - shift);
-    const int n_words = (p.w + shift + 3) / 4;
-    for (int c = lane * 4; c * 4 < p.ld_out; c += 256) {
-      uint32_t v[5];
+  const uint8_t* const src = p.src + r * p.ld * ELT;
+  uint8_t* const dst = p.dst + r * p.ld_out * ELT;
+  const int width = p.w * ELT, out = p.ld_out * ELT;
+  // 16 bytes per lane from the aligned words that hold them, shifted into place; a word is read only if some of its
+  // bytes are the row's, and those behind the row become zeros
+  const int shift = (int)((uintptr_t)src & 3);
+  const rsrc_t words = make_rsrc(src - shift, (uint32_t)(width + shift + 3) / 4 * 4);
+  for (int c0 = lane * 16; c0 < out; c0 += 1024 * U) {
+    uint32_t v[U][5];
 #pragma unroll
-      for (int e = 0; e < 5; ++e) v[e] = c + e < n_words ? words[c + e] : 0u;
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < (ELT == 4 ? 4 : 5); ++e) v[u][e] = load4(words, c0 + 1024 * u + 4 * e);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int c = c0 + 1024 * u;
       i32x4 o;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const uint32_t x = __builtin_amdgcn_alignbyte(v[e + 1], v[e], shift);
-        const int left = p.w - (c + e) * 4;  // bytes of the row in this word
-        o[e] = (int)(left >= 4 ? x : left > 0 ? x & ((1u << 8 * left) - 1u) : 0u);
+        if constexpr (ELT == 4) {
+          o[e] = (int)v[u][e];
+        } else {
+          const uint32_t x = __builtin_amdgcn_alignbyte(v[u][e + 1], v[u][e], shift);
+          const int left = width - (c + 4 * e);  // bytes of the row in this word
+          o[e] = (int)(left >= 4 ? x : left > 0 ? x & ((1u << 8 * left) - 1u) : 0u);
+        }
       }
-      *(i32x4*)(dst + c * 4) = o;
+      if (c < out) *(i32x4*)(dst + c) = o;
     }
-    return;
-  }
-#pragma unroll 8
-  for (int c = lane; c < p.ld_out; c += 64) {
-    if constexpr (ELT == 2)
-      ((uint16_t*)dst)[c] = c < p.w ? ((const uint16_t*)src)[c] : (uint16_t)0;
-    else
-      ((uint32_t*)dst)[c] = c < p.w ? ((const uint32_t*)src)[c] : 0u;
   }
 }
 
