@@ -74,8 +74,8 @@ inline ExpertShape expert_shape(bool weight_grad, int64_t rows, int64_t experts,
     }
   }
   // Few rows whose tiles leave half the CUs without work read the weights slowly: 16 rows, 64 experts of 4096 -> 1024,
-  // 14 of them met, 47 us, in two splits 36; one row, eight of 4096 -> 14336, 42 and 35, one row's gradient of 14336 -> 4096 37
-  // and 27.
+  // 14 of them met, 47 us, in two splits 36; one row, eight of 4096 -> 14336, 42 and 35, the gradient of one row, eight
+  // of 14336 -> 4096, 37 and 27.
   if (!weight_grad && best.v == kFew && best.splits == 1 && k * elt >= 8192 &&
       std::max((double)met, (double)rows / 32 + 0.5 * met) * ((n + 127) / 128) <= 128.)
     best.splits = 2;
