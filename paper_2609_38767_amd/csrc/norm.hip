@@ -42,8 +42,9 @@ __device__ inline double block_sum(double v) {
 
 // q and s of a wave's group: lane holds columns lane and lane + 64 of it.
 __device__ inline void store_group8(uint8_t* q, float* s, int lane, int left, float v0, float v1) {
-  const float sc = scale8(wave_max(max_mag(max_mag(0.f, v0), v1))), r = 1.f / sc;
-  const int w = pack8<false>(over_scale(v0, sc, r), over_scale(v1, sc, r), 0);
+  const float sc = scale8(wave_max(max_mag(max_mag(0.f, v0), v1)));
+  const Quotient8 by(sc);
+  const int w = pack8<false>(by.of(v0), by.of(v1), 0);
   if (lane < left) q[lane] = (uint8_t)w;
   if (lane + 64 < left) q[lane + 64] = (uint8_t)(w >> 8);
   if (lane == 0) *s = sc;
@@ -163,17 +164,18 @@ struct RowOf {
     top = over16(top, [](float a, float b) { return fmaxf(a, b); });
     if constexpr (N < 8) top = fmaxf(top, __shfl_xor(top, 16));
     if constexpr (N < 4) top = fmaxf(top, __shfl_xor(top, 32));
-    const float sc = scale8(top), r = 1.f / sc;
+    const float sc = scale8(top);
+    const Quotient8 by(sc);
     if constexpr (!VEC) {
-      const int w = pack8<false>(over_scale(v[0], sc, r), over_scale(v[1], sc, r), 0);
+      const int w = pack8<false>(by.of(v[0]), by.of(v[1]), 0);
       __builtin_amdgcn_raw_buffer_store_b8((char)w, q.r, at(q, c, 0, 1), 0, 0);
       __builtin_amdgcn_raw_buffer_store_b8((char)(w >> 8), q.r, at(q, c, 1, 1), 0, 0);
     } else {
       int w[N / 4];
 #pragma unroll
       for (int e = 0; e < N / 4; ++e)
-        w[e] = pack8<true>(over_scale(v[4 * e + 2], sc, r), over_scale(v[4 * e + 3], sc, r),
-                           pack8<false>(over_scale(v[4 * e], sc, r), over_scale(v[4 * e + 1], sc, r), 0));
+        w[e] = pack8<true>(by.of(v[4 * e + 2]), by.of(v[4 * e + 3]),
+                           pack8<false>(by.of(v[4 * e]), by.of(v[4 * e + 1]), 0));
       if constexpr (N == 8)
         __builtin_amdgcn_raw_buffer_store_b64(i32x2{w[0], w[1]}, q.r, at(q, c, 0, 1), 0, 0);
       else
@@ -495,12 +497,13 @@ __global__ __launch_bounds__(256) void quantize_weight_kernel(const void* __rest
   top = wave_max(top);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = top;
   __syncthreads();
-  const float s = scale8(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]))), inv = 1.f / s;
+  const float s = scale8(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
+  const Quotient8 by(s);
   if (threadIdx.x == 0) S[bo * lds + bi] = s;
   if (c < d)
 #pragma unroll 8
     for (int r = threadIdx.x >> 7; r < n; r += 2)
-      Q[(r0 + r) * ldq + c] = (uint8_t)pack8<false>(over_scale(load_elt<ELT>(W, (r0 + r) * ldw + c), s, inv), 0.f, 0);
+      Q[(r0 + r) * ldq + c] = (uint8_t)pack8<false>(by.of(load_elt<ELT>(W, (r0 + r) * ldw + c)), 0.f, 0);
 }
 
 namespace {

@@ -1,0 +1,61 @@
+"""Norms, 8-bit rows and products and experts' products at the ends of what their
+entry points take: the smallest scales, the most rows, experts that nothing meets,
+operands and outputs off their usual alignment."""
+import numpy as np
+import pytest
+import torch
+
+from model_util import DT, gen, host, rand
+from oracle import block as ob
+
+pytestmark = pytest.mark.gpu
+DTYPES = ["f32", "bf16"]
+
+
+def layers():
+    from paper_2609_38767_amd import layers as m
+    return m
+
+
+# ------------------------------------------------------ 8-bit values under small scales
+def halves(m, e):
+    """A group whose scale is m 2^e, as near as its largest value says: 448 scales, every value halfway between two e4m3
+    values, as near as float32 comes, and zero."""
+    values = sorted({(8 + k) * 2.0 ** (x - 3) for x in range(-6, 9) for k in range(8) if (8 + k) * 2.0 ** (x - 3) <= 448}
+                    | {k * 2.0 ** -9 for k in range(8)})
+    ties = [(a + b) / 2 for a, b in zip(values, values[1:])]
+    assert len(ties) == 126
+    signs = np.where(np.arange(126) % 3 == 0, -1.0, 1.0)
+    return np.concatenate([[448.0], np.array(ties) * signs, [0.0]]) * m * 2.0 ** e
+
+
+def groups(dtype):
+    rng = np.random.default_rng(2)
+    m = [1.0, 1.25, 1.5, 1.75] + ([] if dtype == "bf16" else list(1 + rng.integers(0, 1 << 23, 4) * 2.0 ** -23))
+    return np.stack([halves(v, e) for e in range(-128, -56) for v in m]).astype(np.float32)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_values_under_small_scales(dtype):
+    """The very values of the definition down to the smallest scale, at quotients that a wrong last bit moves."""
+    m = layers()
+    x = torch.from_numpy(groups(dtype)).to(DT[dtype]).cuda()
+    q, s = m.quantize_rows(x)
+    wq, ws = ob.quantize(host(x))
+    assert np.array_equal(host(s), ws) and np.array_equal(host(q), wq)
+    w = x[::16].repeat_interleave(128, 0)  # blocks of one scale
+    q, s = m.quantize_weight(w)
+    wq, ws = ob.quantize(host(w), 128)
+    assert np.array_equal(host(s), ws) and np.array_equal(host(q), wq)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,d", [(3, 128), (2, 4096), (2, 4001), (2, 33024), (2, 66048), (2, 70001), (2049, 1001)])
+def test_norms_under_small_scales(n, d, dtype):
+    """Rows of ones, whose norm is the weight itself: every form that writes 8-bit rows."""
+    m = layers()
+    w = torch.from_numpy(np.resize(groups(dtype).reshape(-1)[::-1], d).copy()).to(DT[dtype]).cuda()
+    (q, s), y = m.rms_norm_8bit(torch.ones(n, d, dtype=DT[dtype], device="cuda"), w, eps=0.0, keep=True)
+    assert torch.equal(y, w.expand(n, d))
+    wq, ws = ob.quantize(host(w)[None])
+    assert np.array_equal(host(s), np.repeat(ws, n, 0)) and np.array_equal(host(q), np.repeat(wq, n, 0))
