@@ -48,10 +48,6 @@ __device__ inline Segment segment(const ExpertArgs& x, int s) {
   return Segment{begin, max(begin, s > x.experts ? x.rows : boundary(x, s))};
 }
 
-// Which tile rows of TM rows each are counted: all of every segment, or those that
-// its rows fill to more than half, or the one that they fill to half at most.
-enum Rows { kAll, kFull, kRest };
-
 // Tile row `at` of all segments' tile rows.
 struct Place {
   int segment, m0, end;
@@ -68,8 +64,7 @@ struct Segments {
   __device__ Segments(const ExpertArgs& x_, int lane_) : x(x_), lane(lane_) { first = load(lane); }
   template <Rows R>
   __device__ static int tiles(const Segment& g) {
-    const int n = g.end - g.begin;
-    return R == kAll ? (n + TM - 1) / TM : R == kFull ? (n + TM / 2 - 1) / TM : n % TM > 0 && n % TM <= TM / 2;
+    return tile_rows(R, g.end - g.begin, TM);
   }
   template <Rows R>
   __device__ int most() const {

@@ -1,4 +1,4 @@
-// How the experts' products are cut (host only, no HIP): tiles, splits of k.
+// How the experts' products are cut (no HIP; all but tile_rows host only): tiles, splits of k.
 // Nothing of the boundaries is known here: the choice goes by the mean rows of an
 // expert.
 #pragma once
@@ -17,6 +17,14 @@ struct ExpertShape {
   int kw;      // bytes of k per stage
   int splits;  // of k: an expert's rows (weight gradients), else all of it
 };
+
+// Which tile rows of tm rows each are counted of a segment of n rows: all that it
+// meets; those that it fills to more than half; the one that it fills to half at
+// most.  n goes up to the largest int32, so nothing is added to it.
+enum Rows { kAll, kFull, kRest };
+constexpr int tile_rows(Rows r, int n, int tm) {
+  return r == kAll ? n / tm + (n % tm > 0) : r == kFull ? n / tm + (n % tm > tm / 2) : n % tm > 0 && n % tm <= tm / 2;
+}
 
 // Whether tiles are split along k at all: the largest have work enough, and float32
 // ones of 64 x 128 lie too near to 32 x 128 whole.

@@ -59,3 +59,20 @@ def test_norms_under_small_scales(n, d, dtype):
     assert torch.equal(y, w.expand(n, d))
     wq, ws = ob.quantize(host(w)[None])
     assert np.array_equal(host(s), np.repeat(ws, n, 0)) and np.array_equal(host(q), np.repeat(wq, n, 0))
+
+
+# ------------------------------------------------------ experts
+def test_experts_of_the_most_rows():
+    """One expert of all rows but one, as many as a call takes: every row is written, the last one too."""
+    m, n = layers(), (1 << 31) - 1
+    off = torch.tensor([0, 1, n], device="cuda")
+    x = torch.zeros(n, 8, dtype=torch.bfloat16, device="cuda")
+    x[0], x[1], x[-40], x[-1] = 1.0, 2.0, 3.0, 4.0
+    w = torch.ones(2, 1, 8, dtype=torch.bfloat16, device="cuda")
+    w[1] = 2.0
+    y = torch.full((n, 1), 7.0, dtype=torch.bfloat16, device="cuda")
+    m.expert_linear(x, w, off, out=y)
+    assert [float(y[k]) for k in (0, 1, -40, -1)] == [8, 32, 48, 64] and int(y.count_nonzero()) == 4
+    y.fill_(7.0)
+    m.expert_linear_input_grad(x, w.view(2, 8, 1), off, out=y)
+    assert [float(y[k]) for k in (0, 1, -40, -1)] == [8, 32, 48, 64] and int(y.count_nonzero()) == 4
