@@ -186,6 +186,19 @@ __global__ __launch_bounds__(256, BM * BN >= 16 ? 1 : 2) void expert_weight_kern
                                                           x0, x1, x2, x3);
 }
 
+// Rows (a) and weights (b, `per` rows of each expert) repacked in one launch, of
+// the weights only those of experts that have rows: the others are not read.
+template <int ELT>
+__global__ __launch_bounds__(256) void expert_repack_kernel(Repack a, Repack b, ExpertArgs x, int per) {
+  const int64_t at = repack_at();
+  if (at >= a.rows + b.rows) return;
+  if (at >= a.rows) {
+    const Segment g = segment(x, (int)((uint32_t)(at - a.rows) / (uint32_t)per) + 1);
+    if (g.begin == g.end) return;
+  }
+  repack_row<ELT>(at < a.rows ? a : b, at < a.rows ? at : at - a.rows);
+}
+
 // Sums of a split product over rows in split order, and the epilogue with the
 // bias of the row's expert: the last one whose rows begin at or before it.
 template <int OP, int ELT>
@@ -423,7 +436,11 @@ hipError_t launch_expert(dattri_linear_op op, int elt, bool aligned, GemmArgs a,
     if (n > 0) {
       dim3 grid;
       if ((e = row_grid((n + 3) / 4, &grid)) != hipSuccess) return e;
-      hipLaunchKernelGGL(elt == 2 ? repack_kernel<2> : repack_kernel<4>, grid, dim3(256), 0, s, ra, rb);
+      if (wgrad)
+        hipLaunchKernelGGL(elt == 2 ? repack_kernel<2> : repack_kernel<4>, grid, dim3(256), 0, s, ra, rb);
+      else
+        hipLaunchKernelGGL(elt == 2 ? expert_repack_kernel<2> : expert_repack_kernel<4>, grid, dim3(256), 0, s, ra, rb, x,
+                           (int)d_out);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
   }

@@ -466,14 +466,13 @@ struct Repack {
   int64_t ld, rows;
   int w, ld_out;
 };
+__device__ inline int64_t repack_at() {  // a wave per row
+  return row_block() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+}
 template <int ELT>
-__global__ __launch_bounds__(256) void repack_kernel(Repack a, Repack b) {
+__device__ DATTRI_INLINE inline void repack_row(const Repack& p, int64_t r) {
   constexpr int U = ELT == 1 ? 2 : 4;  // pieces per lane under way
   const int lane = threadIdx.x & 63;
-  const int64_t at = row_block() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // a wave per row
-  if (at >= a.rows + b.rows) return;
-  const Repack p = at < a.rows ? a : b;
-  const int64_t r = at < a.rows ? at : at - a.rows;
   const uint8_t* const src = p.src + r * p.ld * ELT;
   uint8_t* const dst = p.dst + r * p.ld_out * ELT;
   const int width = p.w * ELT, out = p.ld_out * ELT;
@@ -504,6 +503,12 @@ __global__ __launch_bounds__(256) void repack_kernel(Repack a, Repack b) {
       if (c < out) *(i32x4*)(dst + c) = o;
     }
   }
+}
+template <int ELT>
+__global__ __launch_bounds__(256) void repack_kernel(Repack a, Repack b) {
+  const int64_t at = repack_at();
+  if (at >= a.rows + b.rows) return;
+  repack_row<ELT>(at < a.rows ? a : b, at < a.rows ? at : at - a.rows);
 }
 
 // An operand and where its repacked rows go; updates pointer and stride.

@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from model_util import DT, gen, host, rand
+from model_util import DT, OUT, check, gen, host, product_bound, rand
 from oracle import block as ob
 
 pytestmark = pytest.mark.gpu
@@ -76,3 +76,38 @@ def test_experts_of_the_most_rows():
     y.fill_(7.0)
     m.expert_linear_input_grad(x, w.view(2, 8, 1), off, out=y)
     assert [float(y[k]) for k in (0, 1, -40, -1)] == [8, 32, 48, 64] and int(y.count_nonzero()) == 4
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows", [1, 6, 300])
+def test_weights_that_nothing_meets_stay_where_they_are(rows, dtype):
+    """Widths off 16 bytes are repacked into the workspace, of the weights only those of experts with rows.  All else is
+    NaN, before and after: the other experts' weights and the workspace."""
+    import paper_2609_38767_amd as dt
+    m, g, e, i, o = layers(), gen(rows), 40, 203, 101
+    f = [0] * 9 + [rows // 3] * 20 + [rows] * (e + 1 - 29)  # experts 8 and 28, of one row the latter alone
+    off = torch.tensor(f, dtype=torch.int32, device="cuda")
+    met = [k for k in range(e) if f[k] < f[k + 1]]
+    w = torch.full((e, o, i), float("nan"), dtype=DT[dtype], device="cuda")
+    for k in met:
+        w[k] = rand(g, o, i, dtype=dtype, std=0.1)
+    x, gr = rand(g, rows, i, dtype=dtype), rand(g, rows, o, dtype=dtype)
+    code = dt.DATTRI_F32 if dtype == "f32" else dt.DATTRI_BF16
+    size = w.element_size()
+    for op, a, shape in ((dt.DATTRI_LINEAR_FORWARD, x, (rows, o)), (dt.DATTRI_LINEAR_INPUT_GRAD, gr, (rows, i))):
+        n = dt.dattri_expert_linear_workspace_bytes(op, rows, e, i, o, code, False)
+        ws, y = torch.full((n,), 255, dtype=torch.uint8, device="cuda"), torch.empty(shape, dtype=DT[dtype], device="cuda")
+        if op == dt.DATTRI_LINEAR_FORWARD:
+            dt.dattri_expert_linear(a, 0, w, 0, None, off, 4, dt.DATTRI_ACT_NONE, None, 0, y, 0, None, 0, rows, e, i, o, code,
+                                    ws, n)
+            want, hw = ob.expert_linear(host(a), host(w), f)[0], [host(w[k]).T for k in range(e)]
+        else:
+            dt.dattri_expert_linear_input_grad(a, 0, w, 0, off, 4, None, 0, dt.DATTRI_ACT_NONE, None, 0, None, 0, y, 0, rows, e,
+                                               i, o, code, ws, n)
+            want, hw = ob.expert_input_grad(host(a), host(w), f)[0], [host(w[k]) for k in range(e)]
+        for k in met:
+            s = slice(f[k], f[k + 1])
+            b = product_bound(host(a[s]), hw[k])
+            check(y[s], want[s], b + OUT[dtype] * (np.abs(want[s]) + b), (op, k))
+        wide = -(-i * size // 16) * 16  # of a packed row of the weights
+        assert int((ws != 255).sum()) <= n - (e - len(met)) * o * wide
