@@ -427,8 +427,9 @@ hipError_t launch_expert(dattri_linear_op op, int elt, bool aligned, GemmArgs a,
   }
   if (L.pack_a || L.pack_b) {
     Repack ra = {}, rb = {};
-    if (L.pack_a) ra = repack_of(&a.A, &a.lda, L.a_w, L.a_rows, elt, ws + L.off_a);
-    if (L.pack_b) {
+    // the layout has room for both as soon as one is off 16 bytes
+    if (!on_chunks(a.A, a.lda, L.a_w, elt)) ra = repack_of(&a.A, &a.lda, L.a_w, L.a_rows, elt, ws + L.off_a);
+    if (!on_chunks(a.B, a.ldb, L.b_w, elt)) {
       rb = repack_of(&a.B, &a.ldb, L.b_w, L.b_rows, elt, ws + L.off_b);
       if (!wgrad) x.stride = a.ldb * d_out;
     }

@@ -407,14 +407,17 @@ hipError_t launch_linear8(int elt, bool aligned, GemmArgs a, const Scales8& sc, 
   auto on4 = [&](const void* p, int64_t ld) { return !p || ((uintptr_t)p % (4 * elt) == 0 && ld % 4 == 0); };
   a.vec = on4(a.bias, 0) && on4(a.R, a.ldr) && on4(a.Z, a.ldz) && on4(a.out, a.ldo);
   if (l.pack) {
-    const tile::Repack rx = tile::repack_of(&a.A, &a.lda, a.K, a.M, 1, ws + l.off_x),
-                       rw = tile::repack_of(&a.B, &a.ldb, a.K, a.N, 1, ws + l.off_w);
+    // the layout has room for both as soon as one is off 16 bytes
+    tile::Repack rx = {}, rw = {};
+    const int64_t d_in = a.K;
+    if (!tile::on_chunks(a.A, a.lda, d_in, 1)) rx = tile::repack_of(&a.A, &a.lda, d_in, a.M, 1, ws + l.off_x);
+    if (!tile::on_chunks(a.B, a.ldb, d_in, 1)) rw = tile::repack_of(&a.B, &a.ldb, d_in, a.N, 1, ws + l.off_w);
     dim3 grid;
     hipError_t e = row_grid((rx.rows + rw.rows + 3) / 4, &grid);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(tile::repack_kernel<1>, grid, dim3(256), 0, s, rx, rw);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    a.K = (int)a.lda;
+    a.K = (int)((d_in + 15) / 16 * 16);
   }
   float* part = (float*)(ws + l.off_part);
   return elt == 2 ? launch_product<2>(a, sc, l.g, part, s) : launch_product<4>(a, sc, l.g, part, s);

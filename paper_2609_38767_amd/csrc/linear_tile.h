@@ -511,6 +511,11 @@ __global__ __launch_bounds__(256) void repack_kernel(Repack a, Repack b) {
   repack_row<ELT>(at < a.rows ? a : b, at < a.rows ? at : at - a.rows);
 }
 
+// Whether rows of `w` elements can be read in 16-byte pieces as they are.
+inline bool on_chunks(const void* p, int64_t ld, int64_t w, int elt) {
+  return (uintptr_t)p % 16 == 0 && ld * elt % 16 == 0 && w * elt % 16 == 0;
+}
+
 // An operand and where its repacked rows go; updates pointer and stride.
 inline Repack repack_of(const void** src, int64_t* ld, int64_t w, int64_t rows, int elt, uint8_t* dst) {
   const int ld_out = (int)((w * elt + 15) / 16 * 16 / elt);

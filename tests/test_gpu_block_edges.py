@@ -111,3 +111,56 @@ def test_weights_that_nothing_meets_stay_where_they_are(rows, dtype):
             check(y[s], want[s], b + OUT[dtype] * (np.abs(want[s]) + b), (op, k))
         wide = -(-i * size // 16) * 16  # of a packed row of the weights
         assert int((ws != 255).sum()) <= n - (e - len(met)) * o * wide
+
+
+def off_by_one(t):
+    """t's values, dense, one element behind a place on 16 bytes."""
+    flat = torch.empty(t.numel() + 1, dtype=t.dtype, device=t.device)[1:].view(t.shape)
+    flat.view(torch.uint8 if t.element_size() == 1 else t.dtype).copy_(t.view(torch.uint8) if t.element_size() == 1 else t)
+    assert flat.data_ptr() % 16 != 0
+    return flat
+
+
+def packed(t):
+    return t.numel() // t.shape[-1] * (-(-t.shape[-1] * t.element_size() // 16) * 16)
+
+
+@pytest.mark.parametrize("which", [0, 1], ids=["rows", "weights"])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n", [1, 70, 700])
+def test_only_the_operand_off_16_bytes_is_repacked(n, dtype, which):
+    """The other one is read where it is: its part of the workspace stays as it was, and the results are the same bits."""
+    import paper_2609_38767_amd as dt
+    m, g, e, i, o = layers(), gen(n + which), 5, 208, 112
+    code, t = dt.DATTRI_F32 if dtype == "f32" else dt.DATTRI_BF16, DT[dtype]
+    f = [0, n // 3, n // 3, n // 2, n, n]
+    off = torch.tensor(f, dtype=torch.int32, device="cuda")
+    x, gr, w = rand(g, n, i, dtype=dtype), rand(g, n, o, dtype=dtype), rand(g, e, o, i, dtype=dtype, std=0.1)
+    (x8, sx), (w8, sw) = m.quantize_rows(x), m.quantize_weight(w[0])
+
+    def room(need):
+        return torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    none = dt.DATTRI_ACT_NONE
+    for op, a, b, want in (("fwd", x, w, m.expert_linear(x, w, off)), ("in", gr, w, m.expert_linear_input_grad(gr, w, off)),
+                           ("wgt", gr, x, m.expert_linear_weight_grad(gr, x, off)), ("8", x8, w8, m.linear_8bit((x8, sx), (w8, sw), dtype=t))):
+        if which:
+            b = off_by_one(b)
+        else:
+            a = off_by_one(a)
+        y = torch.full_like(want, float("nan"))
+        if op == "8":
+            need = dt.dattri_linear_scaled_workspace_bytes(n, i, o, code, False)
+            ws = room(need)
+            dt.dattri_linear_scaled(a, 0, sx, 0, b, 0, sw, 0, None, none, None, 0, y, 0, None, 0, n, i, o, code, ws, need)
+        else:
+            need = dt.dattri_expert_linear_workspace_bytes(("fwd", "in", "wgt").index(op), n, e, i, o, code, False)
+            ws = room(need)
+            if op == "fwd":
+                dt.dattri_expert_linear(a, 0, b, 0, None, off, 4, none, None, 0, y, 0, None, 0, n, e, i, o, code, ws, need)
+            elif op == "in":
+                dt.dattri_expert_linear_input_grad(a, 0, b, 0, off, 4, None, 0, none, None, 0, None, 0, y, 0, n, e, i, o, code,
+                                                   ws, need)
+            else:
+                dt.dattri_expert_linear_weight_grad(a, 0, b, 0, off, 4, y, 0, None, False, n, e, i, o, code, ws, need)
+        assert torch.equal(y, want), op
+        assert int((ws != 255).sum()) <= need - packed(a if which else b), op
