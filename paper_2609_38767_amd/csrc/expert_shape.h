@@ -81,10 +81,15 @@ inline ExpertShape expert_shape(bool weight_grad, int64_t rows, int64_t experts,
       }
     }
   }
-  // Few rows whose tiles leave half the CUs without work read the weights slowly: 16 rows, 64 experts of 4096 -> 1024,
-  // 14 of them met, 47 us, in two splits 36; one row, eight of 4096 -> 14336, 42 and 35, the gradient of one row, eight
-  // of 14336 -> 4096, 37 and 27.
-  if (!weight_grad && best.v == kFew && best.splits == 1 && k * elt >= 8192 &&
+  // Few rows whose tiles leave half the CUs without work read the weights slowly, and two splits of k give the others
+  // some; `met` is the most experts that the rows can meet.  us whole and in two splits, 64 experts, weights out of the
+  // caches, rows spread by chance:
+  //   forward of 4096 -> 1024 bf16: 8 rows 38/26, 16 rows (128 tiles) 42/33, 18 rows (144) 44/48, 20 rows 45/52;
+  //   of 16 rows and k -> 1024, bf16: k 768 12.4/12.8, 1024 14.1/14.0, 1280 18.1/15.7, 2048 23.8/19.0; float32: k 256
+  //   10.7/11.6, 512 15.6/14.7, 768 21.2/17.7; input gradients of 1024 <- k bf16: 768 11.5/12.1, 1024 14.1/13.4, 1280
+  //   15.6/14.6, 4096 38/29.
+  // Below 2560 bytes of k a split has too few stages for what its join takes.
+  if (!weight_grad && best.v == kFew && best.splits == 1 && k * elt >= 2560 &&
       std::max((double)met, (double)rows / 32 + 0.5 * met) * ((n + 127) / 128) <= 128.)
     best.splits = 2;
   if (best.splits > 1 && !weight_grad) {  // whole rounds of the buffers

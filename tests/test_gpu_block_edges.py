@@ -5,7 +5,8 @@ import numpy as np
 import pytest
 import torch
 
-from model_util import DT, OUT, check, gen, host, product_bound, rand
+from expert_cuts import FEW
+from model_util import DT, OUT, U, check, gen, host, product_bound, rand
 from oracle import block as ob
 
 pytestmark = pytest.mark.gpu
@@ -164,3 +165,35 @@ def test_only_the_operand_off_16_bytes_is_repacked(n, dtype, which):
                 dt.dattri_expert_linear_weight_grad(a, 0, b, 0, off, 4, y, 0, None, False, n, e, i, o, code, ws, need)
         assert torch.equal(y, want), op
         assert int((ws != 255).sum()) <= need - packed(a if which else b), op
+
+
+def boundaries(n, e, seed):
+    """e experts of very different sizes, every seventh one empty, rows of no expert at both ends."""
+    rng = np.random.default_rng(seed)
+    share = rng.exponential(1.0, e) * (np.arange(e) % 7 != 3)
+    at = n // 50 + np.concatenate([[0.0], np.cumsum(share / share.sum())]) * (n - n // 50 - n // 70)
+    return [int(v) for v in at]
+
+
+def product(op, dtype, n, e, i, o, f, g):
+    """A product over rows with its residual, checked expert by expert (float64 products on the GPU)."""
+    m = layers()
+    off = torch.tensor(f, dtype=torch.int32, device="cuda")
+    a, w = rand(g, n, i if op == 0 else o, dtype=dtype), rand(g, e, o, i, dtype=dtype, std=0.1)
+    r = rand(g, n, o if op == 0 else i, dtype=dtype)
+    got = m.expert_linear(a, w, off, residual=r) if op == 0 else m.expert_linear_input_grad(a, w, off, residual=r)
+    for q, s in ob.expert_rows(f, n):
+        want, b = r[s].double(), 2 * U * r[s].double().abs()
+        if q is not None and s.stop > s.start:
+            x, y = a[s].double(), (w[q].double().t() if op == 0 else w[q].double()).contiguous()
+            b = b + 2 * (x.shape[1] + 8) * U * (x.abs() @ y.abs())
+            want = want + x @ y
+        b = b + 2 * U * want.abs()
+        assert ((got[s].double() - want).abs() <= b + OUT[dtype] * (want.abs() + b)).all(), (q, s)
+
+
+@pytest.mark.parametrize("case", FEW, ids=lambda c: "-".join(map(str, c)))
+def test_few_rows_split_in_two(case):
+    op, dtype, n, e, i, o, _ = case
+    f = boundaries(n, e, FEW.index(case))
+    product(op, dtype, n, e, i, o, f, gen(FEW.index(case)))

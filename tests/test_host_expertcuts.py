@@ -6,6 +6,8 @@ import subprocess
 
 import pytest
 
+from expert_cuts import FEW
+
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 MAIN = r"""
 #include <cstdio>
@@ -55,3 +57,12 @@ def test_tile_rows_of_any_segment(ask):
             k = 3 * sizes.index(n)
             more = rest > tm // 2
             assert [v for v, in got[k:k + 3]] == [full + (rest > 0), full + more, int(rest > 0 and not more)], (n, tm)
+
+
+def cut(ask, cases):
+    return ask([f"e {op} {4 if t == 'f32' else 2} {n} {e} {i} {o}" for op, t, n, e, i, o, *_ in cases])
+
+
+def test_few_rows_split_in_two(ask):
+    assert [(v, splits) for v, splits, _ in cut(ask, FEW)] == [(3, c[6]) for c in FEW]
+    assert {(c[0], c[1], c[6]) for c in FEW} == {(op, t, s) for op in (0, 1) for t in ("f32", "bf16") for s in (1, 2)}
