@@ -9,7 +9,7 @@ backward products are the linear layers of a model of experts; ``linear_8bit``
 is the linear layer of a model whose weights are held in 8 bits, with
 ``rms_norm_8bit`` or ``quantize_rows`` for its rows and ``quantize_weight`` and
 ``transpose_8bit`` for its weights.  All computation happens in libdattri's HIP
-kernels.
+kernels (``transpose_8bit`` only moves values).
 
 Nothing here is differentiated by autograd: results do not require grad whatever
 the inputs do, and the backward products are calls of their own.  Writing into a
@@ -422,11 +422,17 @@ def quantize_weight(weight, stream=None):
 
 def transpose_8bit(weight):
     """The transposed 8-bit weight, with which ``linear_8bit`` carries a gradient
-    back through the layer.  Laid out once, beside the weight."""
+    back through the layer.  Laid out once, beside the weight: torch's copies,
+    which compute nothing, into memory of its own."""
     q, s = weight
     if q.dtype != torch.float8_e4m3fn or q.dim() != 2 or s.shape != (_groups(q.shape[0]), _groups(q.shape[1])):
         raise ValueError("weight must be float8_e4m3fn of two axes with a scale for each 128 x 128 block")
-    return q.view(torch.uint8).t().contiguous().view(torch.float8_e4m3fn), s.t().contiguous()
+    return _transposed(q.view(torch.uint8)).view(torch.float8_e4m3fn), _transposed(s)
+
+
+def _transposed(t):
+    """A dense copy (t() of a single row or column may be t's own memory, dense already)."""
+    return torch.empty((t.shape[1], t.shape[0]), dtype=t.dtype, device=t.device).copy_(t.detach().t())
 
 
 def linear_8bit(x, weight, bias=None, act="none", residual=None, keep_preact=False, dtype=torch.bfloat16, out=None,
