@@ -420,13 +420,19 @@ def quantize_weight(weight, stream=None):
     return q, s
 
 
-def transpose_8bit(weight):
+def transpose_8bit(weight, stream=None):
     """The transposed 8-bit weight, with which ``linear_8bit`` carries a gradient
     back through the layer.  Laid out once, beside the weight: torch's copies,
     which compute nothing, into memory of its own."""
     q, s = weight
     if q.dtype != torch.float8_e4m3fn or q.dim() != 2 or s.shape != (_groups(q.shape[0]), _groups(q.shape[1])):
         raise ValueError("weight must be float8_e4m3fn of two axes with a scale for each 128 x 128 block")
+    if q.is_cuda or s.is_cuda or stream is not None:
+        _on_gpu(q, s)
+        ctx = _elsewhere(q, stream)
+        if ctx is not None:
+            with ctx:
+                return transpose_8bit(weight)
     return _transposed(q.view(torch.uint8)).view(torch.float8_e4m3fn), _transposed(s)
 
 

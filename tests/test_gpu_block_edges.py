@@ -197,3 +197,30 @@ def test_few_rows_split_in_two(case):
     op, dtype, n, e, i, o, _ = case
     f = boundaries(n, e, FEW.index(case))
     product(op, dtype, n, e, i, o, f, gen(FEW.index(case)))
+
+
+# ------------------------------------------------------ the transposed weight
+@pytest.mark.parametrize("o,i", [(1, 200), (300, 1), (264, 520)])
+def test_transposed_weight_on_a_stream_and_in_a_graph(o, i):
+    m, g = layers(), gen(o)
+    q, s = m.quantize_weight(rand(g, o, i))
+    want = q.view(torch.uint8).t().clone(), s.t().clone()
+
+    def same(w):
+        return torch.equal(w[0].view(torch.uint8), want[0]) and torch.equal(w[1], want[1]) and w[0].is_contiguous()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = [m.transpose_8bit((q, s), stream=v) for v in (side, side.cuda_stream, 0)]
+    torch.cuda.synchronize()
+    assert all(same(w) for w in got)
+    with pytest.raises(ValueError, match="on the GPU"):
+        m.transpose_8bit((q, s.cpu()))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        w = m.transpose_8bit((q, s))
+    for k in range(3):
+        q.view(torch.uint8).bitwise_xor_(k + 1)
+        s.mul_(2)
+        want = q.view(torch.uint8).t().clone(), s.t().clone()
+        graph.replay()
+        assert same(w)
