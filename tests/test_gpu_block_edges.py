@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from expert_cuts import FEW
+from expert_cuts import BIG, FEW, PADDED
 from model_util import DT, OUT, U, check, gen, host, product_bound, rand
 from oracle import block as ob
 
@@ -197,6 +197,111 @@ def test_few_rows_split_in_two(case):
     op, dtype, n, e, i, o, _ = case
     f = boundaries(n, e, FEW.index(case))
     product(op, dtype, n, e, i, o, f, gen(FEW.index(case)))
+
+
+@pytest.mark.parametrize("case", BIG, ids=lambda c: "-".join(map(str, c)))
+def test_largest_tiles_of_many_experts(case):
+    """Tile rows, whole and half ones, of segments behind the first 64."""
+    op, dtype, n, e, i, o = case
+    f = boundaries(n, e, BIG.index(case))
+    left = {(b - a) % 256 for a, b in zip(f[62:], f[63:])}
+    assert any(0 < v <= 128 for v in left) and any(v > 128 for v in left)
+    product(op, dtype, n, e, i, o, f, gen(50 + BIG.index(case)))
+
+
+def test_boundaries_out_of_order_in_the_largest_tiles():
+    """Offsets that no caller should pass: whatever comes out, nothing outside the outputs is written."""
+    m, g = layers(), gen(60)
+    _, dtype, n, e, i, o = BIG[0]
+    f = torch.tensor(boundaries(n, e, 0))
+    rng = torch.Generator().manual_seed(1)
+    x, w, gr = rand(g, n, i, dtype=dtype), rand(g, e, o, i, dtype=dtype), rand(g, n, i, dtype=dtype)
+    wt = rand(g, e, i, o, dtype=dtype)
+    for off in (f.flip(0), f[torch.randperm(e + 1, generator=rng)], torch.tensor([0, n] * (e // 2) + [0]),
+                f * 1000003 - n, torch.full((e + 1,), 1 << 40), f - (1 << 40)):
+        off = off.cuda()
+        out = torch.full((n + 2, o), 7.0, dtype=DT[dtype], device="cuda")
+        m.expert_linear(x, w, off, out=out[1:-1])
+        assert (out[0] == 7).all() and (out[-1] == 7).all()
+        out.fill_(7.0)
+        m.expert_linear_input_grad(gr, wt, off, out=out[1:-1])
+        assert (out[0] == 7).all() and (out[-1] == 7).all()
+
+
+@pytest.mark.parametrize("pad", [3, 4])
+@pytest.mark.parametrize("case", PADDED, ids=lambda c: "-".join(map(str, c)))
+def test_padded_weight_gradients(case, pad):
+    """As the dense gradient, bit for bit; what lies between its rows stays."""
+    dtype, n, e, i, o, _, _ = case
+    m, g = layers(), gen(n + pad)
+    f = boundaries(n, e, n)
+    off = torch.tensor(f, device="cuda")
+    gr, x = rand(g, n, o, dtype=dtype), rand(g, n, i, dtype=dtype)
+    dense = m.expert_linear_weight_grad(gr, x, off)
+    wide = torch.full((e * o, i + pad), 7.0, device="cuda")
+    out = wide[:, :i].unflatten(0, (e, o))
+    assert m.expert_linear_weight_grad(gr, x, off, out=out) is out
+    assert torch.equal(out, dense) and (wide[:, i:] == 7).all()
+    w0 = rand(g, e, o, i)
+    dense, out[:] = w0.clone(), w0
+    m.expert_linear_weight_grad(gr, x, off, out=dense, accumulate=True)
+    m.expert_linear_weight_grad(gr, x, off, out=out, accumulate=True)
+    assert torch.equal(out, dense) and (wide[:, i:] == 7).all()
+
+
+# ------------------------------------------------------ strides of 8-bit outputs
+class Padded:
+    """Bytes and scales in padded rows, `offset` bytes into their buffer; all of it 0xA5 (and 7) at first."""
+
+    def __init__(self, n, srows, d, offset, pad, spad):
+        k = -(-d // 128)
+        self.bytes = torch.full((offset + n * (d + pad) + 8,), 0xA5, dtype=torch.uint8, device="cuda")
+        self.q = self.bytes[offset:offset + n * (d + pad)].view(n, d + pad)
+        self.s = torch.full((srows + 1, k + spad), 7.0, device="cuda")
+        self.n, self.d, self.k, self.offset = n, d, k, offset
+        self.ld_q, self.ld_s = d + pad, k + spad
+
+    def holds(self, q, s):
+        """The values and scales of the oracle, and nothing else was written."""
+        assert np.array_equal(host(self.s[:-1, :self.k]), s)
+        assert np.array_equal(host(self.q[:, :self.d].contiguous().view(torch.float8_e4m3fn)), q)
+        assert (self.q[:, self.d:] == 0xA5).all() and (self.bytes[:self.offset] == 0xA5).all()
+        assert (self.bytes[-8:] == 0xA5).all() and (self.s[-1] == 7).all() and (self.s[:, self.k:] == 7).all()
+
+
+PLACES = [(0, 0, 1), (1, 3, 0), (4, 4, 2), (8, 8, 1), (2, 16, 3)]  # offset and padding of the bytes, padding of the scales
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("offset,pad,spad", PLACES)
+@pytest.mark.parametrize("n,d", [(1, 1), (9, 64), (5, 128), (33, 264), (3, 769), (2049, 513), (130, 1024), (3, 4096), (2, 33024),
+                                 (2, 66048), (2, 70001)])
+def test_strides_of_8bit_rows(n, d, offset, pad, spad, dtype):
+    """The norm of rows of +-1, which is +-w (the sums are whole numbers, their mean 1), and quantize_rows of it."""
+    import paper_2609_38767_amd as dt
+    g, code = gen(d + offset), dt.DATTRI_F32 if dtype == "f32" else dt.DATTRI_BF16
+    w = rand(g, d, dtype=dtype)
+    x = (torch.randint(0, 2, (n, 1), generator=g, device="cuda") * 2 - 1).to(DT[dtype]).expand(n, d).contiguous()
+    y = x * w
+    want = ob.quantize(host(y))
+    p = Padded(n, n, d, offset, pad, spad)
+    dt.dattri_rms_norm(x, 0, None, 0, w, 0.0, None, 0, None, 0, p.q, p.ld_q, p.s, p.ld_s, n, d, code)
+    p.holds(*want)
+    p = Padded(n, n, d, offset, pad, spad)
+    dt.dattri_quantize_rows(y, 0, n, d, code, p.q, p.ld_q, p.s, p.ld_s)
+    p.holds(*want)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("offset,pad,spad", PLACES)
+@pytest.mark.parametrize("o,i", [(1, 1), (128, 128), (129, 300), (300, 1040)])
+def test_strides_of_8bit_weights(o, i, offset, pad, spad, dtype):
+    import paper_2609_38767_amd as dt
+    g, code = gen(o + offset), dt.DATTRI_F32 if dtype == "f32" else dt.DATTRI_BF16
+    w = rand(g, o, i, dtype=dtype)
+    p = Padded(o, -(-o // 128), i, offset, pad, spad)
+    dt.dattri_quantize_weight(w, 0, o, i, code, p.q, p.ld_q, p.s, p.ld_s)
+    p.holds(*ob.quantize(host(w), 128))
 
 
 # ------------------------------------------------------ the transposed weight

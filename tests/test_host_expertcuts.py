@@ -6,7 +6,7 @@ import subprocess
 
 import pytest
 
-from expert_cuts import FEW
+from expert_cuts import BIG, FEW, PADDED
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 MAIN = r"""
@@ -66,3 +66,13 @@ def cut(ask, cases):
 def test_few_rows_split_in_two(ask):
     assert [(v, splits) for v, splits, _ in cut(ask, FEW)] == [(3, c[6]) for c in FEW]
     assert {(c[0], c[1], c[6]) for c in FEW} == {(op, t, s) for op in (0, 1) for t in ("f32", "bf16") for s in (1, 2)}
+
+
+def test_largest_tiles_of_many_experts(ask):
+    assert [v for v, _, _ in cut(ask, BIG)] == [0] * len(BIG)
+    assert all(c[3] + 2 > 64 for c in BIG)  # segments: more than a wave has lanes
+
+
+def test_padded_weight_gradients(ask):
+    got = ask([f"e 2 {4 if t == 'f32' else 2} {n} {e} {i} {o}" for t, n, e, i, o, _, _ in PADDED])
+    assert [(["256x256", "128x128", "64x128"][v], splits > 1) for v, splits, _ in got] == [c[5:] for c in PADDED]
