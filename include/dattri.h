@@ -933,12 +933,14 @@ dattri_status dattri_quantize_weight(const void* W, int64_t ld_w, int64_t d_out,
 /* Linear layer of 8-bit rows and weights with their scales:
  *   Z[m][n] = sum over groups b of SX[m][b] SW[n / 128][b] sum over k in b of
  *             X[m][k] W[n][k]  + bias[n],   Y = act(Z) + R.
- * The scales multiply each group's float32 sum.  Float32 results: products and
- * sums are float32.  bf16 results: of eight products of neighbouring k (from a
- * multiple of 8) each loses the bits below 2^-13 of the largest one's power of
- * two, as the 8-bit matrix instructions add them; all other sums are float32.  The
- * gradient of the layer's input is the same call with the transposed weight:
- * its bytes and its scales transposed, rows of the gradient in 8 bits.
+ * The scales multiply each group's float32 sum as one float32 product, which
+ * loses bits below 2^-126 and is infinite past float32's range.  Float32
+ * results: products and sums are float32.  bf16 results: of eight products of
+ * neighbouring k (from a multiple of 8) each loses the bits below 2^-13 of the
+ * largest one's power of two, as the 8-bit matrix instructions add them; all
+ * other sums are float32.  The gradient of the layer's input is the same call
+ * with the transposed weight: its bytes and its scales transposed, rows of the
+ * gradient in 8 bits.
  *   X: device [rows of d_in] e4m3, SX: device float32 [rows of ceil(d_in/128)],
  *   W: device [d_out rows of d_in] e4m3, SW: device float32 [ceil(d_out/128)
  *   rows of ceil(d_in/128)]; bias, R, Y, Z as for dattri_linear, of dtype.

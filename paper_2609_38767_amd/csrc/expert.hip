@@ -12,11 +12,15 @@
 // each other, so wrong ones give wrong rows, never an access out of range.
 //
 // What bounds it: the matrix cores, as the linear layers' products, and the last
-// round of tiles.  Eight experts of 4096 -> 14336, 16384 rows, bf16: forward 1728 us
-// (1.11 PFLOP/s; with experts of equal size 1593, one dense layer 1554), input
-// gradient 1698, weight gradient 1670; 64 experts of 4096 -> 1024, 32768 rows:
-// 365, equal experts 269.  Few rows: memory.  16 rows that meet 14 experts of
-// 4096 -> 14336 298 us, 5.5 TB/s of those experts' weights.
+// round of tiles, whose prologue and epilogue overlap nothing.  bf16, over several
+// sets of row counts: eight experts of 4096 -> 14336, 16384 rows: forward 1570 to
+// 1615 us (1.2 PFLOP/s; with experts of equal size 1535, one dense layer 1490),
+// input gradient 1710 to 1750 alone, 1820 to 1880 with a residual and a slope
+// (equal 1555 alone), weight gradient 1690 (equal 1665); 64 experts of 4096 -> 1024,
+// 32768 rows, with bias, silu and the kept pre-activation: 365 to 417, for 2.2 to
+// 2.3 rounds of tiles take 2.5 or 3 (equal experts, two rounds, 299).  Few rows:
+// memory.  16 rows that meet 14 experts of 4096 -> 14336 298 us, 5.5 TB/s of those
+// experts' weights.
 #include <algorithm>
 
 #include "api_common.h"

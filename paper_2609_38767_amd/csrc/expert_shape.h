@@ -44,8 +44,12 @@ constexpr bool expert_splits(Variant v, int elt) { return v != kBig && !(v == kS
 // 769 -> 1030, 1531 rows: 284/75/50/50; one of 3232 -> 392, 28 rows, without a
 // split: 64 in 32 x 128.
 // float32 weight gradients leave out 256 x 256 (3% more at most) and take 64 x 128
-// too: five experts of 769 -> 1030, 1531 rows, 50 us, in 128 x 128 64; bf16 ones
-// would gain little there (24 and 27) and lose elsewhere.
+// too; bf16 ones would gain little there (24 and 27) and lose elsewhere.  us in 128
+// x 128 / 64 x 128, * the model's choice: 1531 rows, five experts of 769 -> 1030
+// 67/49*, one 52/61*, 16 of 1536 -> 1536 96*/98; 6000 rows, five of 512 -> 2048
+// 179/108*, one 112*/180, 32 153*/136, eight of 256 -> 300 30/48*; 300 rows, 32 of
+// 1536 -> 1536 109*/121.  Of 108 sizes (1 to 32 experts, 300 to 6000 rows, six
+// pairs of widths) it was within 6% of the better of the two in 91.
 inline ExpertShape expert_shape(bool weight_grad, int64_t rows, int64_t experts, int64_t m, int64_t n, int64_t k,
                                 int elt, bool bc) {
   const double rate[4] = {elt == 2 ? 5.2e6 : 0.58e6, elt == 2 ? 3.4e6 : 0.565e6, elt == 2 ? 2.4e6 : 0.5e6,

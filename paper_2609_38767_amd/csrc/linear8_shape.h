@@ -36,14 +36,15 @@ inline Shape8 shape8(int64_t M, int64_t N, int64_t K, int elt) {
     return g;
   };
   // Without tiles every 16 weight rows read all rows of X again.  us without and with tiles, weights out of the caches:
-  // 4096 -> 14336 one row 14.6/16.5, four 16.3/16.6, eight 17.9/16.4, sixteen 22.5/16.7; 14336 -> 4096 eight 18.1/16.9
-  // (float32 18.3/18.0); 8192 -> 4096, 34M weights, eight 11.0/13.3, sixteen 13.3/13.7.
+  // 4096 -> 14336 one row 14.4/16.3, four 16.3/16.3, seven 17.2/16.5 (float32 18.1/17.7), eight 17.8/16.5, sixteen
+  // 22.4/16.7; 14336 -> 4096 seven 17.8/17.0 (float32 17.9/18.4), eight 18.0/16.9; 8192 -> 4096, 34M weights, eight
+  // 11.1/13.3, sixteen 13.3/13.8; 4096 -> 4096 one row 6.2/10.7.
   if (M < 8 || (M <= 16 && N * K < 40000000)) return cut(kFew, 1);
-  // One workgroup per CU, whose ring keeps 75 KB of loads under way: 64 x 4096 -> 14336 17.3 us in two splits, 17.8
-  // whole, 22.5 in six; 64 x 14336 -> 4096 17.8 in eight, 46.2 whole.  With half the CUs at work splits of eight groups
-  // of k or more do (weights out of the caches: 64 x 4096 -> 4096 14.0 us in four, 15.1 in eight; 64 x 8192 -> 2048 14.3
-  // in eight, 15.3 in sixteen; but 64 x 4096 -> 1024 12.0 in four, 10.9 in eight), and eight groups stay whole (64 x
-  // 1024 -> 4096 8.5, in two 9.7).
+  // One workgroup per CU, whose ring keeps 75 KB of loads under way (weights out of the caches): 64 x 4096 -> 14336 20.1
+  // us in two splits, 25.0 whole, 26.5 in six; 64 x 14336 -> 4096 20.4 in eight, 26.2 in four, 69.6 whole.  With half
+  // the CUs at work splits of eight groups of k or more do (64 x 4096 -> 4096 14.0 us in four, 14.9 in eight; 64 x
+  // 8192 -> 2048 14.3 in eight, 15.3 in sixteen; but 64 x 4096 -> 1024 11.9 in four, 10.8 in eight), and eight groups
+  // stay whole (64 x 1024 -> 4096 8.5, in two 9.7).
   if (M <= 64) {
     const int64_t strips = (N + 127) / 128;
     return cut(kSlim, stages <= 8 ? 1 : std::min<int64_t>({64, 256 / strips, std::max<int64_t>(128 / strips, stages / 8)}));

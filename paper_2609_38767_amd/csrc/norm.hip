@@ -11,10 +11,12 @@
 // wave's piece, so its largest magnitude is one reduction over 16, 32 or 64 lanes.
 //
 // What bounds it: memory.  16384 rows of 4096 bf16: sum, norm and 8 bits 72 us
-// (471 MB, 6.5 TB/s), gradients 87 + 5 (537 MB, 6.2); 65536 rows of 128 12.1 us
+// (471 MB, 6.5 TB/s), gradients 89 + 5 (537 MB, 6.0); 65536 rows of 128 12.1 us
 // (67 MB); 8192 rows of 4099, most of them off 16 bytes, 54 us (5.0 TB/s), the
 // gradients 67.  One row of 4096 2.1 us: the launch.  Rows that no registers hold
 // are read twice: 4096 of 40000 float32 834 us, 3.9 TB/s of what it then moves.
+// Times of variants below are of kernels alone, measured in turn: between runs the
+// gradient's kernel moves from 83 to 89 us, so each is to be read beside its pair.
 #include <algorithm>
 #include <type_traits>
 
@@ -348,8 +350,8 @@ __global__ __launch_bounds__(T <= 64 ? 256 : T) void norm_grad_kernel(NormGradAr
     const float u = T < 64 && row0 + p.sub >= a.rows ? 0.f : 1.f / sqrtf(s[0] / a.d + a.eps), k = u * u * (s[1] / a.d);
     if (row0 >= a.rows) continue;  // rows of the wave that are not there are zeros, and are not written
     const auto out = p.buffer(a.D, row0, a.ldd, a.rows);
-    // 1024 threads: the floats of before are formed again rather than kept, for bf16 takes half the registers
-    // (fewer threads: 16384 rows of 4096 in 73 us kept, 80 formed again)
+    // 1024 threads: the floats of before are formed again rather than kept, for bf16 takes half the registers (4096 rows
+    // of 16384 with the joining of dW 118 us, kept 211; with 256 threads, 16384 rows of 4096, 99.6 and 93.0)
     if constexpr (T == 1024)
 #pragma unroll
       for (int c = 0; c < C; ++c) asm volatile("" : "+v"(rg[c]), "+v"(rh[c]), "+v"(rw[c]));
