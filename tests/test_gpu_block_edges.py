@@ -114,6 +114,36 @@ def test_weights_that_nothing_meets_stay_where_they_are(rows, dtype):
         assert int((ws != 255).sum()) <= n - (e - len(met)) * o * wide
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_other_experts_are_met_in_a_replay(dtype):
+    """Widths off 16 bytes in a captured graph whose boundaries and weights change: what is repacked follows them."""
+    m, g = layers(), gen(77)
+    n, e, i, o = 60, 12, 203, 101
+    x, gr, w = rand(g, n, i, dtype=dtype), rand(g, n, o, dtype=dtype), rand(g, e, o, i, dtype=dtype, std=0.1)
+    off = torch.zeros(e + 1, dtype=torch.int64, device="cuda")
+
+    def run():
+        return m.expert_linear(x, w, off), m.expert_linear_input_grad(gr, w, off)
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = run()
+    for f in ([0] + [30] * 6 + [60] * 6, [0] * 8 + [1] + [60] * 4, list(range(0, 61, 5)), [0] * 13):
+        off.copy_(torch.tensor(f))
+        w.mul_(-0.75)
+        graph.replay()
+        want = run()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), f
+        for k, at in ob.expert_rows(f, n):
+            for y, a, b in ((want[0], x, w.transpose(1, 2)), (want[1], gr, w)):
+                if k is None:
+                    assert not y[at].any()
+                else:
+                    e64 = product_bound(host(a[at]), host(b[k]))
+                    check(y[at], host(a[at]) @ host(b[k]), e64 + OUT[dtype] * (np.abs(host(a[at]) @ host(b[k])) + e64), (f, k))
+
+
 def off_by_one(t):
     """t's values, dense, one element behind a place on 16 bytes."""
     flat = torch.empty(t.numel() + 1, dtype=t.dtype, device=t.device)[1:].view(t.shape)
