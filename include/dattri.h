@@ -825,7 +825,8 @@ typedef DATTRI_ENUM {
 
 /* Device bytes of workspace a call of `op` needs (0 is possible).  aligned:
  * nonzero if both operands of the product have 16-byte aligned pointers and
- * row strides of a multiple of 16 bytes (with 0 the size is enough for either).
+ * row strides of a multiple of 16 bytes (with 0 the size is enough for either,
+ * and a bias gradient alone has no operands: either value will do).
  * Errors: INVALID_ARG, DTYPE, UNSUPPORTED. */
 dattri_status dattri_linear_workspace_bytes(dattri_linear_op op, int64_t rows, int64_t d_in,
                                             int64_t d_out, dattri_dtype dtype, int32_t aligned,

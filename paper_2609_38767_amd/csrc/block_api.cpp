@@ -390,7 +390,7 @@ dattri_status dattri_expert_linear_weight_grad(const void* G, int64_t ld_g, cons
   TRY(check_rows("dW", dW, &ld_dw, experts * d_out, d_in, 4, false));
   TRY(check_bias("dbias", dbias, 4));
   if (!dW && !dbias) return fail(DATTRI_E_INVALID_ARG, "nothing to compute: dW and dbias are NULL");
-  const bool aligned = on_16(G, ld_g, X, ld_x, elt);
+  const bool aligned = !dW || on_16(G, ld_g, X, ld_x, elt);  // bias alone: no operands
   const size_t need = expert_workspace_need(DATTRI_LINEAR_WEIGHT_GRAD, rows, experts, d_in, d_out, elt, aligned);
   TRY(check_workspace(workspace, ws_bytes, need));
   {

@@ -216,7 +216,7 @@ dattri_status dattri_linear_weight_grad(const void* G, int64_t ld_g, const void*
   TRY(check_rows("dW", dW, &ld_dw, d_out, d_in, 4, false));
   if ((uintptr_t)dbias % 4) return fail(DATTRI_E_INVALID_ARG, "dbias is not aligned to its elements");
   if (!dW && !dbias) return fail(DATTRI_E_INVALID_ARG, "nothing to compute: dW and dbias are NULL");
-  const bool aligned = on_16(G, ld_g, X, ld_x, elt);
+  const bool aligned = !dW || on_16(G, ld_g, X, ld_x, elt);  // bias alone: no operands
   const size_t need = linear_workspace_need(DATTRI_LINEAR_WEIGHT_GRAD, rows, d_in, d_out, elt, aligned);
   TRY(check_workspace(workspace, ws_bytes, need));
   {

@@ -279,6 +279,29 @@ def test_padded_weight_gradients(case, pad):
     assert torch.equal(out, dense) and (wide[:, i:] == 7).all()
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,e,i,o,offset", [(300, 4, 203, 96, 0), (5000, 2, 203, 101, 1), (0, 3, 9, 16, 0)])
+def test_bias_gradients_alone(n, e, i, o, offset, dtype):
+    """Without a weight gradient there are no operands of a product: the workspace of aligned ones is enough."""
+    import paper_2609_38767_amd as dt
+    g, code = gen(n + i), dt.DATTRI_F32 if dtype == "f32" else dt.DATTRI_BF16
+    gr = rand(g, n, o, dtype=dtype, offset=offset)
+    f = boundaries(n, e, n)
+    off = torch.tensor(f, device="cuda")
+    want = np.stack([host(gr[s]).sum(0) for k, s in ob.expert_rows(f, n) if k is not None])
+    bound = 2 * (n + 8) * U * np.stack([np.abs(host(gr[s])).sum(0) for k, s in ob.expert_rows(f, n) if k is not None])
+    db = torch.full((e, o), 7.0, device="cuda")
+    need = dt.dattri_expert_linear_workspace_bytes(dt.DATTRI_LINEAR_WEIGHT_GRAD, n, e, i, o, code, True)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    dt.dattri_expert_linear_weight_grad(gr, 0, None, 0, off, 8, None, 0, db, False, n, e, i, o, code, ws, need)
+    check(db, want, bound)
+    db = torch.full((o,), 7.0, device="cuda")
+    need = dt.dattri_linear_workspace_bytes(dt.DATTRI_LINEAR_WEIGHT_GRAD, n, i, o, code, True)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    dt.dattri_linear_weight_grad(gr, 0, None, 0, None, 0, db, False, n, i, o, code, ws, need)
+    check(db, host(gr).sum(0), 2 * (n + 8) * U * np.abs(host(gr)).sum(0))
+
+
 # ------------------------------------------------------ strides of 8-bit outputs
 class Padded:
     """Bytes and scales in padded rows, `offset` bytes into their buffer; all of it 0xA5 (and 7) at first."""
